@@ -369,6 +369,106 @@ pd_status pd_quantize_fp8_blocks(const void* w, int32_t ldw, int32_t n, int32_t 
 pd_status pd_gemm_fp8_blockwise(const void* a_codes, const float* a_scales, const void* b_codes, const float* b_scales,
                                 void* c, int32_t m, int32_t n, int32_t k, int32_t* err_word, void* stream);
 
+/* h = x + residual, RMSNorm and FP8 codes of a row in one pass: the step between two projections of a layer whose
+ * projections take block-wise (pd_gemm_fp8_blockwise) or per-row (pd_gemm_fp8) FP8 operands (reading of the paper's FP8
+ * deployment, Evaluation section).
+ *   h = bf16(x + residual),  n = h * rsqrt(mean(h^2) + eps) * gain  (fp32, from the rounded h),
+ *   s = max|n| / 448 (1 for an all-zero block; never below the smallest normal float),  code = E4M3(n / s)
+ * with one s per row and 128 channels (group = 128, d a multiple of 128) or per row (group = 0, d a multiple of 16).  The
+ * codes are those of the fp32 n: there is no bf16 rounding between the norm and the quantiser.
+ *   x, residual   device bf16 [rows, d], row pitches ldx and ldr elements (multiples of 8); residual may be NULL (h = x)
+ *   gain          device bf16 [d]
+ *   sum_out       h, device bf16 [rows, d] contiguous, or NULL; may alias x or residual where that one's pitch is d
+ *   norm_out      n rounded to bf16, device [rows, d] contiguous, or NULL
+ *   codes, scales device uint8 [rows, d] and fp32 [rows, d / 128] or [rows], contiguous; codes may be NULL if norm_out is
+ *                 not (scales is then not used)
+ * Tensors start on 16-byte boundaries; d at most 16384.  A row with a non-finite h has non-finite results, visibly: NaN
+ * values and codes.  The squares of a row are summed
+ * in fp32, whose range (a sum of 3e38) they must not leave.  Enqueues one kernel; rows = 0 does nothing. */
+pd_status pd_add_rmsnorm_fp8(const void* x, int32_t ldx, const void* residual, int32_t ldr, const void* gain, float eps,
+                             int32_t rows, int32_t d, int32_t group, void* sum_out, void* norm_out, void* codes,
+                             float* scales, void* stream);
+
+/* ------------------------------------------------------ 8-bit paged KV cache */
+
+/* KV cache of fixed-size pages in 8 bits (the paper hands the KV cache of a request from a prefill to a decode instance and
+ * keeps it there for the request's life; pages let requests of any length share one pool, and 8 bits halve what is moved,
+ * kept and read.  The paper fixes no cache format).
+ *   k_codes, v_codes    device uint8 (E4M3) [n_pages, Hkv, page_len, hd], 16-byte aligned
+ *   k_scales, v_scales  device fp32 [n_pages, Hkv]: one scale per page and head, a power of two 2^e, e in -117 .. 120
+ *   page_table          device int32 [n_seqs, table_ld]: position p of sequence s lies in page page_table[s][p / page_len],
+ *                       row p % page_len.  Entries of pages that hold no token are not read.
+ *   page_len            16, 32, 64 or 128;  table_ld * page_len below 2^31
+ * value = E4M3(code) * scale.  The scale of a page is the smallest power of two with max|value| <= 448 * scale over the
+ * tokens appended since the page's first row was last written; it only grows until then.  A power of two, so that codes
+ * move to a larger scale without rounding (but for values that become subnormal codes) however many times the scale
+ * grows, and decode to bf16 exactly; the relative precision of E4M3 does not depend on the scale.
+ * All buffers are the caller's; they need no initialisation.  A sequence's pages are its own while it is appended to; full
+ * pages may be shared for reading. */
+typedef struct {
+  uint32_t struct_size;
+  void* k_codes;
+  void* v_codes;
+  float* k_scales;
+  float* v_scales;
+  const int32_t* page_table;
+  int32_t n_pages, page_len, n_seqs, table_ld;
+} pd_paged_kv_cache;
+
+/* The (cos, sin) table of the rotary position embedding that the layer calls use, for pd_paged_kv_append: host fp32
+ * [max_pos, hd / 2, 2], cos and sin of pos * rope_theta^(-2 i / hd), angles in double.  Uses head_dim, rope_theta and
+ * max_pos of cfg.  Host only. */
+pd_status pd_rope_table(const pd_layer_cfg* cfg, float* table_host);
+
+/* Rotates fresh q and k heads to their positions and appends k and v to the cache.
+ *   qkv          device bf16 [T, ldqkv]: q heads, k heads, v heads of a row as the QKV projection leaves them (before the
+ *                rotation); ldqkv a multiple of 8
+ *   q_out        rotated q, device bf16 [T, Hq*hd] contiguous; NULL: only the cache is written
+ *   rope_tab     device fp32 [max_pos, hd / 2, 2] (pd_rope_table)
+ *   cu_seqlens   as for pd_prefill_layer (device and host copy); both NULL: one row per request (a decode step)
+ *   kv_len_dev   device int32[n_req]: tokens that sequence r holds already; its rows take positions kv_len[r],
+ *                kv_len[r] + 1, ...  A negative value leaves the request out (padding of a captured batch): none of its rows
+ *                is read, written or cached.  kv_len itself is not modified.
+ *   err_word     optional device int32, set to 2 where a row has no place: a position beyond the table, or a page
+ *                number outside the pool (q is still written, k and v are left out); a position beyond max_pos (the row is left out)
+ * k is rotated in fp32 and rounded once, to its code.  An infinite or NaN element is stored as NaN and takes no part in
+ * the scale.  Rows of a page behind the last appended token are left as they were: appending at an earlier position again
+ * replaces the tokens from there on (the scale stays as large as it was unless the page is begun again).  Two requests of
+ * one call must not append to the same page.  Only enqueues work; one kernel; no workspace. */
+pd_status pd_paged_kv_append(const pd_layer_cfg* cfg, const void* qkv, int32_t ldqkv, void* q_out, const float* rope_tab,
+                             const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, int32_t n_req,
+                             const int32_t* kv_len_dev, const pd_paged_kv_cache* cache, int32_t* err_word, void* stream);
+
+/* pd_decode_attention over the 8-bit paged cache: sequence b attends to entries 0 .. kv_len[b] of page_table row b.
+ *   q, out        device bf16 [B, ldq] / [B, Hq*hd], q 16-byte aligned, ldq a multiple of 8
+ *   kv_len_dev    device int32[B]; a sequence with kv_len[b] < 0 gets an all-zero row; entries beyond the table are left out
+ *   max_kv_len    host upper bound of kv_len[b] + 1, at most table_ld * page_len (it sizes the split of the key range; a
+ *                 longer sequence is still computed whole)
+ *   workspace     at least pd_paged_decode_attention_workspace_bytes() bytes, 256-byte aligned (may be NULL where that is
+ *                 0); calls that can overlap on the GPU, captured graphs included, need one each
+ *   err_word      optional device int32, set to 2 where kv_len reaches past the table or a page number lies outside the
+ *                 pool (the keys of such a page are left out)
+ * Only the head counts and head_dim of cfg are used.  Only enqueues work. */
+pd_status pd_paged_decode_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t B, int32_t max_kv_len,
+                                                    size_t* out_bytes);
+pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int32_t ldq, void* out,
+                                    const int32_t* kv_len_dev, int32_t B, int32_t max_kv_len,
+                                    const pd_paged_kv_cache* cache, void* workspace, size_t workspace_bytes,
+                                    int32_t* err_word, void* stream);
+
+/* pd_prefill_attention over the 8-bit paged cache: row t of request r is the query at position prefix[r] + t and attends to
+ * positions 0 .. prefix[r] + t of page_table row r (its own tokens must have been appended).  Arguments as there; the cached
+ * pages are decoded (exactly) to bf16 in the workspace, at least pd_paged_prefill_attention_workspace_bytes() bytes for the
+ * longest prefix[r] + len_r, 256-byte aligned, not shared by calls that can overlap.  err_word: 1 if a bounded wait gave
+ * up, 2 if a page number lies outside the pool (the output of that request is then not meaningful). */
+pd_status pd_paged_prefill_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t n_req, int32_t max_kv_len,
+                                                     size_t* out_bytes);
+pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const void* q, int32_t ldq, void* out,
+                                     const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, int32_t n_req,
+                                     const int32_t* prefix_dev, const int32_t* prefix_host,
+                                     const pd_paged_kv_cache* cache, void* workspace, size_t workspace_bytes,
+                                     int32_t* err_word, void* stream);
+
 /* Failure-detection test hook.  Every wait inside the tensor-core kernels (on a tile load, an accumulator, a
  * partner block) is bounded by wall clock (4 s); when a wait gives up, the block raises its abort flag, leaves
  * through the normal teardown (tensor memory freed, cluster barrier of a CTA pair passed) and sets the error
@@ -393,7 +493,8 @@ int64_t pd_launch_count(void);
 #define PD_TRACE_CLASSES 16
 enum {
   PD_K_GEMM_QKV = 0, PD_K_GEMM_O = 1, PD_K_GEMM_GATE_UP = 2, PD_K_GEMM_DOWN = 3, PD_K_ATTN_PREFILL = 4,
-  PD_K_ATTN_DECODE = 5, PD_K_RMSNORM = 6, PD_K_EMBED = 7, PD_K_LM_HEAD = 8, PD_K_SAMPLE = 9
+  PD_K_ATTN_DECODE = 5, PD_K_RMSNORM = 6, PD_K_EMBED = 7, PD_K_LM_HEAD = 8, PD_K_SAMPLE = 9,
+  PD_K_KV_APPEND = 10
 };
 typedef struct {
   uint32_t struct_size;

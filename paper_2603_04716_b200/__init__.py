@@ -42,10 +42,12 @@ EXPORTS = [
     "pd_refine_next_batch", "pd_prefill_chunk_stack", "pd_test_inject_wait_timeout",
     "pd_gemm_workspace_bytes", "pd_gemm_bf16_ws",
     "pd_quantize_fp8_groups", "pd_quantize_fp8_blocks", "pd_gemm_fp8_blockwise",
+    "pd_add_rmsnorm_fp8", "pd_rope_table", "pd_paged_kv_append", "pd_paged_decode_attention_workspace_bytes",
+    "pd_paged_decode_attention", "pd_paged_prefill_attention_workspace_bytes", "pd_paged_prefill_attention",
 ]
 
 TRACE_CLASSES = ["gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "attn_prefill", "attn_decode", "rmsnorm",
-                 "embed", "lm_head", "sample"]
+                 "embed", "lm_head", "sample", "kv_append"]
 
 
 class PdError(RuntimeError):
@@ -81,6 +83,12 @@ class pd_model_weights(C.Structure):
 class pd_kv_cache(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("batch_cap", C.c_int32), ("len_cap", C.c_int32)]
+
+
+class pd_paged_kv_cache(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32)] +
+                [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales", "page_table")] +
+                [(n, C.c_int32) for n in ("n_pages", "page_len", "n_seqs", "table_ld")])
 
 
 MEASURE_GRID_MAX = 128
@@ -177,6 +185,19 @@ _lib.pd_prefill_attention.argtypes = [C.POINTER(pd_layer_cfg), _P, C.c_int32, _P
                                       _P, C.POINTER(C.c_int32), _P, C.POINTER(pd_kv_cache), _P, _P]
 _lib.pd_decode_attention_noalloc.argtypes = [C.POINTER(pd_layer_cfg), _P, C.c_int32, _P, _P, C.c_int32, C.c_int32,
                                              C.POINTER(pd_kv_cache), _P]
+_lib.pd_add_rmsnorm_fp8.argtypes = [_P, C.c_int32, _P, C.c_int32, _P, C.c_float, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P,
+                                    _P, _P]
+_lib.pd_rope_table.argtypes = [C.POINTER(pd_layer_cfg), _P]
+_lib.pd_paged_kv_append.argtypes = [C.POINTER(pd_layer_cfg), _P, C.c_int32, _P, _P, _P, C.POINTER(C.c_int32), C.c_int32, _P,
+                                    C.POINTER(pd_paged_kv_cache), _P, _P]
+_lib.pd_paged_decode_attention_workspace_bytes.argtypes = [C.POINTER(pd_layer_cfg), C.c_int32, C.c_int32,
+                                                           C.POINTER(C.c_size_t)]
+_lib.pd_paged_decode_attention.argtypes = [C.POINTER(pd_layer_cfg), _P, C.c_int32, _P, _P, C.c_int32, C.c_int32,
+                                           C.POINTER(pd_paged_kv_cache), _P, C.c_size_t, _P, _P]
+_lib.pd_paged_prefill_attention_workspace_bytes.argtypes = [C.POINTER(pd_layer_cfg), C.c_int32, C.c_int32,
+                                                            C.POINTER(C.c_size_t)]
+_lib.pd_paged_prefill_attention.argtypes = [C.POINTER(pd_layer_cfg), _P, C.c_int32, _P, _P, C.POINTER(C.c_int32), C.c_int32,
+                                            _P, C.POINTER(C.c_int32), C.POINTER(pd_paged_kv_cache), _P, C.c_size_t, _P, _P]
 _lib.pd_model_create.argtypes = [C.POINTER(_P), C.c_int32, C.POINTER(pd_model_weights), _P, C.POINTER(_P)]
 _lib.pd_model_destroy.argtypes = [_P]
 _lib.pd_model_check.argtypes = [_P, _P]
@@ -508,6 +529,80 @@ def pd_quantize_fp8_blocks(w, n: int, k: int, codes, scales, ldw: int = 0, strea
 def pd_gemm_fp8_blockwise(a_codes, a_scales, b_codes, b_scales, c, m: int, n: int, k: int, err_word=None, stream=None):
     _check(_lib.pd_gemm_fp8_blockwise(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), _ptr(c), m, n, k,
                                       _ptr(err_word), _stream_ptr(stream)), "pd_gemm_fp8_blockwise")
+
+
+def pd_add_rmsnorm_fp8(x, rows: int, d: int, gain, codes, scales, residual=None, sum_out=None, norm_out=None, eps: float = 1e-6,
+                       group: int = 128, ldx: int = 0, ldr: int = 0, stream=None):
+    """x, residual: device bf16 [rows, d] -> sum_out = x + residual, norm_out = RMSNorm(sum_out) * gain (bf16 [rows, d], both
+    optional) and the norm's codes uint8 [rows, d] with scales fp32 [rows, d / 128] (group = 128) or [rows] (group = 0)."""
+    _check(_lib.pd_add_rmsnorm_fp8(_ptr(x), ldx or d, _ptr(residual), ldr or d, _ptr(gain), eps, rows, d, group,
+                                   _ptr(sum_out), _ptr(norm_out), _ptr(codes), _ptr(scales), _stream_ptr(stream)),
+           "pd_add_rmsnorm_fp8")
+
+
+def paged_kv_cache_struct(k_codes, v_codes, k_scales, v_scales, page_table, n_pages: int, page_len: int, n_seqs: int,
+                          table_ld: int) -> pd_paged_kv_cache:
+    return pd_paged_kv_cache(C.sizeof(pd_paged_kv_cache), _ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales),
+                             _ptr(page_table), n_pages, page_len, n_seqs, table_ld)
+
+
+def pd_rope_table(cfg: LayerConfig):
+    """numpy float32 [max_pos, head_dim / 2, 2]: cos and sin of every position and pair (host)."""
+    import numpy as np
+    if cfg.max_pos <= 0 or cfg.head_dim <= 0:
+        raise PdError(PD_ERR_INVALID_ARG, "pd_rope_table")
+    out = np.empty((cfg.max_pos, cfg.head_dim // 2, 2), dtype=np.float32)
+    _check(_lib.pd_rope_table(C.byref(cfg.c_struct()), out.ctypes.data), "pd_rope_table")
+    return out
+
+
+def pd_paged_kv_append(cfg: LayerConfig, qkv, ldqkv: int, q_out, rope_tab, cache: pd_paged_kv_cache, kv_len_dev, n_req: int,
+                       cu_seqlens_dev=None, cu_seqlens_host=None, err_word=None, stream=None):
+    """Without cu_seqlens every request brings one row (a decode step)."""
+    cu = None
+    if cu_seqlens_host is not None:
+        if len(cu_seqlens_host) != n_req + 1:
+            raise ValueError("cu_seqlens has one entry more than there are requests")
+        cu = _i32_array(cu_seqlens_host)
+    _check(_lib.pd_paged_kv_append(C.byref(cfg.c_struct()), _ptr(qkv), ldqkv, _ptr(q_out), _ptr(rope_tab),
+                                   _ptr(cu_seqlens_dev), cu, n_req, _ptr(kv_len_dev), C.byref(cache), _ptr(err_word),
+                                   _stream_ptr(stream)), "pd_paged_kv_append")
+
+
+def pd_paged_decode_attention_workspace_bytes(cfg: LayerConfig, batch: int, max_kv_len: int) -> int:
+    out = C.c_size_t(0)
+    _check(_lib.pd_paged_decode_attention_workspace_bytes(C.byref(cfg.c_struct()), batch, max_kv_len, C.byref(out)),
+           "pd_paged_decode_attention_workspace_bytes")
+    return out.value
+
+
+def pd_paged_decode_attention(cfg: LayerConfig, q, ldq: int, out, kv_len_dev, batch: int, max_kv_len: int,
+                              cache: pd_paged_kv_cache, workspace, workspace_bytes: int, err_word=None, stream=None):
+    _check(_lib.pd_paged_decode_attention(C.byref(cfg.c_struct()), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch,
+                                          max_kv_len, C.byref(cache), _ptr(workspace), workspace_bytes, _ptr(err_word),
+                                          _stream_ptr(stream)), "pd_paged_decode_attention")
+
+
+def pd_paged_prefill_attention_workspace_bytes(cfg: LayerConfig, n_req: int, max_kv_len: int) -> int:
+    out = C.c_size_t(0)
+    _check(_lib.pd_paged_prefill_attention_workspace_bytes(C.byref(cfg.c_struct()), n_req, max_kv_len, C.byref(out)),
+           "pd_paged_prefill_attention_workspace_bytes")
+    return out.value
+
+
+def pd_paged_prefill_attention(cfg: LayerConfig, q, ldq: int, out, cu_seqlens_dev, cu_seqlens_host, prefix_dev, prefix_host,
+                               cache: pd_paged_kv_cache, workspace, workspace_bytes: int, err_word=None, stream=None):
+    """prefix_dev and prefix_host: tokens cached before the rows of each request (both None: 0)."""
+    cu = _i32_array(cu_seqlens_host)
+    pre = None
+    if prefix_host is not None:
+        if len(prefix_host) != len(cu_seqlens_host) - 1:
+            raise ValueError("one prefix per request")
+        pre = _i32_array(prefix_host)
+    _check(_lib.pd_paged_prefill_attention(C.byref(cfg.c_struct()), _ptr(q), ldq, _ptr(out), _ptr(cu_seqlens_dev), cu,
+                                           len(cu_seqlens_host) - 1, _ptr(prefix_dev), pre, C.byref(cache),
+                                           _ptr(workspace), workspace_bytes, _ptr(err_word), _stream_ptr(stream)),
+           "pd_paged_prefill_attention")
 
 
 def pd_measure(cfg: LayerConfig, *, n_layers_run: int, n_layers_model: int, warmup: int = 3, reps: int = 10,

@@ -417,6 +417,26 @@ extern "C" pd_status pd_workspace_offsets(const pd_layer_cfg* cfg, int32_t token
   return PD_OK;
 }
 
+// (cos, sin)(pos * theta^(-2i/hd)), angles in double.
+extern "C" pd_status pd_rope_table(const pd_layer_cfg* cfg, float* table) {
+  if (!cfg || cfg->struct_size != sizeof(pd_layer_cfg) || !table) return PD_ERR_INVALID_ARG;
+  if (cfg->max_pos <= 0 || !(cfg->rope_theta > 0.f)) return PD_ERR_INVALID_ARG;
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) return PD_ERR_UNSUPPORTED_SHAPE;
+  const int half = cfg->head_dim / 2;
+  double inv_freq[64];
+  for (int i = 0; i < half; ++i)
+    inv_freq[i] = std::pow(static_cast<double>(cfg->rope_theta), -2.0 * static_cast<double>(i) / cfg->head_dim);
+  for (int p = 0; p < cfg->max_pos; ++p) {
+    float* row = table + static_cast<size_t>(p) * cfg->head_dim;
+    for (int i = 0; i < half; ++i) {
+      const double ang = static_cast<double>(p) * inv_freq[i];
+      row[2 * i] = static_cast<float>(std::cos(ang));
+      row[2 * i + 1] = static_cast<float>(std::sin(ang));
+    }
+  }
+  return PD_OK;
+}
+
 extern "C" pd_status pd_layer_create(const pd_layer_cfg* cfg, const pd_layer_weights* w, void* stream,
                                      pd_layer** out) {
   PD_TRY(check_cfg(cfg));
@@ -483,16 +503,9 @@ extern "C" pd_status pd_layer_create(const pd_layer_cfg* cfg, const pd_layer_wei
     for (auto& q : qs) { cudaFree(*q.src); *q.src = nullptr; }
   }
 
-  // RoPE table in double on the host: (cos, sin)(pos * theta^(-2i/hd))
   std::vector<float2> tab(static_cast<size_t>(cfg->max_pos) * half);
-  std::vector<double> inv_freq(half);
-  for (size_t i = 0; i < half; ++i)
-    inv_freq[i] = std::pow(static_cast<double>(cfg->rope_theta), -2.0 * static_cast<double>(i) / cfg->head_dim);
-  for (int p = 0; p < cfg->max_pos; ++p)
-    for (size_t i = 0; i < half; ++i) {
-      const double ang = static_cast<double>(p) * inv_freq[i];
-      tab[static_cast<size_t>(p) * half + i] = make_float2(static_cast<float>(std::cos(ang)), static_cast<float>(std::sin(ang)));
-    }
+  const pd_status tab_st = pd_rope_table(cfg, reinterpret_cast<float*>(tab.data()));
+  if (tab_st != PD_OK) { pd_layer_destroy(L); return tab_st; }
   // the table is a stack temporary: copy synchronously with respect to the host
   if ((e = cudaMemcpy(L->rope_tab, tab.data(), tab.size() * sizeof(float2), cudaMemcpyHostToDevice)) != cudaSuccess)
     return fail(e);
