@@ -223,19 +223,30 @@ def _ptr(t):
     """Device/host address of a torch tensor, a numpy array, an int, or None."""
     if t is None:
         return None
+    try:
+        return t.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(t, int):
         return t
-    if hasattr(t, "data_ptr"):
-        return t.data_ptr()
     if hasattr(t, "ctypes"):
         return t.ctypes.data
     raise TypeError(type(t))
 
 
+_torch_cuda = None
+
+
 def _stream_ptr(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        # torch.cuda.current_stream() builds a Stream object: 2 us of a call that may take 5
+        global _torch_cuda
+        if _torch_cuda is None:
+            import torch
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            _torch_cuda = (lambda: raw(torch.cuda.current_device())) if raw else (
+                lambda: torch.cuda.current_stream().cuda_stream)
+        return _torch_cuda()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -259,6 +270,14 @@ class LayerConfig:
     fp8_projections: bool = False
 
     def c_struct(self) -> pd_layer_cfg:
+        """The C struct, made once per configuration (the library only reads it)."""
+        made = self.__dict__.get("_c_struct")
+        if made is None:
+            made = self._make_c_struct()
+            object.__setattr__(self, "_c_struct", made)
+        return made
+
+    def _make_c_struct(self) -> pd_layer_cfg:
         return pd_layer_cfg(C.sizeof(pd_layer_cfg), self.d_model, self.n_q_heads, self.n_kv_heads, self.head_dim,
                             self.d_ff, self.rms_eps, self.rope_theta, self.max_pos, int(self.fp8_projections))
 
