@@ -397,7 +397,7 @@ pd_status pd_add_rmsnorm_fp8(const void* x, int32_t ldx, const void* residual, i
  *   k_codes, v_codes    device uint8 (E4M3) [n_pages, Hkv, page_len, hd], 16-byte aligned
  *   k_scales, v_scales  device fp32 [n_pages, Hkv]: one scale per page and head, a power of two 2^e, e in -117 .. 120
  *   page_table          device int32 [n_seqs, table_ld]: position p of sequence s lies in page page_table[s][p / page_len],
- *                       row p % page_len.  Entries of pages that hold no token are not read.
+ *                       row p % page_len.  Entries of pages that hold no token are not used (they may be read).
  *   page_len            16, 32, 64 or 128;  table_ld * page_len below 2^31
  * value = E4M3(code) * scale.  The scale of a page is the smallest power of two with max|value| <= 448 * scale over the
  * tokens appended since the page's first row was last written; it only grows until then.  A power of two, so that codes
