@@ -178,11 +178,33 @@ __global__ void __launch_bounds__(AD_WARPS * 32) append_decode_kernel(const Appe
 
 // ----------------------------------------------------------------------- runs of tokens
 constexpr int AP_THREADS = 256;
-constexpr int AP_Q_HEADS = 8;  // query heads per block
+constexpr int AP_Q_HEADS = 4;  // query heads per block
 
-// Block x is a page of a request: request r owns the blocks floor(cu[r] / P) + 2 r .. floor(cu[r+1] / P) + 2 r + 1, at
-// least one more than the pages that its rows can touch, so the host needs no lengths.  Block y: the K pages of each
-// head, then the V pages, then groups of query heads.
+// The request that owns block `item`: request r owns the blocks floor(cu[r] / P) + 2 r .. floor(cu[r+1] / P) + 2 r + 1, at
+// least one more than the pages that its rows can touch, so the host needs no lengths.  All lanes of a warp search
+// together, 32 candidates at a time; for up to 32 requests the warp has every request's numbers after one load.
+template <int LOG2P>
+__device__ __forceinline__ void find_request(const AppendArgs& a, int item, int& req, int& start, int& end, int& pre) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = a.n_req;  // the request lies in lo .. lo + n - 1
+  while (n > 32) {
+    const int stride = (n + 31) / 32, r = lo + lane * stride;
+    const bool at_or_before = lane * stride < n && (a.cu_seqlens[r] >> LOG2P) + 2 * r <= item;
+    const int k = 31 - __clz(__ballot_sync(0xffffffffu, at_or_before) | 1u);
+    lo += k * stride;
+    n = min(stride, n - k * stride);
+  }
+  const int r = lo + min(lane, n - 1);
+  const int c0 = a.cu_seqlens[r], c1 = a.cu_seqlens[r + 1], kv = a.kv_len[r];
+  const int k = 31 - __clz(__ballot_sync(0xffffffffu, lane < n && (c0 >> LOG2P) + 2 * r <= item) | 1u);
+  req = lo + k;
+  start = __shfl_sync(0xffffffffu, c0, k);
+  end = __shfl_sync(0xffffffffu, c1, k);
+  pre = __shfl_sync(0xffffffffu, kv, k);
+}
+
+// Block x is a page of a request, block y a group of query heads or, behind those, the K and V rows of a KV head.  Short
+// blocks with a chain of dependent loads in front: all rows of a block are in flight at once, K and V share the chain.
 template <int HD, int LOG2P>
 __global__ void __launch_bounds__(AP_THREADS) append_pages_kernel(const AppendArgs a) {
   constexpr int P = 1 << LOG2P, J = HD / 16;
@@ -190,17 +212,12 @@ __global__ void __launch_bounds__(AP_THREADS) append_pages_kernel(const AppendAr
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
   const int item = blockIdx.x;
-  int lo = 0, hi = a.n_req - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if ((a.cu_seqlens[mid] >> LOG2P) + 2 * mid <= item) lo = mid; else hi = mid - 1;
-  }
-  const int req = lo;
-  const int start = a.cu_seqlens[req], len = min(a.cu_seqlens[req + 1], a.n_tokens) - start;
-  const int pre = a.kv_len[req];
+  int req, start, stop, pre;
+  find_request<LOG2P>(a, item, req, start, stop, pre);
+  const int len = min(stop, a.n_tokens) - start;
   if (len <= 0 || pre < 0) return;
   const int pi = (pre >> LOG2P) + item - ((start >> LOG2P) + 2 * req);
-  // positions of this page that the call fills, as far as the table and the cache's page list go
+  // positions of this page that the call fills, as far as the rotation table goes
   const int total = static_cast<int>(min(static_cast<long long>(pre) + len, 0x7fffffffll));
   const long long page_pos = static_cast<long long>(pi) << LOG2P;
   const int p0 = static_cast<int>(max(static_cast<long long>(pre), page_pos));
@@ -210,78 +227,113 @@ __global__ void __launch_bounds__(AP_THREADS) append_pages_kernel(const AppendAr
   if (n_rows <= 0) return;
   const int tasks = n_rows * J;
   const int row0 = start + (p0 - pre);
+  const int q_blocks = gridDim.y - a.n_kv_heads;
 
-  if (static_cast<int>(blockIdx.y) >= 2 * a.n_kv_heads) {
+  if (static_cast<int>(blockIdx.y) < q_blocks) {
     // ------------------------------------------------------------------ query heads
-    const int h0 = (blockIdx.y - 2 * a.n_kv_heads) * AP_Q_HEADS, h1 = min(h0 + AP_Q_HEADS, a.n_q_heads);
+    const int h0 = blockIdx.y * AP_Q_HEADS, n_h = min(AP_Q_HEADS, a.n_q_heads - h0);
     for (int t = threadIdx.x; t < tasks; t += AP_THREADS) {
       const int r = t / J, j = t % J;
+      const bf16* src = a.qkv + static_cast<size_t>(row0 + r) * a.ldqkv + h0 * HD;
+      bf16* dst = a.q_out + static_cast<size_t>(row0 + r) * (a.n_q_heads * HD) + h0 * HD;
+      uint4 w[AP_Q_HEADS][2];
+#pragma unroll
+      for (int h = 0; h < AP_Q_HEADS; ++h) {
+        if (h < n_h) {
+          w[h][0] = *reinterpret_cast<const uint4*>(src + h * HD + j * 8);
+          w[h][1] = *reinterpret_cast<const uint4*>(src + h * HD + HD / 2 + j * 8);
+        }
+      }
       float cs[16];
       load_angles(a.rope + static_cast<size_t>(p0 + r) * (HD / 2), j, cs);
-      const bf16* src = a.qkv + static_cast<size_t>(row0 + r) * a.ldqkv;
-      bf16* dst = a.q_out + static_cast<size_t>(row0 + r) * (a.n_q_heads * HD);
-#pragma unroll 2
-      for (int h = h0; h < h1; ++h) {
-        float q[16];
-        load_task<HD>(src + h * HD, j, q);
-        rotate(q, cs);
-        *reinterpret_cast<uint4*>(dst + h * HD + j * 8) = pack8(q);
-        *reinterpret_cast<uint4*>(dst + h * HD + HD / 2 + j * 8) = pack8(q + 8);
+#pragma unroll
+      for (int h = 0; h < AP_Q_HEADS; ++h) {
+        if (h < n_h) {
+          float q[16];
+          unpack8(w[h][0], q);
+          unpack8(w[h][1], q + 8);
+          rotate(q, cs);
+          *reinterpret_cast<uint4*>(dst + h * HD + j * 8) = pack8(q);
+          *reinterpret_cast<uint4*>(dst + h * HD + HD / 2 + j * 8) = pack8(q + 8);
+        }
       }
     }
     return;
   }
-  const bool is_v = static_cast<int>(blockIdx.y) >= a.n_kv_heads;
-  const int kvh = blockIdx.y - (is_v ? a.n_kv_heads : 0);
+  const int kvh = blockIdx.y - q_blocks;
   const int page = pi < a.c.table_ld ? a.c.table[static_cast<size_t>(req) * a.c.table_ld + pi] : -1;
   if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.c.n_pages)) {
     if (threadIdx.x == 0) report(a.err_word);
     return;
   }
-  float f[NT][16];
-  float amax = 0.f;
+  const size_t ph = static_cast<size_t>(page) * a.n_kv_heads + kvh;
+  const int off = p0 & (P - 1);
+  const float old_k = off > 0 ? a.c.k_scale[ph] : 0.f, old_v = off > 0 ? a.c.v_scale[ph] : 0.f;
+  float k[NT][16];
+  uint4 v[NT][2];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int t = threadIdx.x + i * AP_THREADS;
     if (t < tasks) {
-      const int r = t / J, j = t % J;
-      load_task<HD>(a.qkv + static_cast<size_t>(row0 + r) * a.ldqkv + (a.n_q_heads + (is_v ? a.n_kv_heads : 0) + kvh) * HD, j, f[i]);
-      if (!is_v) {
-        float cs[16];
-        load_angles(a.rope + static_cast<size_t>(p0 + r) * (HD / 2), j, cs);
-        rotate(f[i], cs);
-      }
-      amax = finite_max(f[i], amax);
+      const bf16* src = a.qkv + static_cast<size_t>(row0 + t / J) * a.ldqkv + (a.n_q_heads + kvh) * HD + (t % J) * 8;
+      unpack8(*reinterpret_cast<const uint4*>(src), k[i]);
+      unpack8(*reinterpret_cast<const uint4*>(src + HD / 2), k[i] + 8);
+      v[i][0] = *reinterpret_cast<const uint4*>(src + a.n_kv_heads * HD);
+      v[i][1] = *reinterpret_cast<const uint4*>(src + a.n_kv_heads * HD + HD / 2);
     }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-  __shared__ float red[AP_THREADS / 32];
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
-  const size_t ph = static_cast<size_t>(page) * a.n_kv_heads + kvh;
-  float* sp = (is_v ? a.c.v_scale : a.c.k_scale) + ph;
-  const int off = p0 & (P - 1);
-  const float old = off > 0 ? *sp : 0.f;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < AP_THREADS / 32; ++w) amax = fmaxf(amax, red[w]);
-  const float s = fmaxf(old, page_scale(amax));
-  uint8_t* base = (is_v ? a.c.v : a.c.k) + (ph << LOG2P) * HD;
-  if (off > 0 && s > old) rescale_rows(base, off * HD, old * pow2_inverse(s), threadIdx.x, AP_THREADS);
-  const float inv = pow2_inverse(s);
+  float amax_k = 0.f, amax_v = 0.f;
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int t = threadIdx.x + i * AP_THREADS;
-    if (t < tasks) store_codes<HD>(base + (off + t / J) * HD, t % J, f[i], inv);
+    if (t < tasks) {
+      float cs[16], f[16];
+      load_angles(a.rope + static_cast<size_t>(p0 + t / J) * (HD / 2), t % J, cs);
+      rotate(k[i], cs);
+      amax_k = finite_max(k[i], amax_k);
+      unpack8(v[i][0], f);
+      unpack8(v[i][1], f + 8);
+      amax_v = finite_max(f, amax_v);
+    }
   }
-  // (every thread has read the old scale before the barrier above)
-  if (threadIdx.x == 0) *sp = s;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    amax_k = fmaxf(amax_k, __shfl_xor_sync(0xffffffffu, amax_k, o));
+    amax_v = fmaxf(amax_v, __shfl_xor_sync(0xffffffffu, amax_v, o));
+  }
+  __shared__ float2 red[AP_THREADS / 32];
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_float2(amax_k, amax_v);
+  __syncthreads();  // (also: every thread has read the old scales)
+#pragma unroll
+  for (int w = 0; w < AP_THREADS / 32; ++w) {
+    amax_k = fmaxf(amax_k, red[w].x);
+    amax_v = fmaxf(amax_v, red[w].y);
+  }
+  const float s_k = fmaxf(old_k, page_scale(amax_k)), s_v = fmaxf(old_v, page_scale(amax_v));
+  uint8_t* base_k = a.c.k + (ph << LOG2P) * HD;
+  uint8_t* base_v = a.c.v + (ph << LOG2P) * HD;
+  if (off > 0 && s_k > old_k) rescale_rows(base_k, off * HD, old_k * pow2_inverse(s_k), threadIdx.x, AP_THREADS);
+  if (off > 0 && s_v > old_v) rescale_rows(base_v, off * HD, old_v * pow2_inverse(s_v), threadIdx.x, AP_THREADS);
+  const float inv_k = pow2_inverse(s_k), inv_v = pow2_inverse(s_v);
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int t = threadIdx.x + i * AP_THREADS;
+    if (t < tasks) {
+      float f[16];
+      unpack8(v[i][0], f);
+      unpack8(v[i][1], f + 8);
+      finite_max(f, 0.f);
+      store_codes<HD>(base_k + (off + t / J) * HD, t % J, k[i], inv_k);
+      store_codes<HD>(base_v + (off + t / J) * HD, t % J, f, inv_v);
+    }
+  }
+  if (threadIdx.x == 0) { a.c.k_scale[ph] = s_k; a.c.v_scale[ph] = s_v; }
 }
 
 template <int HD, int LOG2P>
 cudaError_t launch_pages(const AppendArgs& a, cudaStream_t s) {
   const dim3 grid((a.n_tokens >> LOG2P) + 2 * a.n_req,
-                  2 * a.n_kv_heads + (a.q_out ? (a.n_q_heads + AP_Q_HEADS - 1) / AP_Q_HEADS : 0));
+                  a.n_kv_heads + (a.q_out ? (a.n_q_heads + AP_Q_HEADS - 1) / AP_Q_HEADS : 0));
   return launch_pdl(append_pages_kernel<HD, LOG2P>, grid, dim3(AP_THREADS), 0, s, a);
 }
 
