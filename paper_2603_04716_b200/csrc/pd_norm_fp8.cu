@@ -26,20 +26,47 @@ struct AddNormArgs {
   float eps;
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
-  f[0] = ptx::bf16_lo(v.x); f[1] = ptx::bf16_hi(v.x);
-  f[2] = ptx::bf16_lo(v.y); f[3] = ptx::bf16_hi(v.y);
-  f[4] = ptx::bf16_lo(v.z); f[5] = ptx::bf16_hi(v.z);
-  f[6] = ptx::bf16_lo(v.w); f[7] = ptx::bf16_hi(v.w);
+// Eight elements as four pairs: the packed fp32 instructions do two at a time.
+__device__ __forceinline__ void unpack8(const uint4& v, uint64_t (&f)[4]) {
+  f[0] = ptx::pack_f32x2(ptx::bf16_lo(v.x), ptx::bf16_hi(v.x));
+  f[1] = ptx::pack_f32x2(ptx::bf16_lo(v.y), ptx::bf16_hi(v.y));
+  f[2] = ptx::pack_f32x2(ptx::bf16_lo(v.z), ptx::bf16_hi(v.z));
+  f[3] = ptx::pack_f32x2(ptx::bf16_lo(v.w), ptx::bf16_hi(v.w));
 }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-  return make_uint4(ptx::pack_bf16(f[0], f[1]), ptx::pack_bf16(f[2], f[3]), ptx::pack_bf16(f[4], f[5]),
-                    ptx::pack_bf16(f[6], f[7]));
+__device__ __forceinline__ uint32_t round2(uint64_t f) {
+  float lo, hi;
+  ptx::unpack_f32x2(f, lo, hi);
+  return ptx::pack_bf16(lo, hi);
+}
+__device__ __forceinline__ uint4 pack8(const uint64_t (&f)[4]) {
+  return make_uint4(round2(f[0]), round2(f[1]), round2(f[2]), round2(f[3]));
+}
+__device__ __forceinline__ float max_abs(const uint64_t (&f)[4]) {
+  float m = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float lo, hi;
+    ptx::unpack_f32x2(f[j], lo, hi);
+    m = ptx::fmax3(m, fabsf(lo), fabsf(hi));
+  }
+  return m;
+}
+__device__ __forceinline__ uint32_t codes2(uint64_t f, uint64_t inv) {
+  float lo, hi;
+  ptx::unpack_f32x2(ptx::mul_f32x2(f, inv), lo, hi);
+  return ptx::cvt_e4m3x2(lo, hi);
 }
 
-// max / 448, 1 for an all-zero block; kept at the smallest normal number so that its reciprocal is finite.
+// max / 448, 1 for an all-zero block; kept at the smallest normal number so that its reciprocal is finite.  Product and
+// approximate reciprocal (each within 1.5 units in the last place) instead of divisions, whose instructions had been a third
+// of the kernel's: a code can then differ from that of the exact quotient only where the two lie 2^-22 from a tie.
 __device__ __forceinline__ float scale_of(float amax) {
-  return amax > 0.f ? fmaxf(__fdiv_rn(amax, 448.f), 1.17549435e-38f) : 1.f;
+  return amax > 0.f ? fmaxf(amax * (1.f / 448.f), 1.17549435e-38f) : 1.f;
+}
+__device__ __forceinline__ float reciprocal(float s) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+  return r;
 }
 
 // NCH: 16-byte chunks per thread.  GROUPS: one scale per 128 channels (16 neighbouring threads) instead of one per row.
@@ -53,41 +80,36 @@ __global__ void __launch_bounds__(AN_THREADS) add_rmsnorm_fp8_kernel(const AddNo
   const uint4* xr = reinterpret_cast<const uint4*>(a.x + row * a.ldx);
   const uint4* rr = a.r ? reinterpret_cast<const uint4*>(a.r + row * a.ldr) : nullptr;
   const uint4* gr = reinterpret_cast<const uint4*>(a.gain);
-  uint4 h[NCH], g[NCH];
+  uint64_t f[NCH][4];  // the sum, then the norm
+  uint4 g[NCH];
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
     const int c = threadIdx.x + i * AN_THREADS;
-    h[i] = g[i] = make_uint4(0u, 0u, 0u, 0u);
+    uint4 h = make_uint4(0u, 0u, 0u, 0u);
+    g[i] = h;
     if (c < chunks) {
-      h[i] = xr[c];
+      h = xr[c];
       if (rr) {
-        const uint4 rv = rr[c];
-        float f[8], e[8];
-        unpack8(h[i], f);
-        unpack8(rv, e);
+        uint64_t e[4];
+        unpack8(rr[c], e);
+        unpack8(h, f[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] += e[j];
-        h[i] = pack8(f);
+        for (int j = 0; j < 4; ++j) f[i][j] = ptx::add_f32x2(f[i][j], e[j]);
+        h = pack8(f[i]);
       }
       g[i] = gr[c];
+      if (a.sum_out) reinterpret_cast<uint4*>(a.sum_out + row * a.d)[c] = h;
     }
+    unpack8(h, f[i]);  // the norm sees the stored (rounded) sum; chunks beyond the row are zero
   }
-  float ss = 0.f;
+  uint64_t ss2 = 0ull;
 #pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    float f[8];
-    unpack8(h[i], f);  // the norm sees the stored (rounded) sum; chunks beyond the row are zero
+  for (int i = 0; i < NCH; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(f[j], f[j], ss);
-  }
-  if (a.sum_out) {
-    uint4* sr = reinterpret_cast<uint4*>(a.sum_out + row * a.d);
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = threadIdx.x + i * AN_THREADS;
-      if (c < chunks) sr[c] = h[i];
-    }
-  }
+    for (int j = 0; j < 4; ++j) ss2 = ptx::fma_f32x2(f[i][j], f[i][j], ss2);
+  float ss, ss_hi;
+  ptx::unpack_f32x2(ss2, ss, ss_hi);
+  ss += ss_hi;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
   if ((threadIdx.x & 31) == 0) red[0][threadIdx.x >> 5] = ss;
@@ -96,18 +118,20 @@ __global__ void __launch_bounds__(AN_THREADS) add_rmsnorm_fp8_kernel(const AddNo
 #pragma unroll
   for (int w = 0; w < AN_THREADS / 32; ++w) tot += red[0][w];
   const float rs = rsqrtf(tot / static_cast<float>(a.d) + a.eps);
+  const uint64_t rs2 = ptx::pack_f32x2(rs, rs);
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    uint64_t e[4];
+    unpack8(g[i], e);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[i][j] = ptx::mul_f32x2(ptx::mul_f32x2(f[i][j], rs2), e[j]);
+  }
 
   float inv_row = 1.f;
   if (!GROUPS && a.codes) {
     float amax = 0.f;
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      float f[8], gg[8];
-      unpack8(h[i], f);
-      unpack8(g[i], gg);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(f[j] * rs * gg[j]));
-    }
+    for (int i = 0; i < NCH; ++i) amax = fmaxf(amax, max_abs(f[i]));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     if ((threadIdx.x & 31) == 0) red[1][threadIdx.x >> 5] = amax;
@@ -116,34 +140,28 @@ __global__ void __launch_bounds__(AN_THREADS) add_rmsnorm_fp8_kernel(const AddNo
 #pragma unroll
     for (int w = 0; w < AN_THREADS / 32; ++w) mx = fmaxf(mx, red[1][w]);
     const float s = scale_of(mx);
-    inv_row = __frcp_rn(s);
+    inv_row = reciprocal(s);
     if (threadIdx.x == 0) a.scales[row] = s;
   }
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
     const int c = threadIdx.x + i * AN_THREADS;
-    float f[8], gg[8];
-    unpack8(h[i], f);
-    unpack8(g[i], gg);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = f[j] * rs * gg[j];
-    if (a.norm_out && c < chunks) reinterpret_cast<uint4*>(a.norm_out + row * a.d)[c] = pack8(f);
+    if (a.norm_out && c < chunks) reinterpret_cast<uint4*>(a.norm_out + row * a.d)[c] = pack8(f[i]);
     if (a.codes) {
       float inv = inv_row;
       if (GROUPS) {
-        float amax = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(f[j]));
+        float amax = max_abs(f[i]);
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
         const float s = scale_of(amax);
-        inv = __frcp_rn(s);
+        inv = reciprocal(s);
         if ((threadIdx.x & 15) == 0 && c < chunks) a.scales[row * (a.d / 128) + (c >> 4)] = s;
       }
       if (c < chunks) {
+        const uint64_t inv2 = ptx::pack_f32x2(inv, inv);
         uint2 o;
-        o.x = ptx::cvt_e4m3x2(f[0] * inv, f[1] * inv) | (ptx::cvt_e4m3x2(f[2] * inv, f[3] * inv) << 16);
-        o.y = ptx::cvt_e4m3x2(f[4] * inv, f[5] * inv) | (ptx::cvt_e4m3x2(f[6] * inv, f[7] * inv) << 16);
+        o.x = codes2(f[i][0], inv2) | (codes2(f[i][1], inv2) << 16);
+        o.y = codes2(f[i][2], inv2) | (codes2(f[i][3], inv2) << 16);
         reinterpret_cast<uint2*>(a.codes + row * a.d)[c] = o;
       }
     }
