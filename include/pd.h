@@ -457,10 +457,18 @@ pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int3
                                     int32_t* err_word, void* stream);
 
 /* pd_prefill_attention over the 8-bit paged cache: row t of request r is the query at position prefix[r] + t and attends to
- * positions 0 .. prefix[r] + t of page_table row r (its own tokens must have been appended).  Arguments as there; the cached
- * pages are decoded (exactly) to bf16 in the workspace, at least pd_paged_prefill_attention_workspace_bytes() bytes for the
- * longest prefix[r] + len_r, 256-byte aligned, not shared by calls that can overlap.  err_word: 1 if a bounded wait gave
- * up, 2 if a page number lies outside the pool (the output of that request is then not meaningful). */
+ * positions 0 .. prefix[r] + t of page_table row r (its own tokens must have been appended).  Serves whole prompts, chunks of
+ * prompts and a few drafted tokens per sequence: one of three kernels is taken from the host lengths (a streaming one for few
+ * rows, a tensor-memory one on the codes themselves, or the kernel of pd_prefill_attention on a decoded copy for long runs);
+ * they agree within the rounding of the softmax weights to 16 bits and of the result.
+ *   q, out        as for pd_prefill_attention (q 16-byte aligned, out 32-byte aligned)
+ *   cu_seqlens    device and host copy;  prefix  device and host copy, both or neither (NULL = 0)
+ *   workspace     at least pd_paged_prefill_attention_workspace_bytes() bytes for the longest prefix[r] + len_r, 256-byte
+ *                 aligned, not shared by calls that can overlap on the GPU
+ *   err_word      optional device int32: 1 if a bounded wait gave up, 2 if a page number lies outside the pool (the output
+ *                 of that request is then not meaningful, that of the others is)
+ * Page scales within a sequence may differ by 2^15 without loss; V values of pages further below the largest lose low bits
+ * first.  Only enqueues work. */
 pd_status pd_paged_prefill_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t n_req, int32_t max_kv_len,
                                                      size_t* out_bytes);
 pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const void* q, int32_t ldq, void* out,
@@ -479,7 +487,7 @@ pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const void* q, int
  * unaffected.  PD_INJECT_NONE disarms.  (The paper has no counterpart; it exists so that the timeout path can
  * be exercised without a real fault.) */
 enum { PD_INJECT_NONE = 0, PD_INJECT_ATTN_PREFILL = 1, PD_INJECT_GEMM = 2, PD_INJECT_GEMM_PAIR = 3,
-       PD_INJECT_GEMM_FP8_BLOCKWISE = 4 };
+       PD_INJECT_GEMM_FP8_BLOCKWISE = 4, PD_INJECT_ATTN_PAGED = 5 };
 pd_status pd_test_inject_wait_timeout(int32_t kernel_kind, uint64_t wait_limit_ns);
 
 /* Kernels launched so far by the calling thread through this library. */

@@ -1,0 +1,893 @@
+// Prefill attention over the 8-bit paged KV cache on the 5th-generation tensor cores (tcgen05 + tensor memory).
+//
+// The tile structure is that of pd_attn_prefill_tc.cu: a block works on two row tiles of 128 rows whose softmax and products
+// ping-pong over key tiles of 128, S / P and O live in tensor memory, one thread issues the products.  What differs:
+//   * Rows are (token, query head of the group) pairs, the head fastest: a key tile is read and decoded once for all heads
+//     that share it, and a short run of tokens still fills the rows (16 tokens of a group of 8 are one row tile).
+//   * S = Q K^T takes the K codes as they are: a key tile is copied from its pages by TMA and multiplied as E4M3.  q goes in
+//     as the sum of two E4M3 numbers, scaled per row by a power of two to a largest entry in [128, 256): the products are
+//     exact, the second number leaves an error of at most 2^-10, 2^-17 of the row's largest entry.  Two 8-bit products take
+//     the time of one 16-bit product.  The K scales of the pages multiply the scores in the softmax, per 16 keys.
+//   * O += P V has both operands in f16.  V codes come by TMA as well, two warps turn them into f16 operand rows (exact, one
+//     instruction for two codes).  V counts in a unit that only grows over the key tiles of an item (with
+//     two octaves to spare when it does), and O is rescaled when it grows; a page's scale relative to it multiplies the
+//     codes, exact down to 2^-15 of the unit.  p is kept as 2^7 p; the row reference of the exponent may lag the maximum by
+//     2^8.  There is no decoded copy of the cache in global memory.
+//   * When there are fewer items than SMs, the key range of every item is cut into equal parts, the parts write
+//     unnormalised fp32 rows with their maximum and sum, and a second kernel joins them.
+//   * Items are handed out by the hardware: the grid has one block per item, a resident block that is done takes over the
+//     next block that has not been started (clusterlaunchcontrol), so there is no counter in memory to share or to reset.
+//   warp 0      : producer     - takes items over, publishes them in a ring, starts the copies of Q, K and V tiles and
+//                 publishes the scales of the pages
+//   warp 1      : MMA issuer   - S = Q K^T, O += P V (P read from tensor memory), whichever is ready
+//   warps 2-5, 6-9 : softmax of row tile 0, 1, one row per thread; they also turn the next item's Q into codes, while the
+//                 last product of the current one runs, and store the output rows
+//   warps 10-11 : V tiles, 64 keys each, from codes to f16
+// Every wait is wall-clock bounded and leaves through the common teardown.
+#include <math_constants.h>
+
+#include "pd_paged.cuh"
+
+namespace pd {
+namespace {
+
+constexpr int TQ = 128;                    // rows per row tile
+constexpr int TK = 128;                    // keys per key tile
+constexpr int THREADS = 384;
+constexpr float LOG2E_F = 1.4426950408889634f;
+constexpr float RESCALE_THRESHOLD = 8.f;   // log2 units
+constexpr float P_SHIFT = 7.f;             // p is kept as 2^7 p: at most 2^15, below f16's 65504
+constexpr int K_SLOTS = 4, V_SLOTS = 2, R_SLOTS = 2, ITEM_SLOTS = 4, INFO_SLOTS = 8;
+constexpr int kNoPage = static_cast<int>(0x80000000u);  // beyond the keys of a tile
+constexpr int kNoRows = -1000;
+constexpr int MAX_SPLIT_ITEMS = 148;       // parts of items while there are splits (sizes the workspace)
+
+template <int HD>
+struct Cfg {
+  static constexpr int CODE_BYTES = TQ * HD;                // one tile of codes: K, or one of the two numbers of Q
+  static constexpr int Q_BYTES = 2 * CODE_BYTES;
+  static constexpr int V_BYTES = TK * HD * 2;
+  static constexpr int V_SUB_BYTES = TK * 128;              // V: sub-tiles of 64 features
+  static constexpr int Q_OFF = 0;                           // two Q tiles
+  static constexpr int K_OFF = 2 * Q_BYTES;
+  static constexpr int V_OFF = K_OFF + K_SLOTS * CODE_BYTES;
+  static constexpr int R_OFF = V_OFF + V_SLOTS * V_BYTES;   // codes of V tiles
+  static constexpr int AUX_OFF = R_OFF + R_SLOTS * CODE_BYTES;
+  static constexpr int SMEM_BYTES_MIN = AUX_OFF + 2048 + 1024;  // (the last for the alignment of the tiles)
+  // always more than half of the SM's shared memory, so that one block owns the SM and its 512 tensor-memory columns
+  static constexpr int SMEM_BYTES = SMEM_BYTES_MIN > 120 * 1024 ? SMEM_BYTES_MIN : 120 * 1024;
+  static constexpr int S_COL = 0, O_COL = 128, TILE_COLS = 256;  // tensor-memory columns of a row tile
+};
+
+// barrier indices
+constexpr int B_QFULL = 0, B_QEMPTY = 2, B_KFULL = 4, B_KEMPTY = B_KFULL + K_SLOTS, B_VFULL = B_KEMPTY + K_SLOTS,
+              B_VEMPTY = B_VFULL + V_SLOTS, B_SFULL = B_VEMPTY + V_SLOTS, B_PREADY = B_SFULL + 2, B_ODONE = B_PREADY + 2,
+              B_OREAD = B_ODONE + 2, B_IFULL = B_OREAD + 2, B_IEMPTY = B_IFULL + ITEM_SLOTS, B_CLC = B_IEMPTY + ITEM_SLOTS,
+              B_QRAW = B_CLC + 1, B_RFULL = B_QRAW + 2, B_REMPTY = B_RFULL + R_SLOTS, N_BARS = B_REMPTY + R_SLOTS;
+
+struct PagedPrefillDev {
+  const bf16* q;
+  bf16* o;
+  const int32_t* cu_seqlens;
+  const int32_t* prefix;
+  PagedParts parts;        // used when n_splits > 1
+  int* err_word;
+  PagedCache c;
+  int ldq, n_req, n_tokens, n_q_heads, n_kv_heads;
+  int tile_tokens;         // tokens of a row tile: 128 / group
+  int n_slots, n_splits;   // items = n_slots x n_splits x n_kv_heads
+  unsigned long long wait_limit_ns;
+  int test_skip_arrive;    // test hook: the second V warp leaves out one arrival
+};
+
+// A work item as warp 0 publishes it.
+struct Item {
+  int kvh, start, len, t0, pre, req, jb, n_kv0, n_kv1, split;  // n_kv0 = -1: no more items
+};
+// Per 16 keys of a tile: factor of the scores and exponent of V's page scale relative to the unit of V (<= 0; kNoRows: no
+// such page); the unit.
+struct alignas(16) TileInfo { float k_mul[TK / 16]; int v_rel[TK / 16]; int v_exp; };
+
+struct Shared {
+  uint64_t bars[N_BARS + 1];
+  Item items[ITEM_SLOTS];
+  TileInfo info[INFO_SLOTS];
+  int8_t row_exp[2][2][TQ];   // [items with work & 1][row tile][row]: exponent that q of the row was divided by
+  uint4 clc;                  // the answer to a request for another block
+  uint32_t tmem;
+  int abort_flag;
+};
+static_assert(sizeof(Shared) <= 2048, "AUX area");
+static_assert(Cfg<128>::SMEM_BYTES <= 227 * 1024, "shared memory");
+
+__device__ __forceinline__ constexpr uint32_t idesc_f16(int m, int n) {  // f16 A and B, both K-major, fp32 accumulator
+  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ float exp2_int(int e) {  // 2^e, e within -126 .. 127
+  return __uint_as_float(static_cast<uint32_t>(min(max(e, -126), 127) + 127) << 23);
+}
+__device__ __forceinline__ void sts64(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+// Byte offset of 16-byte chunk c (8 features) of a row of a V tile: sub-tiles of 64 features, 128-byte rows, swizzled.
+template <int HD>
+__device__ __forceinline__ uint32_t v_off(int row, int c) {
+  return static_cast<uint32_t>((c >> 3) * Cfg<HD>::V_SUB_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+}
+// Byte offset of 8 codes (features 8 c ..) of a row of a code tile: rows of HD bytes, swizzled as TMA lays K out.
+template <int HD>
+__device__ __forceinline__ uint32_t code_off(int row, int c) {
+  const int x = HD == 128 ? (row & 7) : ((row >> 1) & 3);
+  return static_cast<uint32_t>(row * HD + (((c >> 1) ^ x) << 4) + (c & 1) * 8);
+}
+template <int HD>
+__device__ __forceinline__ uint64_t code_desc(uint32_t addr) {
+  return HD == 128 ? ptx::umma_desc_sw128(addr) : ptx::umma_desc_sw64(addr);
+}
+
+// ------------------------------------------------------------------------------------------------ items
+// Item `idx` of the grid: KV head fastest, then the part of the key range, then slots from the last one down (of a request
+// the rows with the longest key ranges come first).  All lanes of a warp call; false: nothing to do.
+__device__ __forceinline__ bool decode_item(const PagedPrefillDev& p, int idx, Item& it) {
+  const int tb = 2 * p.tile_tokens;
+  const int per_slot = p.n_kv_heads * p.n_splits;
+  const int rest = idx % per_slot;
+  const TokenBlock b = find_block(p.cu_seqlens, p.prefix, p.n_req, p.n_tokens, p.n_slots - 1 - idx / per_slot, tb);
+  it.kvh = rest % p.n_kv_heads;
+  it.split = rest / p.n_kv_heads;
+  it.req = b.req; it.start = b.start; it.len = b.len; it.pre = b.pre; it.t0 = b.t0;
+  if (it.t0 >= it.len) return false;
+  const int n0 = (it.pre + min(it.len, it.t0 + p.tile_tokens) + TK - 1) / TK;
+  const int n1 = it.t0 + p.tile_tokens < it.len ? (it.pre + min(it.len, it.t0 + tb) + TK - 1) / TK : 0;
+  const int n_all = max(n0, n1);
+  it.jb = static_cast<int>(1ll * n_all * it.split / p.n_splits);
+  const int je = static_cast<int>(1ll * n_all * (it.split + 1) / p.n_splits);
+  it.n_kv0 = max(0, min(n0, je) - it.jb);
+  it.n_kv1 = max(0, min(n1, je) - it.jb);
+  return true;
+}
+
+// Rows of row tile t of an item that hold a (token, head) pair.
+__device__ __forceinline__ int tile_rows(const PagedPrefillDev& p, const Item& it, int t, int group) {
+  return min(max(it.len - it.t0 - t * p.tile_tokens, 0), p.tile_tokens) * group;
+}
+
+// q of 32 rows of a row tile, in place: the buffer holds the bf16 rows as TMA has brought them, the first half of the
+// features of a row where the first number of that row goes, the second half where the second goes; they become two E4M3
+// numbers and the rows' exponents.  Four lanes share a row, eight rows at a time.  All lanes of a warp call.  A function of
+// its own (never inlined), like the roles below, so that its registers are allocated apart from the softmax code.
+template <int HD>
+__device__ __noinline__ void convert_q(const uint32_t tile, const int first, int8_t* exps) {
+  const int lane = threadIdx.x & 31, quarter = lane & 3;
+  constexpr int NC = HD / 32;  // chunks of 8 features per lane
+  const uint32_t raw = tile + (quarter >> 1) * Cfg<HD>::CODE_BYTES + (quarter & 1) * (HD / 2);
+#pragma unroll 1
+  for (int r0 = first; r0 < first + 32; r0 += 8) {
+    const int r = r0 + (lane >> 2);
+    uint4 w[NC];
+    float amax = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[c].x), "=r"(w[c].y), "=r"(w[c].z), "=r"(w[c].w)
+                   : "r"(raw + r * HD + c * 16));
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].x)), fabsf(ptx::bf16_hi(w[c].x)));
+      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].y)), fabsf(ptx::bf16_hi(w[c].y)));
+      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].z)), fabsf(ptx::bf16_hi(w[c].z)));
+      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].w)), fabsf(ptx::bf16_hi(w[c].w)));
+    }
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));  // (also: the rows have been read whole)
+    // 2^(e + 7) <= amax < 2^(e + 8), e kept where 2^e and 2^-e are normal
+    const int e2 = min(max(static_cast<int>(__float_as_uint(amax) >> 23) - 127 - 7, -126), 120);
+    const float inv = exp2_int(-e2);
+    const bool finite = amax <= 3.402823466e38f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const uint32_t ww[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float h[2], l[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float x = (i ? ptx::bf16_hi(ww[e]) : ptx::bf16_lo(ww[e])) * inv;
+          // an infinite q: E4M3 has no infinity, and the conversion would saturate
+          if (!finite && !(fabsf(x) <= 3.402823466e38f)) x = __int_as_float(0x7fc00000);
+          // h: x rounded to four significant bits (a product with 2^20 + 1 and two differences), l: the rest, exactly
+          const float s = __fmul_rn(x, 1048577.f);
+          h[i] = __fsub_rn(s, __fsub_rn(s, x));
+          l[i] = __fsub_rn(x, h[i]);
+        }
+        hi[e] = ptx::cvt_e4m3x2(h[0], h[1]);
+        lo[e] = ptx::cvt_e4m3x2(l[0], l[1]);
+      }
+      const uint32_t at = tile + code_off<HD>(r, quarter * NC + c);
+      sts64(at, hi[0] | (hi[1] << 16), hi[2] | (hi[3] << 16));
+      sts64(at + Cfg<HD>::CODE_BYTES, lo[0] | (lo[1] << 16), lo[2] | (lo[3] << 16));
+    }
+    if (quarter == 0) exps[r] = static_cast<int8_t>(e2);
+    __syncwarp();
+  }
+  ptx::fence_proxy_async();
+  __syncwarp();
+}
+
+// --------------------------------------------------------------------------------------------- warp 0: producer
+template <int HD>
+__device__ __noinline__ void producer(const CUtensorMap* tmap_q, const CUtensorMap* tmap_k, const CUtensorMap* tmap_v,
+                                      const PagedPrefillDev& p, const uint32_t smem_base, Shared* sh, const uint64_t limit) {
+  using C = Cfg<HD>;
+  const uint32_t bar0 = ptx::smem_u32(sh->bars), clc = ptx::smem_u32(&sh->clc);
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  volatile int* abort_flag = &sh->abort_flag;
+  const int lane = threadIdx.x & 31;
+  const int group = p.n_q_heads / p.n_kv_heads;
+  const int q_bytes = p.tile_tokens * group * HD;  // half of a Q tile
+  const int l2p = p.c.log2_page, ppt = TK >> l2p;  // pages per key tile
+  const uint32_t page_bytes = static_cast<uint32_t>(HD) << l2p;
+  int published = 0, act[2] = {0, 0}, asked = 0;
+  int idx = blockIdx.x;
+  bool ok = true, more = true;
+  auto wait = [&](int b, uint32_t parity) {
+    ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(b), parity, abort_flag, limit));
+    return ok;
+  };
+  // the next block of the grid, if one is left that has not been started
+  auto take = [&] {
+    if (lane == 0) {
+      ptx::mbar_arrive_expect_tx(bar(B_CLC), 16);
+      ptx::clc_try_cancel(clc, bar(B_CLC));
+    }
+    __syncwarp();
+    if (!wait(B_CLC, asked & 1)) return;
+    ++asked;
+    more = ptx::clc_answer(clc, idx);
+    __syncwarp();
+    ptx::fence_proxy_async();
+  };
+  int g = 0;  // key tiles started so far
+  Item it;
+  bool have = false;
+  auto next_item = [&] {  // the first item with something to do
+    have = decode_item(p, idx, it);
+    while (!have && more) {
+      take();
+      if (!ok || !more) break;
+      have = decode_item(p, idx, it);
+    }
+  };
+  next_item();
+  while (ok) {
+    if (!have) { it.n_kv0 = -1; it.n_kv1 = 0; }
+    {
+      const int s = published & (ITEM_SLOTS - 1);
+      if (!wait(B_IEMPTY + s, ((published / ITEM_SLOTS) & 1) ^ 1u)) break;
+      if (lane == 0) {
+        sh->items[s] = it;
+        ptx::mbar_arrive(bar(B_IFULL + s));  // release: the item is visible to whoever sees the phase flip
+      }
+      __syncwarp();
+      ++published;
+    }
+    if (!have) break;
+    const int n = max(it.n_kv0, it.n_kv1), n_kv[2] = {it.n_kv0, it.n_kv1};
+    const int total = it.pre + it.len;  // keys that the request holds
+    const int32_t* table = p.c.table + static_cast<size_t>(it.req) * p.c.table_ld;
+    const int kvh = it.kvh, jb = it.jb, q_token = it.start + it.t0;
+
+    // lane l < ppt holds page l of a tile: its number (-1: no such page, or no key in it), its K scale, the exponent of its
+    // V scale.  Values are looked at a tile after they have been asked for, so that no load is waited for.
+    auto fetch_ids = [&](int j) {
+      const long long page = (static_cast<long long>(jb + j) * ppt) + lane;
+      return j < n && lane < ppt && (page << l2p) < total && page < p.c.table_ld ? table[page] : kNoPage;
+    };
+    auto checked = [&](int id) {
+      if (id != kNoPage && static_cast<unsigned>(id) >= static_cast<unsigned>(p.c.n_pages) && p.err_word) atomicExch(p.err_word, 2);
+      return static_cast<unsigned>(id) < static_cast<unsigned>(p.c.n_pages) ? id : -1;
+    };
+    auto page_head = [&](int id) { return static_cast<size_t>(id) * p.n_kv_heads + kvh; };
+    auto fetch_v_scale = [&](int id) { return id >= 0 ? __float_as_uint(p.c.v_scale[page_head(id)]) : 0u; };
+    auto fetch_k_scale = [&](int id) { return id >= 0 ? p.c.k_scale[page_head(id)] : 1.f; };
+    // The unit of V: at least the largest exponent so far, two octaves more when it has to grow.
+    int unit = -126;
+    bool unit_set = false;
+    // copies the pages of tile g (a ring position) and publishes its scales.  (Rows of a page behind the last key hold
+    // anything: their scores are masked, their V rows become zeros.)
+    auto start_tile = [&](int ids, float ks, uint32_t vs) {
+      const int ev = ids >= 0 ? static_cast<int>(vs >> 23) - 127 : kNoRows;
+      const int ev_max = __reduce_max_sync(0xffffffffu, ev);
+      if (ev_max > kNoRows && (!unit_set || ev_max > unit)) { unit = ev_max + 2; unit_set = true; }
+      const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, ids >= 0)) * page_bytes;
+      const int row = static_cast<int>(page_head(ids) << l2p);
+      const int s = g % K_SLOTS, r = g % R_SLOTS;
+      if (!wait(B_KEMPTY + s, ((g / K_SLOTS) & 1) ^ 1u)) return;
+      TileInfo& info = sh->info[g % INFO_SLOTS];
+      const int page16 = (16 * (lane & 7)) >> l2p;  // the page of 16 keys
+      const float mul = __shfl_sync(0xffffffffu, ks, page16);
+      const int rel = __shfl_sync(0xffffffffu, ev, page16);
+      if (lane < TK / 16) {
+        info.k_mul[lane] = mul;
+        info.v_rel[lane] = rel == kNoRows ? kNoRows : rel - unit;
+      }
+      if (lane == 0) info.v_exp = unit;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_expect_tx(bar(B_KFULL + s), bytes);
+      __syncwarp();
+      if (ids >= 0) ptx::tma_load_2d(smem_base + C::K_OFF + s * C::CODE_BYTES + lane * page_bytes, tmap_k, 0, row, bar(B_KFULL + s));
+      if (!wait(B_REMPTY + r, ((g / R_SLOTS) & 1) ^ 1u)) return;
+      if (lane == 0) ptx::mbar_arrive_expect_tx(bar(B_RFULL + r), bytes);
+      __syncwarp();
+      if (ids >= 0) ptx::tma_load_2d(smem_base + C::R_OFF + r * C::CODE_BYTES + lane * page_bytes, tmap_v, 0, row, bar(B_RFULL + r));
+      ++g;
+    };
+    auto start_q = [&](int t) {
+      if (n_kv[t] == 0) return;
+      // the tile's Q buffer is free once the last Q K^T of its previous item has been executed
+      if (!wait(B_QEMPTY + t, (act[t] & 1) ^ 1u)) return;
+      if (lane == 0) {
+        // (tokens of the tile that belong to the next request, or zeros behind the last one, come along: they are not used)
+        const uint32_t tile = smem_base + C::Q_OFF + t * C::Q_BYTES;
+        ptx::mbar_arrive_expect_tx(bar(B_QRAW + t), 2 * q_bytes);
+        for (int h = 0; h < 2; ++h)
+          ptx::tma_load_3d(tile + h * C::CODE_BYTES, tmap_q, h * (HD / 2), kvh * group, q_token + t * p.tile_tokens, bar(B_QRAW + t));
+      }
+      __syncwarp();
+      ++act[t];
+    };
+
+    int ids0 = fetch_ids(0), ids1 = fetch_ids(1), raw2 = fetch_ids(2);
+    if (published == 1) { start_q(0); start_q(1); }  // the block's first item: the buffers are free
+    ids0 = checked(ids0); ids1 = checked(ids1);
+    uint32_t vs0 = fetch_v_scale(ids0), vs1 = fetch_v_scale(ids1);
+    float ks0 = fetch_k_scale(ids0), ks1 = fetch_k_scale(ids1);
+#pragma unroll 1
+    for (int j = 0; j < n && ok; ++j) {
+      const int raw3 = fetch_ids(j + 3), ids2 = checked(raw2);
+      const uint32_t vs2 = fetch_v_scale(ids2);
+      const float ks2 = fetch_k_scale(ids2);
+      start_tile(ids0, ks0, vs0);
+      // (a later item's q waits for the current one's last product: its first key tiles go before it)
+      if (ok && published > 1 && j == min(1, n - 1)) { start_q(0); if (ok) start_q(1); }
+      ids0 = ids1; ids1 = ids2; raw2 = raw3; vs0 = vs1; vs1 = vs2; ks0 = ks1; ks1 = ks2;
+      if (!ok) break;
+      // Another block is taken over only when the copies of this item are nearly all under way: early enough to bring the next
+      // one's operands in time, and no block waits here while another SM has nothing to do.
+      if (j == max(n - 2, 0)) { if (more) take(); }
+    }
+    if (ok && n == 0 && more) take();  // (a part of a key range with no tile in it)
+    if (!ok) break;
+    have = false;
+    if (more) next_item();
+  }
+  if (!ok) {
+    // the answer to a request still out, and copies in flight, must land before the block's shared memory is released
+#pragma unroll 1
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+}
+
+// -------------------------------------------------------------------------------------------- warp 1: MMA issuer
+template <int HD>
+__device__ __noinline__ void mma_issuer(const uint32_t smem_base, const uint32_t tmem_base, Shared* sh, const uint64_t limit) {
+  using C = Cfg<HD>;
+  const uint32_t bar0 = ptx::smem_u32(sh->bars);
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  volatile int* abort_flag = &sh->abort_flag;
+  constexpr uint32_t idesc_qk = ptx::umma_idesc_e4m3(TQ, TK);
+  constexpr uint32_t idesc_pv = idesc_f16(TQ, HD) | (1u << 16);  // V: MN-major
+  // Per row tile: the item it is working on and how far it has got.  The two tiles walk the same item sequence and share
+  // the K / V rings, but each advances as soon as its own inputs are ready.
+  int kv0[2] = {0, 0}, kv1[2] = {0, 0};
+  bool have[2] = {false, false}, done[2] = {false, false};
+  int seq[2] = {0, 0};      // items taken from the ring so far
+  int base[2] = {0, 0};     // ring position of the current item's first K / V tile
+  int n[2] = {0, 0};        // key tiles of the current item for this row tile
+  int jq[2] = {0, 0};       // next Q K^T to issue
+  int jp[2] = {0, 0};       // next P V to issue
+  int act[2] = {0, 0};      // items with work for this row tile finished so far
+  int pv_cnt[2] = {0, 0};   // P V products issued so far (phase of p_ready)
+  uint32_t k_used = 0, v_used = 0;  // users that have consumed the tile in each ring slot, 4 bits per slot
+  uint64_t t_idle = 0;
+  uint32_t idle_polls = 0;
+  bool ok = true;
+  while (ok && !(done[0] && done[1])) {
+    bool progress = false;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (done[t]) continue;
+      if (!have[t]) {
+        const int s = seq[t] & (ITEM_SLOTS - 1);
+        if (!ptx::mbar_test_wait(bar(B_IFULL + s), (seq[t] / ITEM_SLOTS) & 1)) continue;
+        kv0[t] = sh->items[s].n_kv0;
+        kv1[t] = sh->items[s].n_kv1;
+        ptx::mbar_arrive(bar(B_IEMPTY + s));
+        ++seq[t];
+        progress = true;
+        if (kv0[t] < 0) { done[t] = true; continue; }
+        n[t] = t == 0 ? kv0[t] : kv1[t];
+        if (n[t] == 0) {  // this item has rows or keys for the other tile only
+          base[t] += max(kv0[t], kv1[t]);
+          continue;
+        }
+        have[t] = true; jq[t] = 0; jp[t] = 0;
+      }
+      if (jp[t] < jq[t]) {
+        // ---- O_t += P_t V_j
+        const int j = jp[t], g = base[t] + j, s = g % V_SLOTS;
+        if (!ptx::mbar_test_wait(bar(B_PREADY + t), pv_cnt[t] & 1)) continue;
+        if (!ptx::mbar_test_wait(bar(B_VFULL + s), (g / V_SLOTS) & 1)) continue;
+        // the first product of an item overwrites O: the previous item's output must have been read out
+        if (j == 0 && act[t] > 0 && !ptx::mbar_test_wait(bar(B_OREAD + t), (act[t] - 1) & 1)) continue;
+        ptx::tc_fence_after();
+        const uint32_t sv = smem_base + C::V_OFF + s * C::V_BYTES;
+        const uint32_t d = tmem_base + t * C::TILE_COLS + C::O_COL;
+        const uint32_t a = tmem_base + t * C::TILE_COLS + C::S_COL;
+#pragma unroll
+        for (int kk = 0; kk < TK / 16; ++kk) {
+          // 16 keys = 16 rows of 128 bytes further into the V tile; 8 packed columns further into P
+          ptx::umma_bf16_ts(d, a + kk * 8, ptx::umma_desc_mn_sw128(sv + kk * 2048, C::V_SUB_BYTES), idesc_pv,
+                            (j > 0 || kk > 0) ? 1u : 0u);
+        }
+        ptx::umma_commit(bar(B_ODONE + t));
+        const uint32_t users = (j < kv0[t] ? 1u : 0u) + (j < kv1[t] ? 1u : 0u);
+        v_used += 1u << (4 * s);
+        if (((v_used >> (4 * s)) & 15u) == users) { ptx::umma_commit(bar(B_VEMPTY + s)); v_used &= ~(15u << (4 * s)); }
+        ++pv_cnt[t]; ++jp[t];
+        progress = true;
+        if (jp[t] == n[t]) {  // item finished for this tile
+          have[t] = false;
+          ++act[t];
+          base[t] += max(kv0[t], kv1[t]);
+          continue;
+        }
+      }
+      if (jq[t] < n[t] && jq[t] == jp[t]) {
+        // ---- S_t = Q_t K_j^T (S is free: the P that aliased it has been consumed by the product above)
+        const int j = jq[t], g = base[t] + j, s = g % K_SLOTS;
+        if (j == 0 && !ptx::mbar_test_wait(bar(B_QFULL + t), act[t] & 1)) continue;
+        if (!ptx::mbar_test_wait(bar(B_KFULL + s), (g / K_SLOTS) & 1)) continue;
+        ptx::tc_fence_after();
+        const uint32_t sq = smem_base + C::Q_OFF + t * C::Q_BYTES;
+        const uint32_t sk = smem_base + C::K_OFF + s * C::CODE_BYTES;
+        const uint32_t d = tmem_base + t * C::TILE_COLS + C::S_COL;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+#pragma unroll
+          for (int kk = 0; kk < HD / 32; ++kk)
+            ptx::umma_f8(d, code_desc<HD>(sq + part * C::CODE_BYTES + kk * 32), code_desc<HD>(sk + kk * 32), idesc_qk,
+                         (part > 0 || kk > 0) ? 1u : 0u);
+        }
+        ptx::umma_commit(bar(B_SFULL + t));
+        const uint32_t users = (j < kv0[t] ? 1u : 0u) + (j < kv1[t] ? 1u : 0u);
+        k_used += 1u << (4 * s);
+        if (((k_used >> (4 * s)) & 15u) == users) { ptx::umma_commit(bar(B_KEMPTY + s)); k_used &= ~(15u << (4 * s)); }
+        ++jq[t];
+        if (jq[t] == n[t]) ptx::umma_commit(bar(B_QEMPTY + t));  // the tile's Q buffer may be refilled
+        progress = true;
+      }
+    }
+    if (progress) {
+      idle_polls = 0;
+      t_idle = 0;
+    } else if ((++idle_polls & 1023u) == 0u) {
+      // nothing could be issued for a while: look at the abort flag and the clock
+      if (*abort_flag) { ok = false; break; }
+      const uint64_t now = ptx::globaltimer_ns();
+      if (t_idle == 0) t_idle = now;
+      else if (now - t_idle > limit) { *abort_flag = 1; ok = false; }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------- warps 10, 11: V tiles
+template <int HD>
+__device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_t smem_base, Shared* sh, const int half,
+                                         const uint64_t limit) {
+  using C = Cfg<HD>;
+  constexpr int LPR = HD / 16, RPL = 32 / LPR;     // lanes per row (16 codes each), rows at a time
+  const uint32_t bar0 = ptx::smem_u32(sh->bars);
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  volatile int* abort_flag = &sh->abort_flag;
+  const int lane = threadIdx.x & 31;
+  const int row_lo = half * 64;                    // this warp's rows of a tile
+  // 16 codes are two chunks of a row; lanes of the second half of a 128-feature row store theirs in the other order, so
+  // that eight lanes cover all banks
+  const int c = (lane % LPR) * 2, odd = HD == 128 ? (lane >> 2) & 1 : 0;
+  int seq = 0, g = 0;  // items taken, tiles converted so far
+  bool ok = true;
+  while (ok) {
+    int n, keys;
+    {
+      const int s = seq & (ITEM_SLOTS - 1);
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
+      if (!ok) break;
+      const Item& it = sh->items[s];
+      n = it.n_kv0 < 0 ? -1 : max(it.n_kv0, it.n_kv1);
+      keys = it.pre + it.len - it.jb * TK;  // that the request holds, from the item's first tile on
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar(B_IEMPTY + s));
+      ++seq;
+    }
+    if (n < 0) break;
+#pragma unroll 1
+    for (int j = 0; j < n; ++j, ++g, keys -= TK) {
+      const int s = g % V_SLOTS, r = g % R_SLOTS;
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_RFULL + r), (g / R_SLOTS) & 1, abort_flag, limit));
+      if (!ok) break;
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_VEMPTY + s), ((g / V_SLOTS) & 1) ^ 1u, abort_flag, limit));
+      if (!ok) break;
+      const uint32_t src = smem_base + C::R_OFF + r * C::CODE_BYTES + lane * 16, dst = smem_base + C::V_OFF + s * C::V_BYTES;
+      // codes * 2^(page exponent - unit) -> f16 operand rows
+#pragma unroll 1
+      for (int r0 = row_lo; r0 < row_lo + 64; r0 += 16) {
+        uint4 v[16 / RPL];
+#pragma unroll
+        for (int q = 0; q < 16 / RPL; ++q)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[q].x), "=r"(v[q].y), "=r"(v[q].z), "=r"(v[q].w)
+                       : "r"(src + (r0 + q * RPL) * HD));
+        const int d = sh->info[g % INFO_SLOTS].v_rel[r0 >> 4];
+        const float m = d < -24 ? 0.f : exp2_int(d);
+        const uint32_t m2 = pack_f16(m, m);
+        // rows past the last key, and rows of a page that does not exist, become zeros: 0 * (whatever) must stay 0
+        const int valid = d == kNoRows ? 0 : keys;
+#pragma unroll
+        for (int q = 0; q < 16 / RPL; ++q) {
+          const int row = r0 + q * RPL + lane / LPR;
+          if (row >= valid) v[q] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const bool second = (h ^ odd) != 0;
+            const uint32_t x = second ? v[q].z : v[q].x, y = second ? v[q].w : v[q].y;
+            const uint32_t h0 = e4m3x2_to_f16x2(static_cast<uint16_t>(x)), h1 = e4m3x2_to_f16x2(static_cast<uint16_t>(x >> 16));
+            const uint32_t h2 = e4m3x2_to_f16x2(static_cast<uint16_t>(y)), h3 = e4m3x2_to_f16x2(static_cast<uint16_t>(y >> 16));
+            sts128(dst + v_off<HD>(row, c + (h ^ odd)), mul_f16x2(h0, m2), mul_f16x2(h1, m2), mul_f16x2(h2, m2), mul_f16x2(h3, m2));
+          }
+        }
+      }
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        ptx::mbar_arrive(bar(B_REMPTY + r));
+        if (!(p.test_skip_arrive && half == 1 && g == 1)) ptx::mbar_arrive(bar(B_VFULL + s));
+      }
+    }
+  }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                     const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ PagedPrefillDev p) {
+  using C = Cfg<HD>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  Shared* sh = reinterpret_cast<Shared*>(smem_raw + (smem_base - ptx::smem_u32(smem_raw)) + C::AUX_OFF);
+  const uint32_t bar0 = ptx::smem_u32(sh->bars);
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  const uint64_t limit = p.wait_limit_ns;
+  volatile int* abort_flag = &sh->abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int i = 0; i < N_BARS; ++i) {
+      int count = 1;
+      if (i >= B_QFULL && i < B_QFULL + 2) count = 4;
+      if (i >= B_VFULL && i < B_VFULL + V_SLOTS) count = 2;         // the two V warps
+      if (i >= B_REMPTY && i < B_REMPTY + R_SLOTS) count = 2;
+      if (i >= B_PREADY && i < B_PREADY + 2) count = 4;             // the four softmax warps of the tile
+      if (i >= B_OREAD && i < B_OREAD + 2) count = 4;
+      if (i >= B_IEMPTY && i < B_IEMPTY + ITEM_SLOTS) count = 12;   // eight softmax warps, the MMA thread once per tile, two V warps
+      ptx::mbar_init(bar(i), count);
+    }
+    ptx::fence_barrier_init();
+    ptx::prefetch_tensormap(&tmap_q);
+    ptx::prefetch_tensormap(&tmap_k);
+    ptx::prefetch_tensormap(&tmap_v);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(ptx::smem_u32(&sh->tmem), 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = sh->tmem;
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+
+  if (warp == 0) {
+    producer<HD>(&tmap_q, &tmap_k, &tmap_v, p, smem_base, sh, limit);
+  } else if (warp == 1) {
+    if (lane == 0) mma_issuer<HD>(smem_base, tmem_base, sh, limit);
+  } else if (warp >= 10) {
+    v_converter<HD>(p, smem_base, sh, warp - 10, limit);
+  } else {
+    // ---------------------------------------------------------------- softmax
+    const int t = (warp - 2) >> 2;       // row tile of this warpgroup
+    const int lane_group = warp & 3;     // tensor-memory lanes this warp may touch
+    const int row = lane_group * 32 + lane;
+    const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(lane_group * 32) << 16) + t * C::TILE_COLS;
+    const int group = p.n_q_heads / p.n_kv_heads;
+    const int row_token = row / group, row_head = row - row_token * group;
+    int seq = 0;    // items taken from the ring so far
+    int base = 0;   // ring position of the current item's first key tile
+    int step = 0;   // key tiles this row tile has processed so far, over all items (phase of s_full / o_done)
+    int act = 0;    // items with work for this row tile
+    bool q_ready = false;  // the next one's q has been converted
+    bool ok = true;
+    while (ok) {
+      Item it;
+      {
+        const int s = seq & (ITEM_SLOTS - 1);
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
+        if (!ok) break;
+        it = sh->items[s];
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(B_IEMPTY + s));
+        ++seq;
+      }
+      if (it.n_kv0 < 0) break;  // no more items
+      const int n_kv = t == 0 ? it.n_kv0 : it.n_kv1;
+      const int item_base = base;
+      base += max(it.n_kv0, it.n_kv1);
+      const int token0 = it.t0 + t * p.tile_tokens;
+      const bool mine = row < tile_rows(p, it, t, group);
+      const size_t out_row = static_cast<size_t>(it.start + token0 + row_token) * p.n_q_heads + it.kvh * group + row_head;
+      if (n_kv == 0) {  // no rows, or no keys in this part of the range
+        if (p.n_splits > 1 && mine)
+          p.parts.ml[static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row] = make_float2(-CUDART_INF_F, 0.f);
+        continue;
+      }
+      if (!q_ready) {  // (a block's first item, or the one after an item without work for this tile)
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_QRAW + t), act & 1, abort_flag, limit));
+        if (!ok) break;
+        convert_q<HD>(smem_base + C::Q_OFF + t * C::Q_BYTES, lane_group * 32, sh->row_exp[act & 1][t]);
+        if (lane == 0) ptx::mbar_arrive(bar(B_QFULL + t));
+      }
+      q_ready = false;
+      const int row_pos = it.pre + token0 + row_token;  // last key the row may see
+      float m_used = -CUDART_INF_F, l_sum = 0.f, row_scale = 0.f;
+      int v_exp = 0;
+#pragma unroll 1
+      for (int j = 0; j < n_kv; ++j, ++step) {
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_SFULL + t), step & 1, abort_flag, limit));
+        if (!ok) break;
+        ptx::tc_fence_after();
+        // (written before the barriers that S waited for)
+        if (j == 0) row_scale = mine ? rsqrtf(static_cast<float>(HD)) * LOG2E_F * exp2_int(sh->row_exp[act & 1][t][row]) : 1.f;
+        const TileInfo& info = sh->info[(item_base + j) % INFO_SLOTS];
+        // factor of the scores, per 16 keys (not 0: -inf * 0); read again where it is used, registers are short
+        auto sl = [&](int c) { return fmaxf(row_scale * *const_cast<volatile const float*>(&info.k_mul[c]), 1.17549435e-38f); };
+        const int tile_v_exp = info.v_exp;
+        const int k0 = (it.jb + j) * TK;
+        uint32_t sv[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_lane + C::S_COL + c * 32, sv[c]);
+        ptx::tmem_ld_wait();
+        if (k0 + TK - 1 > it.pre + token0) {  // warp-uniform: some row of the tile does not see all keys
+          const int lim = row_pos - k0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (c * 32 + e > lim) sv[c][e] = 0xff800000u;  // -inf
+          }
+        }
+        // row maximum: three-input maxima over 16 keys, scaled, over the groups
+        float mx8[TK / 16];
+#pragma unroll
+        for (int c = 0; c < TK / 16; ++c) {
+          const uint32_t(&v)[32] = sv[c >> 1];
+          const int o = (c & 1) * 16;
+          float m = fmaxf(__uint_as_float(v[o]), __uint_as_float(v[o + 1]));
+#pragma unroll
+          for (int e = 2; e < 16; e += 2) m = ptx::fmax3(m, __uint_as_float(v[o + e]), __uint_as_float(v[o + e + 1]));
+          mx8[c] = m * sl(c);
+        }
+        const float mx = fmaxf(ptx::fmax3(ptx::fmax3(mx8[0], mx8[1], mx8[2]), mx8[3], mx8[4]), ptx::fmax3(mx8[5], mx8[6], mx8[7]));
+        // lazy reference: keep the old one unless this tile exceeds it by more than the threshold; the unit of V may grow
+        float factor = 1.f;
+        bool grow = false;
+        if (j == 0) {
+          m_used = mx;
+          v_exp = tile_v_exp;
+        } else {
+          if (mx > m_used + RESCALE_THRESHOLD) {
+            factor = ptx::ex2_approx(m_used - mx);  // (0 if the row had seen no key)
+            m_used = mx;
+            l_sum *= factor;
+            grow = true;
+          }
+          if (tile_v_exp > v_exp) {
+            factor *= exp2_int(v_exp - tile_v_exp);
+            v_exp = tile_v_exp;
+            grow = true;
+          }
+        }
+        if (__any_sync(0xffffffffu, grow)) {
+          // O must be stable: the P V product of the previous tile has finished
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + t), (step - 1) & 1, abort_flag, limit));
+          if (!ok) break;
+          ptx::tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < HD / 32; ++c) {
+            uint32_t ov[32];
+            ptx::tmem_ld_32x32(t_lane + C::O_COL + c * 32, ov);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * factor);
+            ptx::tmem_st_32x32(t_lane + C::O_COL + c * 32, ov);
+          }
+          ptx::tmem_st_wait();
+        }
+        // 2^7 p = 2^(s * scale - m + 7) for a pair of keys at a time
+        const float neg_m = (m_used == -CUDART_INF_F ? 0.f : -m_used) + P_SHIFT;
+        const uint64_t negm_2 = ptx::pack_f32x2(neg_m, neg_m);
+        uint64_t ps[4] = {0ull, 0ull, 0ull, 0ull}, sl2 = 0ull;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            // packed column 32 c + e holds keys 2 (32 c + e) and 2 (32 c + e) + 1
+            const int k_lo = (c * 32 + e) * 2;
+            const uint64_t x2 = ptx::pack_f32x2(__uint_as_float(sv[k_lo >> 5][k_lo & 31]),
+                                                __uint_as_float(sv[k_lo >> 5][(k_lo & 31) + 1]));
+            if (e % 8 == 0) {
+              const float f = sl(k_lo >> 4);
+              sl2 = ptx::pack_f32x2(f, f);
+            }
+            float y0, y1;
+            ptx::unpack_f32x2(ptx::fma_f32x2(x2, sl2, negm_2), y0, y1);
+            const float p0 = ptx::ex2_approx(y0), p1 = ptx::ex2_approx(y1);
+            ps[e & 3] = ptx::add_f32x2(ps[e & 3], ptx::pack_f32x2(p0, p1));
+            pk[e] = pack_f16(p0, p1);
+          }
+          ptx::tmem_st_32x32(t_lane + C::S_COL + c * 32, pk);
+        }
+        {
+          float a0, a1;
+          ptx::unpack_f32x2(ptx::add_f32x2(ptx::add_f32x2(ps[0], ps[1]), ptx::add_f32x2(ps[2], ps[3])), a0, a1);
+          l_sum += a0 + a1;
+        }
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(B_PREADY + t));
+      }
+      if (!ok) break;
+      ++act;
+      // ---- while the item's last P V product runs: q of the next item (its copy started when the last Q K^T had run)
+      {
+        const int s = seq & (ITEM_SLOTS - 1);
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
+        if (!ok) break;
+        if ((t == 0 ? sh->items[s].n_kv0 : sh->items[s].n_kv1) > 0 && sh->items[s].n_kv0 >= 0) {
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_QRAW + t), act & 1, abort_flag, limit));
+          if (!ok) break;
+          convert_q<HD>(smem_base + C::Q_OFF + t * C::Q_BYTES, lane_group * 32, sh->row_exp[act & 1][t]);
+          if (lane == 0) ptx::mbar_arrive(bar(B_QFULL + t));
+          q_ready = true;
+        }
+      }
+      // ---- it has finished: store the tile's rows
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + t), (step - 1) & 1, abort_flag, limit));
+      if (!ok) break;
+      ptx::tc_fence_after();
+      // the whole row first, so that the next item's first product may overwrite O as early as possible
+      uint32_t ov[HD / 32][32];
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) ptx::tmem_ld_32x32(t_lane + C::O_COL + c * 32, ov[c]);
+      ptx::tmem_ld_wait();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar(B_OREAD + t));
+      // o = O 2^(v_exp) / (sum of 2^7 p); the two factors apart, so that neither leaves the normal range
+      const float unit = exp2_int(v_exp);
+      if (mine && p.n_splits == 1) {
+        const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
+        bf16* dst = p.o + out_row * HD;
+        // a thread owns a row, so every store of a warp touches 32 different lines: 32-byte stores halve their number
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 16) {
+            uint32_t w[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              w[q] = ptx::pack_bf16(__uint_as_float(ov[c][e + 2 * q]) * inv * unit, __uint_as_float(ov[c][e + 2 * q + 1]) * inv * unit);
+            ptx::st_global_v8(dst + c * 32 + e, w);
+          }
+        }
+      } else if (mine) {
+        const size_t part = static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row;
+        float* dst = p.parts.o + part * HD;
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t w[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) w[q] = __float_as_uint(__uint_as_float(ov[c][e + q]) * unit);
+            ptx::st_global_v8(dst + c * 32 + e, w);
+          }
+        }
+        p.parts.ml[part] = make_float2(m_used, l_sum);
+      }
+      __syncwarp();
+    }
+  }
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag && p.err_word) atomicExch(p.err_word, 1);
+  if (warp == 1) {
+    __syncwarp();
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem_base, 512);
+  }
+}
+
+template <int HD>
+pd_status launch(const PagedPrefillDev& p, long long items, cudaStream_t s) {
+  static PerDeviceInt smem_opt_in;
+  PD_TRY(opt_in_smem(smem_opt_in, paged_prefill_kernel<HD>, Cfg<HD>::SMEM_BYTES));
+  CUtensorMap tq, tk, tv;
+  PD_TRY(make_tmap_heads(&tq, p.q, p.n_tokens, p.n_q_heads, HD, p.ldq, p.tile_tokens, p.n_q_heads / p.n_kv_heads, HD / 2));
+  const uint64_t rows = (static_cast<uint64_t>(p.c.n_pages) * p.n_kv_heads) << p.c.log2_page;
+  PD_TRY(make_tmap_u8(&tk, p.c.k, rows, HD, HD, 1u << p.c.log2_page, HD));
+  PD_TRY(make_tmap_u8(&tv, p.c.v, rows, HD, HD, 1u << p.c.log2_page, 0));
+  PD_CUDA_TRY(launch_pdl(paged_prefill_kernel<HD>, dim3(static_cast<unsigned>(items)), dim3(THREADS), Cfg<HD>::SMEM_BYTES, s, tq, tk, tv, p));
+  count_launch();
+  if (p.n_splits > 1) return launch_paged_join(p.parts, p.o, 1ll * p.n_tokens * p.n_q_heads, p.n_splits, HD, s);
+  return PD_OK;
+}
+
+}  // namespace
+
+size_t paged_tiles_part_rows() { return static_cast<size_t>(MAX_SPLIT_ITEMS) * 2 * TQ; }
+
+// Key ranges are cut while the parts still fit the SMs together, into parts of at least two key tiles.
+int paged_tiles_splits(long long items, int max_kv) {
+  long long want = MAX_SPLIT_ITEMS / items;
+  const long long most = (max_kv + TK - 1) / TK / 2;
+  if (want > most) want = most;
+  return want > 1 ? static_cast<int>(want) : 1;
+}
+
+pd_status launch_paged_tiles(const PagedRuns& r, const PagedParts& parts, cudaStream_t s) {
+  // rows of K are addressed with 32-bit numbers
+  if ((static_cast<long long>(r.c.n_pages) * r.n_kv_heads << r.c.log2_page) > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
+  PagedPrefillDev p{};
+  p.q = r.q; p.o = r.o; p.cu_seqlens = r.cu_seqlens; p.prefix = r.prefix; p.parts = parts; p.err_word = r.err_word; p.c = r.c;
+  p.ldq = r.ldq; p.n_req = r.n_req; p.n_tokens = r.n_tokens; p.n_q_heads = r.n_q_heads; p.n_kv_heads = r.n_kv_heads;
+  p.tile_tokens = TQ / (r.n_q_heads / r.n_kv_heads);
+  p.n_splits = paged_tiles_splits(r.tile_blocks * r.n_kv_heads, r.max_kv);
+  p.n_slots = first_slot(r.n_tokens, r.n_req, 2 * p.tile_tokens);
+  const long long items = 1ll * p.n_slots * p.n_splits * r.n_kv_heads;
+  if (items > 0x3fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
+  p.wait_limit_ns = 4000000000ull;
+  {
+    unsigned long long inj = 0;
+    if (take_wait_injection(PD_INJECT_ATTN_PAGED, &inj)) { p.wait_limit_ns = inj; p.test_skip_arrive = 1; }
+  }
+  return r.head_dim == 128 ? launch<128>(p, items, s) : launch<64>(p, items, s);
+}
+
+}  // namespace pd

@@ -102,9 +102,15 @@ class TraceScope {
 pd_status make_tmap_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
                          uint32_t box_rows);
 
-// The same for one-byte elements (FP8 codes): boxes of box_rows x 128 columns.
+// The same for one-byte elements (FP8 codes): boxes of box_rows x 128 columns with the 128-byte swizzle, x 64 columns with
+// the 64-byte swizzle, or (box_cols = 0) of whole rows without one.
 pd_status make_tmap_u8(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
-                       uint32_t box_rows);
+                       uint32_t box_rows, uint32_t box_cols = 128);
+
+// 3-D bf16 tensor [tokens, heads, hd] whose token rows are `ld` elements apart, in boxes of box_tokens x box_heads x
+// box_cols elements without a swizzle.
+pd_status make_tmap_heads(CUtensorMap* out, const void* base, uint64_t tokens, uint64_t heads, uint64_t hd, uint64_t ld,
+                          uint32_t box_tokens, uint32_t box_heads, uint32_t box_cols);
 
 // ------------------------------------------------------------------ GEMM
 enum GemmEpilogue : int {

@@ -56,17 +56,36 @@ pd_status make_tmap_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint
 }
 
 pd_status make_tmap_u8(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
-                       uint32_t box_rows) {
+                       uint32_t box_rows, uint32_t box_cols) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) return PD_ERR_CUDA;
-  if ((reinterpret_cast<uintptr_t>(base) & 15u) || ld % 16 != 0 || box_rows == 0 || box_rows > 256)
+  if ((reinterpret_cast<uintptr_t>(base) & 15u) || ld % 16 != 0 || box_rows == 0 || box_rows > 256 ||
+      (box_cols != 128 && box_cols != 64 && box_cols != 0))
     return PD_ERR_INVALID_ARG;
   cuuint64_t dims[2] = {cols, rows};
   cuuint64_t strides[1] = {ld};
-  cuuint32_t box[2] = {128, box_rows};
+  cuuint32_t box[2] = {box_cols ? box_cols : static_cast<cuuint32_t>(cols), box_rows};
   cuuint32_t estr[2] = {1, 1};
   CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 128   ? CU_TENSOR_MAP_SWIZZLE_128B
+                  : box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                   : CU_TENSOR_MAP_SWIZZLE_NONE,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? PD_OK : PD_ERR_INVALID_ARG;
+}
+
+pd_status make_tmap_heads(CUtensorMap* out, const void* base, uint64_t tokens, uint64_t heads, uint64_t hd, uint64_t ld,
+                          uint32_t box_tokens, uint32_t box_heads, uint32_t box_cols) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return PD_ERR_CUDA;
+  if ((reinterpret_cast<uintptr_t>(base) & 15u) || (ld * 2) % 16 != 0 || (box_cols * 2) % 16 != 0) return PD_ERR_INVALID_ARG;
+  cuuint64_t dims[3] = {hd, heads, tokens};
+  cuuint64_t strides[2] = {hd * 2, ld * 2};
+  cuuint32_t box[3] = {box_cols, box_heads, box_tokens};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? PD_OK : PD_ERR_INVALID_ARG;
 }

@@ -66,6 +66,73 @@ __device__ __forceinline__ float page_scale(float amax) {
 // 1 / s of a power of two s = 2^e, |e| <= 126: the exponent field mirrored.
 __device__ __forceinline__ float pow2_inverse(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
 
+// Blocks of `block_tokens` consecutive tokens of one request: request r owns the slots from first_slot(cu[r], r) on, as many as
+// it has such blocks, or one more (a single request exactly as many), so the host needs only the number of tokens.
+__host__ __device__ __forceinline__ int first_slot(int cu, int r, int block_tokens) {
+  return static_cast<int>((static_cast<uint32_t>(cu) + static_cast<uint32_t>(r) * (block_tokens - 1)) / block_tokens);
+}
+struct TokenBlock {
+  int req, start, len, pre;  // request, its first row, its rows, tokens cached before them
+  int t0;                    // the block's first token within the request; not below len: no block in this slot
+};
+// The block of a slot.  All lanes of a warp search together, 32 candidates at a time; for up to 32 requests the warp has
+// every request's numbers after one load.
+__device__ __forceinline__ TokenBlock find_block(const int32_t* cu_seqlens, const int32_t* prefix, int n_req, int n_tokens, int slot,
+                                                 int block_tokens) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = n_req;  // the request lies in lo .. lo + n - 1
+  while (n > 32) {
+    const int stride = (n + 31) / 32, r = lo + lane * stride;
+    const bool at_or_before = lane * stride < n && first_slot(cu_seqlens[r], r, block_tokens) <= slot;
+    const int k = 31 - __clz(__ballot_sync(0xffffffffu, at_or_before) | 1u);
+    lo += k * stride;
+    n = min(stride, n - k * stride);
+  }
+  const int r = lo + min(lane, n - 1);
+  const int c0 = cu_seqlens[r], c1 = cu_seqlens[r + 1], pre = prefix ? prefix[r] : 0;
+  const int k = 31 - __clz(__ballot_sync(0xffffffffu, lane < n && first_slot(c0, r, block_tokens) <= slot) | 1u);
+  TokenBlock b;
+  b.req = lo + k;
+  b.start = __shfl_sync(0xffffffffu, c0, k);
+  b.len = min(__shfl_sync(0xffffffffu, c1, k), n_tokens) - b.start;
+  b.pre = __shfl_sync(0xffffffffu, pre, k);
+  b.t0 = (slot - first_slot(b.start, b.req, block_tokens)) * block_tokens;
+  if (b.t0 < 0 || b.pre < 0) b.t0 = 0x7fffffff;  // (never with consistent inputs)
+  return b;
+}
+
+// Attention of ragged runs of fresh rows over the cache, as the kernels behind pd_paged_prefill_attention take it.
+struct PagedRuns {
+  const bf16* q;              // [T, ldq]
+  bf16* o;                    // [T, Hq*hd]
+  const int32_t* cu_seqlens;  // device [n_req + 1]
+  const int32_t* prefix;      // device [n_req] or NULL
+  int* err_word;
+  PagedCache c;
+  int ldq, n_req, n_tokens, n_q_heads, n_kv_heads, head_dim;
+  int max_kv;                 // longest prefix + run
+  long long tile_blocks;      // blocks of 256 (token, head) rows over all requests and one KV head
+};
+// Partial results of rows whose key range is cut: outputs [n_splits, rows, hd] (relative to m) and (m, l) [n_splits, rows], row =
+// token * Hq + head, m in log2 units.  A part without keys has m = -inf, l = 0 and need not have stored outputs.
+struct PagedParts {
+  float* o;
+  float2* ml;
+};
+inline size_t paged_parts_ml_offset(size_t part_rows, int head_dim) { return align_up(part_rows * head_dim * sizeof(float), 256); }
+inline size_t paged_parts_bytes(size_t part_rows, int head_dim) {
+  return paged_parts_ml_offset(part_rows, head_dim) + align_up(part_rows * sizeof(float2), 256);
+}
+pd_status launch_paged_join(const PagedParts& parts, bf16* o, long long rows, int n_splits, int head_dim, cudaStream_t s);
+// The streaming kernel of decode attention over blocks of a few tokens, and how many (token, head) rows a block has.
+int paged_rows_block(int group, int longest_run);
+pd_status launch_paged_rows(const PagedRuns& r, int longest_run, const PagedParts& parts, cudaStream_t s);
+size_t paged_rows_part_rows();  // rows of partial results that the launch may need
+// The tensor-memory kernel.
+pd_status launch_paged_tiles(const PagedRuns& r, const PagedParts& parts, cudaStream_t s);
+size_t paged_tiles_part_rows();
+int paged_tiles_splits(long long items, int max_kv);  // parts that the key ranges of `items` row blocks are cut into
+
 // Two E4M3 codes (bits 0-15) -> two halves, exactly.
 __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t c) {
   uint32_t r;

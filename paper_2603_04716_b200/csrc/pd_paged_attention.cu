@@ -1,13 +1,13 @@
-// Attention over the 8-bit paged KV cache: one query token per sequence (pd_paged_decode_attention) and the fresh rows of
-// ragged requests (pd_paged_prefill_attention).
+// Attention over the 8-bit paged KV cache for few query rows: one token per sequence (pd_paged_decode_attention) or short runs
+// of tokens (one of the kernels behind pd_paged_prefill_attention).
 //
-// Decode.  o = softmax(q K^T / sqrt(hd)) V per query head over the sequence's pages; K and V of a page are E4M3 codes times
-// one power of two.  HBM-bound: every code byte is read once.  One block per (split of the key range, KV head, sequence);
+// o = softmax(q K^T / sqrt(hd)) V per query head over the sequence's pages; K and V of a page are E4M3 codes times
+// one power of two.  HBM-bound: every code byte is read once (by every block of tokens of a run).  One block per (split of the key range, KV
+// head, sequence or block of tokens);
 // every warp streams its own 16-key tiles through a private cp.async ring (a tile never crosses a page, so it has one page
 // number and one pair of scales).
-//   S^T = K Q^T    m16n8k16 in f16: rows are 16 keys, columns 8 heads of the group.
-//   O^T = V^T P^T  m16n8k16: rows are features, columns 8 heads.  Heads are columns, so a group of at most 8 wastes no
-//                  product (a legacy tensor instruction suffices: both products of a tile are 16 instructions for 4 KB).
+//   S^T = K Q^T    m16n8k16 in f16: rows are 16 keys, columns 8 (token, head of the group) pairs.
+//   O^T = V^T P^T  m16n8k16: rows are features.  Pairs are columns, so a group of at most 8 heads wastes no product (a legacy tensor instruction suffices: both products of a tile are 16 instructions for 4 KB).
 // E4M3 -> f16 is exact and one instruction for two codes.  The contraction order of a product is free, so a lane takes 16
 // neighbouring features of a K row as its share of four k-steps, and 16 neighbouring features of four V rows (byte-permuted
 // into pairs of keys): all shared-memory reads are 16 bytes wide, and the row order within a group of 8 keys is chosen so
@@ -24,14 +24,16 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct PagedDecodeArgs {
-  const bf16* q;          // [B, ldq]
-  bf16* o;                // [B, Hq*hd]
-  const int32_t* kv_len;  // [B]
-  float* partial;         // when n_splits > 1: outputs [B, Hkv, n_splits, G, hd], then (max, sum) pairs [B, Hkv, n_splits, G]
+  const bf16* q;              // [rows, ldq]
+  bf16* o;                    // [rows, Hq*hd]
+  const int32_t* cu_seqlens;  // runs: [n_req + 1]; NULL: sequence b has the one row b
+  const int32_t* kv_len;      // [n_req] position of the first row; runs: may be NULL (0)
+  PagedParts parts;           // used when n_splits > 1
   int* err_word;
   PagedCache c;
-  int ldq, batch, n_q_heads, n_kv_heads;
-  int n_splits, chunk;    // block x covers keys x * chunk .. (the last one whatever lies behind); chunk is a multiple of 64
+  int ldq, rows, n_req, n_q_heads, n_kv_heads;
+  int block_tokens;           // tokens of a block: block_tokens * group columns
+  int n_splits, chunk;        // block x covers keys x * chunk .. (the last one whatever lies behind); chunk is a multiple of 64
 };
 
 constexpr int PA_WARPS = 8;
@@ -40,7 +42,8 @@ constexpr int PA_KEYS = 16;
 constexpr int PA_STAGES = 3;
 // p is kept as 2^7 p relative to a reference that may lag the running maximum by 2^8: at most 2^15, below f16's 65504.
 constexpr float P_SHIFT = 7.f, P_SLACK = 8.f, P_UNIT = 1.f / 128.f;
-constexpr int PA_MIN_CHUNK = 256;               // keys of a run at least
+constexpr int PA_MIN_CHUNK = 256;               // keys of a part at least
+constexpr int PA_RESIDENT = 296;                // blocks that run together (half as many WIDE ones)
 constexpr float P_FAR = 1.f / 1024.f;
 
 template <int HD>
@@ -77,11 +80,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Entries of sequence b that the call attends to.
-__device__ __forceinline__ int visible_keys(const PagedDecodeArgs& a, int b) {
-  const int cap = a.c.table_ld << a.c.log2_page, len = a.kv_len[b];
-  return len >= cap ? cap : max(len + 1, 0);
-}
 // The transpose of an 8 x 8 matrix of halves held one row per four lanes.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
@@ -99,22 +97,33 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   return v;
 }
 
-// WIDE: groups of 9 to 16 query heads (two column groups in both products).
-template <int HD, bool WIDE>
+// WIDE: 9 to 16 columns (two column groups in both products).  RUNS: blocks of several tokens; the one-token form is kept
+// apart because its registers are few (with the masks of several tokens in it, a single long sequence took 1.4 times as long).
+template <int HD, bool WIDE, bool RUNS>
 __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(const PagedDecodeArgs a) {
   using SM = PagedSmem<HD>;
   constexpr int KS = HD / 16;          // k-steps of K Q^T
   constexpr int MT = HD / 16;          // 16-feature tiles of O^T
   constexpr int NC = WIDE ? 2 : 1;     // column groups of 8 heads
   extern __shared__ __align__(128) uint8_t smem[];
-  const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+  const int split = blockIdx.x, kvh = blockIdx.y;
   const int group = a.n_q_heads / a.n_kv_heads;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, t4 = lane & 3;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
 
-  const int l2p = a.c.log2_page;
+  const int l2p = a.c.log2_page, cap = a.c.table_ld << l2p;
+  int b = blockIdx.z, row0 = b, n_tok = 1, pos0 = 0;  // sequence, first row, tokens, position of the first token
+  if (RUNS) {
+    const TokenBlock blk = find_block(a.cu_seqlens, a.kv_len, a.n_req, a.rows, b, a.block_tokens);
+    if (blk.t0 >= blk.len) return;
+    b = blk.req;
+    row0 = blk.start + blk.t0;
+    n_tok = min(a.block_tokens, blk.len - blk.t0);
+    pos0 = blk.pre + blk.t0;
+  }
+  const int n_cols = n_tok * group;
   // Page numbers of 32 tiles of this warp at a time, a tile per lane.  The first 32 are read before the sequence's length is
   // known: entries behind its last page are read, too, but not used.
   const int32_t* table = a.c.table + static_cast<size_t>(b) * a.c.table_ld;
@@ -122,21 +131,35 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
   auto page_of = [&](int tile) { return (split_begin + (tile * PA_WARPS + warp) * PA_KEYS) >> l2p; };
   const long long first_page = page_of(lane);
   int id_cur = first_page < a.c.table_ld ? table[first_page] : -1;
-  // q of head c * 8 + g: this lane's share of every k-step
+  // Column c * 8 + j is token (c * 8 + j) / group, head (c * 8 + j) % group.  q of column c * 8 + g: this lane's share of every
+  // k-step
+  const uint32_t inv_group = 65536u / group + 1u;
+  auto token_of = [&](int col) { return RUNS ? static_cast<int>((col * inv_group) >> 16) : 0; };
   uint2 qw[NC][KS];
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int c = 0; c < NC; ++c) {
+    const int tok = token_of(c * 8 + g), head = c * 8 + g - tok * group;
+    const bf16* src = a.q + static_cast<size_t>(row0 + tok) * a.ldq + (kvh * group + head) * HD + t4 * 16;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-      qw[c][s] = c * 8 + g < group
-                     ? *reinterpret_cast<const uint2*>(a.q + static_cast<size_t>(b) * a.ldq + (kvh * group + c * 8 + g) * HD +
-                                                       (s >> 2) * 64 + t4 * 16 + (s & 3) * 4)
-                     : make_uint2(0u, 0u);
-  if (split == 0 && kvh == 0 && tid == 0 && a.err_word && a.kv_len[b] >= (a.c.table_ld << l2p)) atomicExch(a.err_word, 2);
-  const int total = visible_keys(a, b);
-  const int k_begin = static_cast<int>(min(1ll * total, 1ll * split * a.chunk));
+      qw[c][s] = c * 8 + g < n_cols ? *reinterpret_cast<const uint2*>(src + (s >> 2) * 64 + (s & 3) * 4) : make_uint2(0u, 0u);
+  }
+  if (!RUNS) pos0 = min(a.kv_len[b], cap);
+  if (split == 0 && kvh == 0 && tid == 0 && a.err_word && pos0 + n_tok > cap) atomicExch(a.err_word, 2);
+  // keys that the last token sees; 0: none (a padding row)
+  const int total = max(min(pos0 + n_tok, cap), 0);
+  const int k_begin = static_cast<int>(min(1ll * total, split_begin));
   const int k_end = split == a.n_splits - 1 ? total : static_cast<int>(min(1ll * total, 1ll * k_begin + a.chunk));
-  if (split > 0 && k_begin == k_end) return;  // (the merge knows how many splits hold keys)
+  // the row of column `col` among the partial results, and among the outputs (split 0)
+  auto out_row = [&](int col) {
+    const int tok = token_of(col);
+    return static_cast<size_t>(row0 + tok) * a.n_q_heads + kvh * group + col - tok * group;
+  };
+  const size_t part_row0 = static_cast<size_t>(split) * a.rows * a.n_q_heads;
+  if (split > 0 && k_begin == k_end) {
+    if (tid < n_cols) a.parts.ml[part_row0 + out_row(tid)] = make_float2(-CUDART_INF_F, 0.f);
+    return;
+  }
   const int n_tiles_blk = (k_end - k_begin + PA_KEYS - 1) / PA_KEYS;
   const int my_tiles = (n_tiles_blk > warp) ? (n_tiles_blk - warp + PA_WARPS - 1) / PA_WARPS : 0;
   const uint32_t ring = ptx::smem_u32(smem) + warp * (PA_STAGES * 2 * SM::TILE);
@@ -214,7 +237,7 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
       qb[c][s][1] = pack_f16(ptx::bf16_lo(qw[c][s].y) * inv, ptx::bf16_hi(qw[c][s].y) * inv);
     }
   }
-  // This lane's columns of S^T and O^T are heads c * 8 + 2 t4 + h, h = 0, 1.
+  // This lane's columns of S^T and O^T are c * 8 + 2 t4 + h, h = 0, 1.
   float f_head[NC][2];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -273,7 +296,7 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
       }
     }
     // ---- softmax
-    const bool masked = key0 + PA_KEYS > k_end || ks < 0.f;
+    const bool masked = key0 + PA_KEYS > (RUNS ? min(k_end, pos0 + 1) : k_end) || ks < 0.f;
     float x[NC][4];  // [key half][head] = (e >> 1, e & 1)
     bool grow = false;
 #pragma unroll
@@ -282,9 +305,13 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[c][e] = (st[c][0][e] + st[c][1][e]) * ((e & 1) ? f1 : f0);
       if (masked) {
-        const int lim = ks < 0.f ? -1 : k_end - 1 - key0;
-        if (key_of<HD>(g) > lim) x[c][0] = x[c][1] = -CUDART_INF_F;
-        if (8 + key_of<HD>(g) > lim) x[c][2] = x[c][3] = -CUDART_INF_F;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // the last key of the tile that the column's token sees
+          const int lim = ks < 0.f ? -1 : (RUNS ? min(pos0 + token_of(c * 8 + 2 * t4 + h), k_end - 1) : k_end - 1) - key0;
+          if (key_of<HD>(g) > lim) x[c][h] = -CUDART_INF_F;
+          if (8 + key_of<HD>(g) > lim) x[c][2 + h] = -CUDART_INF_F;
+        }
       }
       // the reference follows the maximum only when that has grown by more than P_SLACK (always at the first key)
       grow |= fmaxf(x[c][0], x[c][2]) > m_ref[c][0] + P_SLACK || fmaxf(x[c][1], x[c][3]) > m_ref[c][1] + P_SLACK;
@@ -391,9 +418,9 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
   for (int c = 0; c < NC; ++c) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int head = c * 8 + t4 * 2 + h;
-      if (head < group) {
-        float* dst_row = mrg + (warp * 16 + head) * RS;
+      const int col = c * 8 + t4 * 2 + h;
+      if (col < n_cols) {
+        float* dst_row = mrg + (warp * 16 + col) * RS;
 #pragma unroll
         for (int n = 0; n < MT; ++n) {
           dst_row[g * (HD / 8) + 2 * n] = o_acc[c][n][h] * (unit * P_UNIT);
@@ -404,7 +431,7 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
     }
   }
   __syncthreads();
-  for (int idx = tid; idx < group * HD; idx += PA_THREADS) {
+  for (int idx = tid; idx < n_cols * HD; idx += PA_THREADS) {
     const int r = idx / HD, d = idx - r * HD;
     float m = -CUDART_INF_F;
 #pragma unroll
@@ -418,48 +445,42 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
       l += src[HD + 1] * f;
       o += src[d] * f;
     }
+    const size_t row = out_row(r);
     if (a.n_splits == 1) {
-      // no visible entry: zeros
-      a.o[static_cast<size_t>(b) * (a.n_q_heads * HD) + (kvh * group + r) * HD + d] = __float2bfloat16(l == 0.f ? 0.f : o / l);
+      a.o[row * HD + d] = __float2bfloat16(l == 0.f ? 0.f : o / l);  // (no visible entry: zeros)
     } else {
-      const size_t row = ((static_cast<size_t>(b) * a.n_kv_heads + kvh) * a.n_splits + split) * group + r;
-      a.partial[row * HD + d] = o;
-      if (d == 0)
-        reinterpret_cast<float2*>(a.partial + static_cast<size_t>(a.batch) * a.n_q_heads * a.n_splits * HD)[row] = make_float2(m, l);
+      a.parts.o[(part_row0 + row) * HD + d] = o;
+      if (d == 0) a.parts.ml[part_row0 + row] = make_float2(m, l);
     }
   }
 }
 
-// Merge of the splits: one block per (query head, sequence).  Every warp computes the weights of all splits (a split per
-// lane), the warps share the splits' rows and add up in shared memory.  All loads of up to 32 splits are issued before
-// the first is used; rows of splits that hold no keys are loaded, too, and left out.
+// Joins the parts of a row: one block per (token, query head).  Every warp computes the weights of all parts (a part per lane),
+// the warps share the parts' outputs and add up in shared memory.  All loads of up to 32 parts are issued before the first
+// is used; outputs of parts without keys are loaded, too, and left out.
 constexpr int PC_WARPS = 4;
 
 template <int HD>
-__global__ void __launch_bounds__(PC_WARPS * 32) paged_combine_kernel(const PagedDecodeArgs a) {
-  constexpr int V = HD / 32, NR = 32 / PC_WARPS;  // features per lane, rows per warp and round
-  const int b = blockIdx.y, hq = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = a.n_q_heads / a.n_kv_heads;
-  const int kvh = hq / group, r = hq - kvh * group;
+__global__ void __launch_bounds__(PC_WARPS * 32) paged_join_kernel(const PagedParts p, bf16* o, long long rows, int n_splits) {
+  constexpr int V = HD / 32, NR = 32 / PC_WARPS;  // features per lane, parts per warp and round
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const size_t row = blockIdx.x;
   __shared__ float acc[PC_WARPS][HD];
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const size_t row0 = (static_cast<size_t>(b) * a.n_kv_heads + kvh) * a.n_splits * group + r;
-  const float2* ml = reinterpret_cast<const float2*>(a.partial + static_cast<size_t>(a.batch) * a.n_q_heads * a.n_splits * HD);
   float m_run = -CUDART_INF_F, l = 0.f, o_sum[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) o_sum[e] = 0.f;
-  const int total = visible_keys(a, b);
-  for (int s0 = 0; s0 < a.n_splits; s0 += 32) {
-    float2 st = s0 + lane < a.n_splits ? ml[row0 + static_cast<size_t>(s0 + lane) * group] : make_float2(0.f, 0.f);
+  for (int s0 = 0; s0 < n_splits; s0 += 32) {
+    const float2 st = s0 + lane < n_splits ? p.ml[static_cast<size_t>(s0 + lane) * rows + row] : make_float2(-CUDART_INF_F, 0.f);
     float v[NR][V];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const int s = s0 + i * PC_WARPS + warp;
 #pragma unroll
       for (int e = 0; e < V; ++e) v[i][e] = 0.f;
-      if (s < a.n_splits) {
-        const float* src = a.partial + (row0 + static_cast<size_t>(s) * group) * HD + lane * V;
+      if (s < n_splits) {
+        const float* src = p.o + (static_cast<size_t>(s) * rows + row) * HD + lane * V;
         if (V == 4) {
           const float4 w = *reinterpret_cast<const float4*>(src);
           v[i][0] = w.x; v[i][1] = w.y; v[i][V - 2] = w.z; v[i][V - 1] = w.w;
@@ -469,132 +490,118 @@ __global__ void __launch_bounds__(PC_WARPS * 32) paged_combine_kernel(const Page
         }
       }
     }
-    const bool held = 1ll * (s0 + lane) * a.chunk < total;  // the split holds keys (so its row was written)
-    if (!held) st = make_float2(-CUDART_INF_F, 0.f);
+    const bool held = st.x != -CUDART_INF_F || st.y != 0.f;  // the part saw keys (so its outputs are there)
     float m = fmaxf(m_run, st.x);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int k = 16; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
     const float m_use = m == -CUDART_INF_F ? 0.f : m;
     const float corr = exp2f(m_run - m_use), f_lane = exp2f(st.x - m_use);
     m_run = m;
     l = l * corr + st.y * f_lane;
 #pragma unroll
     for (int e = 0; e < V; ++e) o_sum[e] *= corr;
+    const uint32_t held_mask = __ballot_sync(0xffffffffu, held);
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const int s = i * PC_WARPS + warp;
       const float f = __shfl_sync(0xffffffffu, f_lane, s);
-      if (1ll * (s0 + s) * a.chunk < total) {
+      if ((held_mask >> s) & 1u) {
 #pragma unroll
         for (int e = 0; e < V; ++e) o_sum[e] = fmaf(v[i][e], f, o_sum[e]);
       }
     }
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  for (int k = 16; k > 0; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
 #pragma unroll
   for (int e = 0; e < V; ++e) acc[warp][lane * V + e] = o_sum[e];
   __syncthreads();
   if (threadIdx.x < HD) {
-    const float o = (acc[0][threadIdx.x] + acc[1][threadIdx.x]) + (acc[2][threadIdx.x] + acc[3][threadIdx.x]);
-    // no visible entry: zeros
-    a.o[static_cast<size_t>(b) * (a.n_q_heads * HD) + hq * HD + threadIdx.x] = __float2bfloat16(l == 0.f ? 0.f : o / l);
+    const float sum = (acc[0][threadIdx.x] + acc[1][threadIdx.x]) + (acc[2][threadIdx.x] + acc[3][threadIdx.x]);
+    o[row * HD + threadIdx.x] = __float2bfloat16(l == 0.f ? 0.f : sum / l);  // (no visible entry: zeros)
   }
 }
 
-template <int HD, bool WIDE>
-pd_status launch_decode(const PagedDecodeArgs& a, cudaStream_t s) {
+template <int HD, bool WIDE, bool RUNS>
+pd_status launch_rows(const PagedDecodeArgs& a, int slots, cudaStream_t s) {
   using SM = PagedSmem<HD>;
   static PerDeviceInt smem_opt_in;
-  PD_TRY(opt_in_smem(smem_opt_in, paged_decode_kernel<HD, WIDE>, SM::BYTES));
-  PD_CUDA_TRY(launch_pdl(paged_decode_kernel<HD, WIDE>, dim3(a.n_splits, a.n_kv_heads, a.batch), dim3(PA_THREADS), SM::BYTES, s, a));
+  PD_TRY(opt_in_smem(smem_opt_in, paged_decode_kernel<HD, WIDE, RUNS>, SM::BYTES));
+  PD_CUDA_TRY(launch_pdl(paged_decode_kernel<HD, WIDE, RUNS>, dim3(a.n_splits, a.n_kv_heads, slots), dim3(PA_THREADS), SM::BYTES, s, a));
   count_launch();
-  if (a.n_splits > 1) {
-    PD_CUDA_TRY(launch_pdl(paged_combine_kernel<HD>, dim3(a.n_q_heads, a.batch), dim3(PC_WARPS * 32), 0, s, a));
-    count_launch();
-  }
+  if (a.n_splits > 1) return launch_paged_join(a.parts, a.o, 1ll * a.rows * a.n_q_heads, a.n_splits, HD, s);
   return PD_OK;
 }
+template <int HD, bool WIDE>
+pd_status launch_rows(const PagedDecodeArgs& a, int slots, cudaStream_t s) {
+  return a.cu_seqlens ? launch_rows<HD, WIDE, true>(a, slots, s) : launch_rows<HD, WIDE, false>(a, slots, s);
+}
+bool rows_wide(const PagedDecodeArgs& a) { return a.block_tokens * (a.n_q_heads / a.n_kv_heads) > 8; }
+pd_status launch_rows_any(const PagedDecodeArgs& a, int head_dim, int slots, cudaStream_t s) {
+  if (head_dim == 128) return rows_wide(a) ? launch_rows<128, true>(a, slots, s) : launch_rows<128, false>(a, slots, s);
+  return rows_wide(a) ? launch_rows<64, true>(a, slots, s) : launch_rows<64, false>(a, slots, s);
+}
 
-// How a segment (sequence, KV head) is cut.  Two blocks of eight warps are resident per SM.  A single sequence is cut into
-// as many equal runs as are resident together (32768 keys, 8 KV heads: 20.3 us at 37 runs a head, 24.4 us at 55).  The
-// sequences of a batch may differ in length, which the host does not know: half as many runs again even that out (24
-// sequences of 100 to 4351 keys: 31.2 us, 37.4 us at one run per resident block).  From as many segments as there are
-// resident blocks nothing is cut: the merge costs more than the last, partly filled wave.
+// Key ranges are cut into equal parts while there are fewer blocks than run together, into parts of at least PA_MIN_CHUNK keys
+// and at most `longest` keys.
 struct Split { int n, chunk; };
-Split paged_decode_split(int batch, int n_kv_heads, int max_kv_len) {
-  const long long blocks = 1ll * batch * n_kv_heads;
+Split rows_split(long long blocks, long long parts, int max_kv_len, int longest) {
   if (blocks <= 0 || max_kv_len <= 0) return {1, PA_MIN_CHUNK};
-  long long want = (batch == 1 ? 296 : 444) / blocks;
+  long long want = parts / blocks;
   if (want < 1) want = 1;
   long long chunk = (max_kv_len + want - 1) / want;
+  if (chunk > longest) chunk = longest;
   if (chunk < PA_MIN_CHUNK) chunk = PA_MIN_CHUNK;
   chunk = (chunk + 63) / 64 * 64;
   return {static_cast<int>((max_kv_len + chunk - 1) / chunk), static_cast<int>(chunk)};
 }
-
-// ------------------------------------------------------------------------------------ pages -> contiguous bf16
-struct GatherArgs {
-  bf16* k;                    // [n_req, Hkv, len_cap, hd]
-  bf16* v;
-  const int32_t* cu_seqlens;  // [n_req + 1]
-  const int32_t* prefix;      // [n_req] or NULL
-  int* err_word;
-  PagedCache c;
-  int n_kv_heads, head_dim, len_cap;
-};
-
-__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t pair, float s) {
-  const uint32_t h = e4m3x2_to_f16x2(static_cast<uint16_t>(pair));
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-  return ptx::pack_bf16(f.x * s, f.y * s);  // exact: four significant bits times a power of two
-}
-
-// Block (page of the sequence, KV head, request): its K and V rows that hold tokens.
-__global__ void __launch_bounds__(256) gather_pages_kernel(const GatherArgs a) {
-  const int pi = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z;
-  ptx::grid_launch_dependents();
-  ptx::grid_dependency_wait();
-  const int n_new = a.cu_seqlens[r + 1] - a.cu_seqlens[r];
-  if (n_new <= 0) return;
-  const int total = min((a.prefix ? a.prefix[r] : 0) + n_new, a.len_cap);
-  const int first = pi << a.c.log2_page;
-  const int rows = min(total - first, 1 << a.c.log2_page);
-  if (rows <= 0) return;
-  const int id = a.c.table[static_cast<size_t>(r) * a.c.table_ld + pi];
-  const bool ok = static_cast<unsigned>(id) < static_cast<unsigned>(a.c.n_pages);
-  if (!ok && threadIdx.x == 0 && a.err_word) atomicExch(a.err_word, 2);
-  const size_t ph = static_cast<size_t>(ok ? id : 0) * a.n_kv_heads + kvh;
-  const uint4* src_k = reinterpret_cast<const uint4*>(a.c.k + (ph << a.c.log2_page) * a.head_dim);
-  const uint4* src_v = reinterpret_cast<const uint4*>(a.c.v + (ph << a.c.log2_page) * a.head_dim);
-  const float ks = ok ? a.c.k_scale[ph] : 0.f, vs = ok ? a.c.v_scale[ph] : 0.f;
-  const size_t dst0 = ((static_cast<size_t>(r) * a.n_kv_heads + kvh) * a.len_cap + first) * a.head_dim;
-  uint4* dst_k = reinterpret_cast<uint4*>(a.k + dst0);
-  uint4* dst_v = reinterpret_cast<uint4*>(a.v + dst0);
-  const int chunks = rows * a.head_dim / 16;
-  for (int i = threadIdx.x; i < chunks; i += blockDim.x) {
-    uint4 wk = make_uint4(0u, 0u, 0u, 0u), wv = wk;
-    if (ok) { wk = src_k[i]; wv = src_v[i]; }
-    dst_k[2 * i] = make_uint4(codes_to_bf16(wk.x, ks), codes_to_bf16(wk.x >> 16, ks), codes_to_bf16(wk.y, ks), codes_to_bf16(wk.y >> 16, ks));
-    dst_k[2 * i + 1] = make_uint4(codes_to_bf16(wk.z, ks), codes_to_bf16(wk.z >> 16, ks), codes_to_bf16(wk.w, ks), codes_to_bf16(wk.w >> 16, ks));
-    dst_v[2 * i] = make_uint4(codes_to_bf16(wv.x, vs), codes_to_bf16(wv.x >> 16, vs), codes_to_bf16(wv.y, vs), codes_to_bf16(wv.y >> 16, vs));
-    dst_v[2 * i + 1] = make_uint4(codes_to_bf16(wv.z, vs), codes_to_bf16(wv.z >> 16, vs), codes_to_bf16(wv.w, vs), codes_to_bf16(wv.w >> 16, vs));
-  }
-}
-
-size_t prefill_scratch_half(const pd_layer_cfg* cfg, int n_req, int max_kv_len) {
-  return align_up(static_cast<size_t>(n_req) * cfg->n_kv_heads * max_kv_len * cfg->head_dim * sizeof(bf16), 256);
+// Decode.  The sequences of a batch may differ in length, which the host does not know, so a part is at most 4096 keys (30
+// sequences of up to 32000 keys: 175 us, 250 us uncut), and from about one block per SM on half as many parts again as run
+// together even the lengths out (24 sequences of 100 to 4351 keys, 192 blocks: 31 us, 37 us at one part per resident block; 4
+// sequences of 8000 keys, 32 blocks: 21 us, 18 us).  More parts cost more in the join than they bring.
+Split decode_split(int batch, int n_kv_heads, int max_kv_len) {
+  const long long blocks = 1ll * batch * n_kv_heads;
+  return rows_split(blocks, blocks <= 148 ? PA_RESIDENT : PA_RESIDENT * 3 / 2, max_kv_len, batch > 1 ? 4096 : max_kv_len);
 }
 
 }  // namespace
+
+pd_status launch_paged_join(const PagedParts& parts, bf16* o, long long rows, int n_splits, int head_dim, cudaStream_t s) {
+  if (rows > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
+  const dim3 grid(static_cast<unsigned>(rows)), block(PC_WARPS * 32);
+  PD_CUDA_TRY(head_dim == 128 ? launch_pdl(paged_join_kernel<128>, grid, block, 0, s, parts, o, rows, n_splits)
+                              : launch_pdl(paged_join_kernel<64>, grid, block, 0, s, parts, o, rows, n_splits));
+  count_launch();
+  return PD_OK;
+}
+
+int paged_rows_block(int group, int longest_run) {
+  // eight columns where the runs fit them (half the registers), else sixteen
+  return (group * longest_run <= 8 ? 8 : 16) / group;
+}
+
+size_t paged_rows_part_rows() { return PA_RESIDENT * 16; }
+
+pd_status launch_paged_rows(const PagedRuns& r, int longest_run, const PagedParts& parts, cudaStream_t s) {
+  PagedDecodeArgs a{};
+  a.q = r.q; a.o = r.o; a.cu_seqlens = r.cu_seqlens; a.kv_len = r.prefix; a.parts = parts; a.err_word = r.err_word; a.c = r.c;
+  a.ldq = r.ldq; a.rows = r.n_tokens; a.n_req = r.n_req; a.n_q_heads = r.n_q_heads; a.n_kv_heads = r.n_kv_heads;
+  a.block_tokens = paged_rows_block(r.n_q_heads / r.n_kv_heads, longest_run);
+  const int slots = first_slot(r.n_tokens, r.n_req, a.block_tokens);
+  if (slots > 65535) return PD_ERR_UNSUPPORTED_SHAPE;
+  const Split sp = rows_split(1ll * slots * r.n_kv_heads, rows_wide(a) ? PA_RESIDENT / 2 : PA_RESIDENT, r.max_kv, r.max_kv);
+  a.n_splits = sp.n; a.chunk = sp.chunk;
+  return launch_rows_any(a, r.head_dim, slots, s);
+}
+
 }  // namespace pd
 
 extern "C" pd_status pd_paged_decode_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t B, int32_t max_kv_len,
                                                                size_t* out_bytes) {
   PD_TRY(pd::check_paged_heads(cfg));
   if (!out_bytes || B < 0 || max_kv_len < 0) return PD_ERR_INVALID_ARG;
-  const int splits = pd::paged_decode_split(B, cfg->n_kv_heads, max_kv_len).n;
-  *out_bytes = splits > 1 ? pd::align_up(static_cast<size_t>(B) * cfg->n_q_heads * splits * (cfg->head_dim + 2) * 4, 256) : 0;
+  const int splits = pd::decode_split(B, cfg->n_kv_heads, max_kv_len).n;
+  *out_bytes = splits > 1 ? pd::paged_parts_bytes(static_cast<size_t>(splits) * B * cfg->n_q_heads, cfg->head_dim) : 0;
   return PD_OK;
 }
 
@@ -612,77 +619,18 @@ extern "C" pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const vo
   if (!q || !out || !kv_len_dev || ldq < cfg->n_q_heads * cfg->head_dim || ldq % 8 != 0) return PD_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(q) & 15u) || (reinterpret_cast<uintptr_t>(out) & 1u)) return PD_ERR_INVALID_ARG;
   if (max_kv_len <= 0 || max_kv_len > (cache->table_ld << a.c.log2_page)) return PD_ERR_INVALID_ARG;
-  const Split sp = paged_decode_split(B, cfg->n_kv_heads, max_kv_len);
+  const Split sp = decode_split(B, cfg->n_kv_heads, max_kv_len);
   a.n_splits = sp.n; a.chunk = sp.chunk;
   if (a.n_splits > 1) {
-    size_t need = 0;
-    PD_TRY(pd_paged_decode_attention_workspace_bytes(cfg, B, max_kv_len, &need));
+    const size_t part_rows = static_cast<size_t>(a.n_splits) * B * cfg->n_q_heads;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PD_ERR_INVALID_ARG;
-    if (workspace_bytes < need) return PD_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < paged_parts_bytes(part_rows, cfg->head_dim)) return PD_ERR_WORKSPACE_TOO_SMALL;
+    a.parts.o = static_cast<float*>(workspace);
+    a.parts.ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + paged_parts_ml_offset(part_rows, cfg->head_dim));
   }
-  a.q = static_cast<const bf16*>(q); a.o = static_cast<bf16*>(out); a.kv_len = kv_len_dev;
-  a.partial = static_cast<float*>(workspace); a.err_word = err_word;
-  a.ldq = ldq; a.batch = B; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
+  a.q = static_cast<const bf16*>(q); a.o = static_cast<bf16*>(out); a.kv_len = kv_len_dev; a.err_word = err_word;
+  a.ldq = ldq; a.rows = B; a.n_req = B; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads; a.block_tokens = 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_ATTN_DECODE, st);
-  const bool wide = cfg->n_q_heads / cfg->n_kv_heads > 8;
-  if (cfg->head_dim == 128) return wide ? launch_decode<128, true>(a, st) : launch_decode<128, false>(a, st);
-  return wide ? launch_decode<64, true>(a, st) : launch_decode<64, false>(a, st);
-}
-
-extern "C" pd_status pd_paged_prefill_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t n_req, int32_t max_kv_len,
-                                                                size_t* out_bytes) {
-  PD_TRY(pd::check_paged_heads(cfg));
-  if (!out_bytes || n_req < 0 || max_kv_len < 0) return PD_ERR_INVALID_ARG;
-  *out_bytes = 2 * pd::prefill_scratch_half(cfg, n_req, max_kv_len);
-  return PD_OK;
-}
-
-extern "C" pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const void* q, int32_t ldq, void* out,
-                                                const int32_t* cu_dev, const int32_t* cu_host, int32_t n_req,
-                                                const int32_t* prefix_dev, const int32_t* prefix_host,
-                                                const pd_paged_kv_cache* cache, void* workspace, size_t workspace_bytes,
-                                                int32_t* err_word, void* stream) {
-  using namespace pd;
-  PD_TRY(check_paged_heads(cfg));
-  GatherArgs ga{};
-  PD_TRY(paged_cache_view(cache, &ga.c));
-  if (!cu_host || n_req < 0 || n_req > 4095 || n_req > cache->n_seqs || (prefix_dev == nullptr) != (prefix_host == nullptr))
-    return PD_ERR_INVALID_ARG;
-  if (cu_host[0] != 0) return PD_ERR_INVALID_ARG;
-  const int cap = cache->table_ld << ga.c.log2_page;
-  int max_len = 0, max_kv = 0;
-  for (int r = 0; r < n_req; ++r) {
-    const long long len = 1ll * cu_host[r + 1] - cu_host[r];
-    const int pre = prefix_host ? prefix_host[r] : 0;
-    if (len < 0 || pre < 0 || pre + len > cap) return PD_ERR_INVALID_ARG;
-    if (len > max_len) max_len = static_cast<int>(len);
-    if (len > 0 && pre + len > max_kv) max_kv = static_cast<int>(pre + len);
-  }
-  const int tokens = cu_host[n_req];
-  if (tokens == 0) return PD_OK;
-  if (!q || !out || !cu_dev || ldq < cfg->n_q_heads * cfg->head_dim || ldq % 8 != 0) return PD_ERR_INVALID_ARG;
-  if ((reinterpret_cast<uintptr_t>(q) & 15u) || (reinterpret_cast<uintptr_t>(out) & 31u)) return PD_ERR_INVALID_ARG;
-  const size_t half = prefill_scratch_half(cfg, n_req, max_kv);
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PD_ERR_INVALID_ARG;
-  if (workspace_bytes < 2 * half) return PD_ERR_WORKSPACE_TOO_SMALL;
-  // cache rows are addressed with 32-bit row numbers
-  if (1ll * n_req * cfg->n_kv_heads * max_kv > 0x7fffffffll - 256) return PD_ERR_UNSUPPORTED_SHAPE;
-  ga.k = static_cast<bf16*>(workspace);
-  ga.v = reinterpret_cast<bf16*>(static_cast<uint8_t*>(workspace) + half);
-  ga.cu_seqlens = cu_dev; ga.prefix = prefix_dev; ga.err_word = err_word;
-  ga.n_kv_heads = cfg->n_kv_heads; ga.head_dim = cfg->head_dim; ga.len_cap = max_kv;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  TraceScope ts(PD_K_ATTN_PREFILL, st);
-  const int pages = (max_kv + (1 << ga.c.log2_page) - 1) >> ga.c.log2_page;
-  PD_CUDA_TRY(launch_pdl(gather_pages_kernel, dim3(pages, cfg->n_kv_heads, n_req), dim3(256), 0, st, ga));
-  count_launch();
-  PrefillAttnArgs a{};
-  a.q = static_cast<const bf16*>(q); a.ldq = ldq;
-  a.k_cache = ga.k; a.v_cache = ga.v;
-  a.o = static_cast<bf16*>(out); a.cu_seqlens = cu_dev; a.prefix = prefix_dev;
-  a.n_req = n_req; a.n_tokens = tokens; a.max_len = max_len;
-  a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads; a.head_dim = cfg->head_dim;
-  a.len_cap = max_kv; a.batch_cap = n_req;
-  return launch_prefill_attention_tc(a, err_word, st);
+  return launch_rows_any(a, cfg->head_dim, B, st);
 }

@@ -93,6 +93,30 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
   }
 }
 
+// ------------------------------------------------------- taking over blocks of the grid
+// Asks for a block of this grid that has not been started: the 16-byte answer goes to `answer` (shared memory, 16-byte
+// aligned) and completes 16 bytes on the mbarrier.  A taken-over block is never started by the hardware.
+__device__ __forceinline__ void clc_try_cancel(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+               ::"r"(answer), "r"(bar) : "memory");
+}
+// Whether a block was taken over, and its blockIdx.x.  After a "no" there must be no further request.
+__device__ __forceinline__ bool clc_answer(uint32_t answer, int& block_x) {
+  uint32_t yes, x;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+      "ld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+      : "=r"(yes), "=r"(x)
+      : "r"(answer)
+      : "memory");
+  block_x = static_cast<int>(x);
+  return yes != 0;
+}
+
 // ------------------------------------------------- programmatic dependent launch
 // A kernel launched with the programmatic-serialization attribute may start while the previous
 // kernel of its stream is still running.  grid_dependency_wait blocks until every grid this one
@@ -110,6 +134,12 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, int3
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
       : "memory");
 }
 
@@ -235,6 +265,16 @@ __device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t smem_addr) {
   d |= static_cast<uint64_t>(1024 >> 4) << 32;                // stride byte offset
   d |= static_cast<uint64_t>(1) << 46;                        // descriptor version for sm_100
   d |= static_cast<uint64_t>(2) << 61;                        // layout: 128-byte swizzle
+  return d;
+}
+// The same for rows of 64 bytes with the 64-byte swizzle: 8-row groups are 512 bytes apart.
+__device__ __forceinline__ uint64_t umma_desc_sw64(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(1) << 16;
+  d |= static_cast<uint64_t>(512 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(4) << 61;                        // layout: 64-byte swizzle
   return d;
 }
 // Instruction descriptor: bf16 A and B, both K-major, fp32 accumulator, M x N tile.

@@ -96,8 +96,9 @@ def test_decode_attention_arguments(pdlib):
 
 def test_prefill_attention_arguments(pdlib):
     c, k = cfg(pdlib), cache(pdlib)
-    need = pdlib.pd_paged_prefill_attention_workspace_bytes(c, 2, 20)
-    ok = dict(cfg=c, q=PTR, ldq=512, out=PTR, cu_seqlens_dev=PTR, cu_seqlens_host=[0, 10, 15], prefix_dev=PTR, prefix_host=[10, 3],
+    need = pdlib.pd_paged_prefill_attention_workspace_bytes(c, 2, 210)
+    assert need > 0 and pdlib.pd_paged_prefill_attention_workspace_bytes(c, 0, 128) == 0
+    ok = dict(cfg=c, q=PTR, ldq=512, out=PTR, cu_seqlens_dev=PTR, cu_seqlens_host=[0, 10, 15], prefix_dev=PTR, prefix_host=[200, 3],
               cache=k, workspace=PTR, workspace_bytes=need)
     call = lambda stream, a: pdlib.pd_paged_prefill_attention(stream=stream, **a)  # noqa: E731
     for bad in [dict(q=None), dict(out=None), dict(cu_seqlens_dev=None), dict(ldq=504), dict(ldq=516), dict(q=PTR + 8), dict(out=PTR + 16),
