@@ -423,7 +423,7 @@ pd_status pd_rope_table(const pd_layer_cfg* cfg, float* table_host);
 /* Rotates fresh q and k heads to their positions and appends k and v to the cache.
  *   qkv          device bf16 [T, ldqkv]: q heads, k heads, v heads of a row as the QKV projection leaves them (before the
  *                rotation); ldqkv a multiple of 8
- *   q_out        rotated q, device bf16 [T, Hq*hd] contiguous; NULL: only the cache is written
+ *   q_out        rotated q, device bf16 [T, Hq*hd] contiguous, not overlapping qkv; NULL: only the cache is written
  *   rope_tab     device fp32 [max_pos, hd / 2, 2] (pd_rope_table)
  *   cu_seqlens   as for pd_prefill_layer (device and host copy); both NULL: one row per request (a decode step)
  *   kv_len_dev   device int32[n_req]: tokens that sequence r holds already; its rows take positions kv_len[r],

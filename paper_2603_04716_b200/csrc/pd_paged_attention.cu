@@ -16,6 +16,8 @@
 // and O are fp32; K's scale is applied to the scores, V's to the weights, relative to the largest V scale so far.
 #include <math_constants.h>
 
+#include <algorithm>
+
 #include "pd_paged.cuh"
 
 namespace pd {
@@ -558,10 +560,12 @@ Split rows_split(long long blocks, long long parts, int max_kv_len, int longest)
 // Decode.  The sequences of a batch may differ in length, which the host does not know, so a part is at most 4096 keys (30
 // sequences of up to 32000 keys: 175 us, 250 us uncut), and from about one block per SM on half as many parts again as run
 // together even the lengths out (24 sequences of 100 to 4351 keys, 192 blocks: 31 us, 37 us at one part per resident block; 4
-// sequences of 8000 keys, 32 blocks: 21 us, 18 us).  More parts cost more in the join than they bring.
+// sequences of 8000 keys, 32 blocks: 21 us, 18 us).  More parts cost more in the join than they bring; no more than 16 are
+// made for the length alone, since max_kv_len may be a capacity far above the lengths.
 Split decode_split(int batch, int n_kv_heads, int max_kv_len) {
   const long long blocks = 1ll * batch * n_kv_heads;
-  return rows_split(blocks, blocks <= 148 ? PA_RESIDENT : PA_RESIDENT * 3 / 2, max_kv_len, batch > 1 ? 4096 : max_kv_len);
+  return rows_split(blocks, blocks <= 148 ? PA_RESIDENT : PA_RESIDENT * 3 / 2, max_kv_len,
+                    batch > 1 ? std::max(4096, max_kv_len / 16) : max_kv_len);
 }
 
 }  // namespace
