@@ -33,7 +33,8 @@ namespace {
 
 constexpr int TQ = 128;                    // rows per row tile
 constexpr int TK = 128;                    // keys per key tile
-constexpr int THREADS = 384;
+constexpr int TH = TK / 2;                 // half a key tile: scores, weights and products advance by it
+constexpr int THREADS = 416;
 constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr float RESCALE_THRESHOLD = 8.f;   // log2 units
 constexpr float P_SHIFT = 7.f;             // p is kept as 2^7 p: at most 2^15, below f16's 65504
@@ -61,8 +62,8 @@ struct Cfg {
 
 // barrier indices
 constexpr int B_QFULL = 0, B_QEMPTY = 2, B_KFULL = 4, B_KEMPTY = B_KFULL + K_SLOTS, B_VFULL = B_KEMPTY + K_SLOTS,
-              B_VEMPTY = B_VFULL + V_SLOTS, B_SFULL = B_VEMPTY + V_SLOTS, B_PREADY = B_SFULL + 2, B_ODONE = B_PREADY + 2,
-              B_OREAD = B_ODONE + 2, B_IFULL = B_OREAD + 2, B_IEMPTY = B_IFULL + ITEM_SLOTS, B_CLC = B_IEMPTY + ITEM_SLOTS,
+              B_VEMPTY = B_VFULL + V_SLOTS, B_SFULL = B_VEMPTY + V_SLOTS, B_PREADY = B_SFULL + 4, B_ODONE = B_PREADY + 4,
+              B_OREAD = B_ODONE + 4, B_IFULL = B_OREAD + 2, B_IEMPTY = B_IFULL + ITEM_SLOTS, B_CLC = B_IEMPTY + ITEM_SLOTS,
               B_QRAW = B_CLC + 1, B_RFULL = B_QRAW + 2, B_REMPTY = B_RFULL + R_SLOTS, N_BARS = B_REMPTY + R_SLOTS;
 
 struct PagedPrefillDev {
@@ -82,7 +83,9 @@ struct PagedPrefillDev {
 
 // A work item as warp 0 publishes it.
 struct Item {
-  int kvh, start, len, t0, pre, req, jb, n_kv0, n_kv1, split;  // n_kv0 = -1: no more items
+  int kvh, start, len, t0, pre, req, jb, split;
+  int n_kv;       // key tiles; -1: no more items
+  int halves[2];  // half key tiles that a row tile works on
 };
 // Per 16 keys of a tile: factor of the scores and exponent of V's page scale relative to the unit of V (<= 0; kNoRows: no
 // such page); the unit.
@@ -150,13 +153,14 @@ __device__ __forceinline__ bool decode_item(const PagedPrefillDev& p, int idx, I
   it.split = rest / p.n_kv_heads;
   it.req = b.req; it.start = b.start; it.len = b.len; it.pre = b.pre; it.t0 = b.t0;
   if (it.t0 >= it.len) return false;
-  const int n0 = (it.pre + min(it.len, it.t0 + p.tile_tokens) + TK - 1) / TK;
-  const int n1 = it.t0 + p.tile_tokens < it.len ? (it.pre + min(it.len, it.t0 + tb) + TK - 1) / TK : 0;
-  const int n_all = max(n0, n1);
+  const int h0 = (it.pre + min(it.len, it.t0 + p.tile_tokens) + TH - 1) / TH;
+  const int h1 = it.t0 + p.tile_tokens < it.len ? (it.pre + min(it.len, it.t0 + tb) + TH - 1) / TH : 0;
+  const int n_all = (max(h0, h1) + 1) / 2;
   it.jb = static_cast<int>(1ll * n_all * it.split / p.n_splits);
   const int je = static_cast<int>(1ll * n_all * (it.split + 1) / p.n_splits);
-  it.n_kv0 = max(0, min(n0, je) - it.jb);
-  it.n_kv1 = max(0, min(n1, je) - it.jb);
+  it.n_kv = je - it.jb;
+  it.halves[0] = max(0, min(h0, 2 * je) - 2 * it.jb);
+  it.halves[1] = max(0, min(h1, 2 * je) - 2 * it.jb);
   return true;
 }
 
@@ -274,7 +278,7 @@ __device__ __noinline__ void producer(const CUtensorMap* tmap_q, const CUtensorM
   };
   next_item();
   while (ok) {
-    if (!have) { it.n_kv0 = -1; it.n_kv1 = 0; }
+    if (!have) it.n_kv = -1;
     {
       const int s = published & (ITEM_SLOTS - 1);
       if (!wait(B_IEMPTY + s, ((published / ITEM_SLOTS) & 1) ^ 1u)) break;
@@ -286,7 +290,7 @@ __device__ __noinline__ void producer(const CUtensorMap* tmap_q, const CUtensorM
       ++published;
     }
     if (!have) break;
-    const int n = max(it.n_kv0, it.n_kv1), n_kv[2] = {it.n_kv0, it.n_kv1};
+    const int n = it.n_kv;
     const int total = it.pre + it.len;  // keys that the request holds
     const int32_t* table = p.c.table + static_cast<size_t>(it.req) * p.c.table_ld;
     const int kvh = it.kvh, jb = it.jb, q_token = it.start + it.t0;
@@ -337,7 +341,7 @@ __device__ __noinline__ void producer(const CUtensorMap* tmap_q, const CUtensorM
       ++g;
     };
     auto start_q = [&](int t) {
-      if (n_kv[t] == 0) return;
+      if ((t == 0 ? it.halves[0] : it.halves[1]) == 0) return;
       // the tile's Q buffer is free once the last Q K^T of its previous item has been executed
       if (!wait(B_QEMPTY + t, (act[t] & 1) ^ 1u)) return;
       if (lane == 0) {
@@ -382,116 +386,86 @@ __device__ __noinline__ void producer(const CUtensorMap* tmap_q, const CUtensorM
   }
 }
 
-// -------------------------------------------------------------------------------------------- warp 1: MMA issuer
+// ------------------------------------------------------------------------- warps 1, 12: MMA issuers, one per row tile
+// S of half a key tile, and P V of it, at a time: the half of S that a product has consumed is written again at once, while
+// the softmax works on the other half.
 template <int HD>
-__device__ __noinline__ void mma_issuer(const uint32_t smem_base, const uint32_t tmem_base, Shared* sh, const uint64_t limit) {
+__device__ __noinline__ void mma_issuer(const int t, const uint32_t smem_base, const uint32_t tmem_base, Shared* sh, const uint64_t limit) {
   using C = Cfg<HD>;
   const uint32_t bar0 = ptx::smem_u32(sh->bars);
   auto bar = [&](int i) { return bar0 + 8u * i; };
   volatile int* abort_flag = &sh->abort_flag;
-  constexpr uint32_t idesc_qk = ptx::umma_idesc_e4m3(TQ, TK);
+  constexpr uint32_t idesc_qk = ptx::umma_idesc_e4m3(TQ, TH);
   constexpr uint32_t idesc_pv = idesc_f16(TQ, HD) | (1u << 16);  // V: MN-major
-  // Per row tile: the item it is working on and how far it has got.  The two tiles walk the same item sequence and share
-  // the K / V rings, but each advances as soon as its own inputs are ready.
-  int kv0[2] = {0, 0}, kv1[2] = {0, 0};
-  bool have[2] = {false, false}, done[2] = {false, false};
-  int seq[2] = {0, 0};      // items taken from the ring so far
-  int base[2] = {0, 0};     // ring position of the current item's first K / V tile
-  int n[2] = {0, 0};        // key tiles of the current item for this row tile
-  int jq[2] = {0, 0};       // next Q K^T to issue
-  int jp[2] = {0, 0};       // next P V to issue
-  int act[2] = {0, 0};      // items with work for this row tile finished so far
-  int pv_cnt[2] = {0, 0};   // P V products issued so far (phase of p_ready)
-  uint32_t k_used = 0, v_used = 0;  // users that have consumed the tile in each ring slot, 4 bits per slot
-  uint64_t t_idle = 0;
-  uint32_t idle_polls = 0;
-  bool ok = true;
-  while (ok && !(done[0] && done[1])) {
-    bool progress = false;
+  const uint32_t s_col = tmem_base + t * C::TILE_COLS + C::S_COL, o_col = tmem_base + t * C::TILE_COLS + C::O_COL;
+  const uint32_t sq = smem_base + C::Q_OFF + t * C::Q_BYTES;
+  auto wait = [&](int b, uint32_t parity) { return ptx::mbar_wait_bounded(bar(b), parity, abort_flag, limit); };
+  int seq = 0;       // items taken from the ring so far
+  int base = 0;      // ring position of the current item's first K / V tile
+  int act = 0;       // items with work for this row tile finished so far
+  uint32_t p_ph = 0; // phases of the two p_ready barriers
+  while (true) {
+    const int s = seq & (ITEM_SLOTS - 1);
+    if (!wait(B_IFULL + s, (seq / ITEM_SLOTS) & 1)) return;
+    const int n_kv = sh->items[s].n_kv, nh = sh->items[s].halves[t];
+    ptx::mbar_arrive(bar(B_IEMPTY + s));
+    ++seq;
+    if (n_kv < 0) return;
+    // S of half i = Q K^T (it overwrites the P that aliased it, which a product issued before has consumed)
+    auto issue_s = [&](int i) {
+      const int h = i & 1, g = base + (i >> 1), slot = g % K_SLOTS;
+      if (h == 0 && !wait(B_KFULL + slot, (g / K_SLOTS) & 1)) return false;
+      ptx::tc_fence_after();
+      const uint32_t sk = smem_base + C::K_OFF + slot * C::CODE_BYTES + h * (TH * HD);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (done[t]) continue;
-      if (!have[t]) {
-        const int s = seq[t] & (ITEM_SLOTS - 1);
-        if (!ptx::mbar_test_wait(bar(B_IFULL + s), (seq[t] / ITEM_SLOTS) & 1)) continue;
-        kv0[t] = sh->items[s].n_kv0;
-        kv1[t] = sh->items[s].n_kv1;
-        ptx::mbar_arrive(bar(B_IEMPTY + s));
-        ++seq[t];
-        progress = true;
-        if (kv0[t] < 0) { done[t] = true; continue; }
-        n[t] = t == 0 ? kv0[t] : kv1[t];
-        if (n[t] == 0) {  // this item has rows or keys for the other tile only
-          base[t] += max(kv0[t], kv1[t]);
-          continue;
-        }
-        have[t] = true; jq[t] = 0; jp[t] = 0;
+      for (int part = 0; part < 2; ++part) {
+#pragma unroll
+        for (int kk = 0; kk < HD / 32; ++kk)
+          ptx::umma_f8(s_col + h * TH, code_desc<HD>(sq + part * C::CODE_BYTES + kk * 32), code_desc<HD>(sk + kk * 32), idesc_qk,
+                       (part > 0 || kk > 0) ? 1u : 0u);
       }
-      if (jp[t] < jq[t]) {
-        // ---- O_t += P_t V_j
-        const int j = jp[t], g = base[t] + j, s = g % V_SLOTS;
-        if (!ptx::mbar_test_wait(bar(B_PREADY + t), pv_cnt[t] & 1)) continue;
-        if (!ptx::mbar_test_wait(bar(B_VFULL + s), (g / V_SLOTS) & 1)) continue;
-        // the first product of an item overwrites O: the previous item's output must have been read out
-        if (j == 0 && act[t] > 0 && !ptx::mbar_test_wait(bar(B_OREAD + t), (act[t] - 1) & 1)) continue;
-        ptx::tc_fence_after();
-        const uint32_t sv = smem_base + C::V_OFF + s * C::V_BYTES;
-        const uint32_t d = tmem_base + t * C::TILE_COLS + C::O_COL;
-        const uint32_t a = tmem_base + t * C::TILE_COLS + C::S_COL;
-#pragma unroll
-        for (int kk = 0; kk < TK / 16; ++kk) {
-          // 16 keys = 16 rows of 128 bytes further into the V tile; 8 packed columns further into P
-          ptx::umma_bf16_ts(d, a + kk * 8, ptx::umma_desc_mn_sw128(sv + kk * 2048, C::V_SUB_BYTES), idesc_pv,
-                            (j > 0 || kk > 0) ? 1u : 0u);
-        }
-        ptx::umma_commit(bar(B_ODONE + t));
-        const uint32_t users = (j < kv0[t] ? 1u : 0u) + (j < kv1[t] ? 1u : 0u);
-        v_used += 1u << (4 * s);
-        if (((v_used >> (4 * s)) & 15u) == users) { ptx::umma_commit(bar(B_VEMPTY + s)); v_used &= ~(15u << (4 * s)); }
-        ++pv_cnt[t]; ++jp[t];
-        progress = true;
-        if (jp[t] == n[t]) {  // item finished for this tile
-          have[t] = false;
-          ++act[t];
-          base[t] += max(kv0[t], kv1[t]);
-          continue;
-        }
-      }
-      if (jq[t] < n[t] && jq[t] == jp[t]) {
-        // ---- S_t = Q_t K_j^T (S is free: the P that aliased it has been consumed by the product above)
-        const int j = jq[t], g = base[t] + j, s = g % K_SLOTS;
-        if (j == 0 && !ptx::mbar_test_wait(bar(B_QFULL + t), act[t] & 1)) continue;
-        if (!ptx::mbar_test_wait(bar(B_KFULL + s), (g / K_SLOTS) & 1)) continue;
-        ptx::tc_fence_after();
-        const uint32_t sq = smem_base + C::Q_OFF + t * C::Q_BYTES;
-        const uint32_t sk = smem_base + C::K_OFF + s * C::CODE_BYTES;
-        const uint32_t d = tmem_base + t * C::TILE_COLS + C::S_COL;
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-#pragma unroll
-          for (int kk = 0; kk < HD / 32; ++kk)
-            ptx::umma_f8(d, code_desc<HD>(sq + part * C::CODE_BYTES + kk * 32), code_desc<HD>(sk + kk * 32), idesc_qk,
-                         (part > 0 || kk > 0) ? 1u : 0u);
-        }
-        ptx::umma_commit(bar(B_SFULL + t));
-        const uint32_t users = (j < kv0[t] ? 1u : 0u) + (j < kv1[t] ? 1u : 0u);
-        k_used += 1u << (4 * s);
-        if (((k_used >> (4 * s)) & 15u) == users) { ptx::umma_commit(bar(B_KEMPTY + s)); k_used &= ~(15u << (4 * s)); }
-        ++jq[t];
-        if (jq[t] == n[t]) ptx::umma_commit(bar(B_QEMPTY + t));  // the tile's Q buffer may be refilled
-        progress = true;
-      }
+      ptx::umma_commit(bar(B_SFULL + 2 * t + h));
+      if (h == 1 || i == nh - 1) ptx::umma_commit(bar(B_KEMPTY + slot));
+      if (i == nh - 1) ptx::umma_commit(bar(B_QEMPTY + t));  // the tile's Q buffer may be refilled
+      return true;
+    };
+    if (nh > 0) {
+      if (!wait(B_QFULL + t, act & 1)) return;
+      if (!issue_s(0)) return;
+      if (nh > 1 && !issue_s(1)) return;
     }
-    if (progress) {
-      idle_polls = 0;
-      t_idle = 0;
-    } else if ((++idle_polls & 1023u) == 0u) {
-      // nothing could be issued for a while: look at the abort flag and the clock
-      if (*abort_flag) { ok = false; break; }
-      const uint64_t now = ptx::globaltimer_ns();
-      if (t_idle == 0) t_idle = now;
-      else if (now - t_idle > limit) { *abort_flag = 1; ok = false; }
+#pragma unroll 1
+    for (int i = 0; i < nh; ++i) {
+      // ---- O += P V of half i
+      const int h = i & 1, g = base + (i >> 1), slot = g % V_SLOTS;
+      if (h == 0 && !wait(B_VFULL + slot, (g / V_SLOTS) & 1)) return;
+      // the first product of an item overwrites O: the previous item's output must have been read out
+      if (i == 0 && act > 0 && !wait(B_OREAD + t, (act - 1) & 1)) return;
+      if (!wait(B_PREADY + 2 * t + h, (p_ph >> h) & 1)) return;
+      p_ph ^= 1u << h;
+      ptx::tc_fence_after();
+      const uint32_t sv = smem_base + C::V_OFF + slot * C::V_BYTES + h * (TH * 128);
+#pragma unroll
+      for (int kk = 0; kk < TH / 16; ++kk) {
+        // 16 keys = 16 rows of 128 bytes further into the V tile; 8 packed columns further into P
+        ptx::umma_bf16_ts(o_col, s_col + h * TH + kk * 8, ptx::umma_desc_mn_sw128(sv + kk * 2048, C::V_SUB_BYTES), idesc_pv,
+                          (i > 0 || kk > 0) ? 1u : 0u);
+      }
+      ptx::umma_commit(bar(B_ODONE + 2 * t + h));
+      if (h == 1 || i == nh - 1) ptx::umma_commit(bar(B_VEMPTY + slot));
+      if (i + 2 < nh && !issue_s(i + 2)) return;
     }
+    // tiles that only the other row tile works on
+#pragma unroll 1
+    for (int j = (nh + 1) / 2; j < n_kv; ++j) {
+      const int g = base + j;
+      if (!wait(B_KFULL + g % K_SLOTS, (g / K_SLOTS) & 1)) return;
+      ptx::mbar_arrive(bar(B_KEMPTY + g % K_SLOTS));
+      if (!wait(B_VFULL + g % V_SLOTS, (g / V_SLOTS) & 1)) return;
+      ptx::mbar_arrive(bar(B_VEMPTY + g % V_SLOTS));
+    }
+    base += n_kv;
+    if (nh > 0) ++act;
   }
 }
 
@@ -518,7 +492,7 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
       ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
       if (!ok) break;
       const Item& it = sh->items[s];
-      n = it.n_kv0 < 0 ? -1 : max(it.n_kv0, it.n_kv1);
+      n = it.n_kv;
       keys = it.pre + it.len - it.jb * TK;  // that the request holds, from the item's first tile on
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B_IEMPTY + s));
@@ -590,9 +564,11 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
       if (i >= B_QFULL && i < B_QFULL + 2) count = 4;
       if (i >= B_VFULL && i < B_VFULL + V_SLOTS) count = 2;         // the two V warps
       if (i >= B_REMPTY && i < B_REMPTY + R_SLOTS) count = 2;
-      if (i >= B_PREADY && i < B_PREADY + 2) count = 4;             // the four softmax warps of the tile
+      if (i >= B_KEMPTY && i < B_KEMPTY + K_SLOTS) count = 2;       // the two row tiles
+      if (i >= B_VEMPTY && i < B_VEMPTY + V_SLOTS) count = 2;
+      if (i >= B_PREADY && i < B_PREADY + 4) count = 4;             // the four softmax warps of the tile
       if (i >= B_OREAD && i < B_OREAD + 2) count = 4;
-      if (i >= B_IEMPTY && i < B_IEMPTY + ITEM_SLOTS) count = 12;   // eight softmax warps, the MMA thread once per tile, two V warps
+      if (i >= B_IEMPTY && i < B_IEMPTY + ITEM_SLOTS) count = 12;   // eight softmax warps, two MMA threads, two V warps
       ptx::mbar_init(bar(i), count);
     }
     ptx::fence_barrier_init();
@@ -613,8 +589,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
 
   if (warp == 0) {
     producer<HD>(&tmap_q, &tmap_k, &tmap_v, p, smem_base, sh, limit);
-  } else if (warp == 1) {
-    if (lane == 0) mma_issuer<HD>(smem_base, tmem_base, sh, limit);
+  } else if (warp == 1 || warp == 12) {
+    if (lane == 0) mma_issuer<HD>(warp == 12, smem_base, tmem_base, sh, limit);
   } else if (warp >= 10) {
     v_converter<HD>(p, smem_base, sh, warp - 10, limit);
   } else {
@@ -627,7 +603,14 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
     const int row_token = row / group, row_head = row - row_token * group;
     int seq = 0;    // items taken from the ring so far
     int base = 0;   // ring position of the current item's first key tile
-    int step = 0;   // key tiles this row tile has processed so far, over all items (phase of s_full / o_done)
+    // Halves of key tiles taken so far from each of the two halves of S, modulo 2: the phases of s_full, and of o_done, which
+    // has two barriers as well: half i of S is seen when the product of half i - 2 has run, but that of i - 1 may not have.
+    uint32_t s_ph = 0;
+    auto wait_product = [&](int h) {  // the last product of P in that half
+      const bool done = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + 2 * t + h), ((s_ph >> h) & 1) ^ 1u, abort_flag, limit));
+      ptx::tc_fence_after();
+      return done;
+    };
     int act = 0;    // items with work for this row tile
     bool q_ready = false;  // the next one's q has been converted
     bool ok = true;
@@ -642,14 +625,14 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         if (lane == 0) ptx::mbar_arrive(bar(B_IEMPTY + s));
         ++seq;
       }
-      if (it.n_kv0 < 0) break;  // no more items
-      const int n_kv = t == 0 ? it.n_kv0 : it.n_kv1;
+      if (it.n_kv < 0) break;  // no more items
+      const int nh = t == 0 ? it.halves[0] : it.halves[1];
       const int item_base = base;
-      base += max(it.n_kv0, it.n_kv1);
+      base += it.n_kv;
       const int token0 = it.t0 + t * p.tile_tokens;
       const bool mine = row < tile_rows(p, it, t, group);
       const size_t out_row = static_cast<size_t>(it.start + token0 + row_token) * p.n_q_heads + it.kvh * group + row_head;
-      if (n_kv == 0) {  // no rows, or no keys in this part of the range
+      if (nh == 0) {  // no rows, or no keys in this part of the range
         if (p.n_splits > 1 && mine)
           p.parts.ml[static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row] = make_float2(-CUDART_INF_F, 0.f);
         continue;
@@ -665,46 +648,53 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
       float m_used = -CUDART_INF_F, l_sum = 0.f, row_scale = 0.f;
       int v_exp = 0;
 #pragma unroll 1
-      for (int j = 0; j < n_kv; ++j, ++step) {
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_SFULL + t), step & 1, abort_flag, limit));
+      for (int i = 0; i < nh; ++i) {
+        const int h = i & 1;
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_SFULL + 2 * t + h), (s_ph >> h) & 1, abort_flag, limit));
         if (!ok) break;
+        s_ph ^= 1u << h;
         ptx::tc_fence_after();
         // (written before the barriers that S waited for)
-        if (j == 0) row_scale = mine ? rsqrtf(static_cast<float>(HD)) * LOG2E_F * exp2_int(sh->row_exp[act & 1][t][row]) : 1.f;
-        const TileInfo& info = sh->info[(item_base + j) % INFO_SLOTS];
-        // factor of the scores, per 16 keys (not 0: -inf * 0); read again where it is used, registers are short
-        auto sl = [&](int c) { return fmaxf(row_scale * *const_cast<volatile const float*>(&info.k_mul[c]), 1.17549435e-38f); };
+        if (i == 0) row_scale = mine ? rsqrtf(static_cast<float>(HD)) * LOG2E_F * exp2_int(sh->row_exp[act & 1][t][row]) : 1.f;
+        const TileInfo& info = sh->info[(item_base + (i >> 1)) % INFO_SLOTS];
         const int tile_v_exp = info.v_exp;
-        const int k0 = (it.jb + j) * TK;
-        uint32_t sv[4][32];
+        // factor of the scores, per 16 keys (not 0: -inf * 0)
+        float sl[TH / 16];
+        {
+          const float4 k_mul = *reinterpret_cast<const float4*>(&info.k_mul[h * (TH / 16)]);
+          sl[0] = fmaxf(row_scale * k_mul.x, 1.17549435e-38f); sl[1] = fmaxf(row_scale * k_mul.y, 1.17549435e-38f);
+          sl[2] = fmaxf(row_scale * k_mul.z, 1.17549435e-38f); sl[3] = fmaxf(row_scale * k_mul.w, 1.17549435e-38f);
+        }
+        const int k0 = it.jb * TK + i * TH;
+        const uint32_t s_addr = t_lane + C::S_COL + h * TH;
+        uint32_t sv[TH / 32][32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_lane + C::S_COL + c * 32, sv[c]);
+        for (int c = 0; c < TH / 32; ++c) ptx::tmem_ld_32x32(s_addr + c * 32, sv[c]);
         ptx::tmem_ld_wait();
-        if (k0 + TK - 1 > it.pre + token0) {  // warp-uniform: some row of the tile does not see all keys
+        if (k0 + TH - 1 > it.pre + token0) {  // warp-uniform: some row of the tile does not see all keys
           const int lim = row_pos - k0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < TH / 32; ++c) {
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (c * 32 + e > lim) sv[c][e] = 0xff800000u;  // -inf
           }
         }
         // row maximum: three-input maxima over 16 keys, scaled, over the groups
-        float mx8[TK / 16];
+        float mx = -CUDART_INF_F;
 #pragma unroll
-        for (int c = 0; c < TK / 16; ++c) {
+        for (int c = 0; c < TH / 16; ++c) {
           const uint32_t(&v)[32] = sv[c >> 1];
           const int o = (c & 1) * 16;
           float m = fmaxf(__uint_as_float(v[o]), __uint_as_float(v[o + 1]));
 #pragma unroll
           for (int e = 2; e < 16; e += 2) m = ptx::fmax3(m, __uint_as_float(v[o + e]), __uint_as_float(v[o + e + 1]));
-          mx8[c] = m * sl(c);
+          mx = fmaxf(mx, m * sl[c]);
         }
-        const float mx = fmaxf(ptx::fmax3(ptx::fmax3(mx8[0], mx8[1], mx8[2]), mx8[3], mx8[4]), ptx::fmax3(mx8[5], mx8[6], mx8[7]));
         // lazy reference: keep the old one unless this tile exceeds it by more than the threshold; the unit of V may grow
         float factor = 1.f;
         bool grow = false;
-        if (j == 0) {
+        if (i == 0) {
           m_used = mx;
           v_exp = tile_v_exp;
         } else {
@@ -721,10 +711,9 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
           }
         }
         if (__any_sync(0xffffffffu, grow)) {
-          // O must be stable: the P V product of the previous tile has finished
-          ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + t), (step - 1) & 1, abort_flag, limit));
+          // O must be stable: the P V product of the previous half has finished
+          ok = wait_product(h ^ 1);
           if (!ok) break;
-          ptx::tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < HD / 32; ++c) {
             uint32_t ov[32];
@@ -740,27 +729,19 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         const float neg_m = (m_used == -CUDART_INF_F ? 0.f : -m_used) + P_SHIFT;
         const uint64_t negm_2 = ptx::pack_f32x2(neg_m, neg_m);
         uint64_t ps[4] = {0ull, 0ull, 0ull, 0ull}, sl2 = 0ull;
+        uint32_t pk[32];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t pk[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            // packed column 32 c + e holds keys 2 (32 c + e) and 2 (32 c + e) + 1
-            const int k_lo = (c * 32 + e) * 2;
-            const uint64_t x2 = ptx::pack_f32x2(__uint_as_float(sv[k_lo >> 5][k_lo & 31]),
-                                                __uint_as_float(sv[k_lo >> 5][(k_lo & 31) + 1]));
-            if (e % 8 == 0) {
-              const float f = sl(k_lo >> 4);
-              sl2 = ptx::pack_f32x2(f, f);
-            }
-            float y0, y1;
-            ptx::unpack_f32x2(ptx::fma_f32x2(x2, sl2, negm_2), y0, y1);
-            const float p0 = ptx::ex2_approx(y0), p1 = ptx::ex2_approx(y1);
-            ps[e & 3] = ptx::add_f32x2(ps[e & 3], ptx::pack_f32x2(p0, p1));
-            pk[e] = pack_f16(p0, p1);
-          }
-          ptx::tmem_st_32x32(t_lane + C::S_COL + c * 32, pk);
+        for (int e = 0; e < 32; ++e) {
+          // packed column e holds keys 2 e and 2 e + 1
+          const uint64_t x2 = ptx::pack_f32x2(__uint_as_float(sv[e >> 4][(2 * e) & 31]), __uint_as_float(sv[e >> 4][(2 * e + 1) & 31]));
+          if (e % 8 == 0) sl2 = ptx::pack_f32x2(sl[e / 8], sl[e / 8]);
+          float y0, y1;
+          ptx::unpack_f32x2(ptx::fma_f32x2(x2, sl2, negm_2), y0, y1);
+          const float p0 = ptx::ex2_approx(y0), p1 = ptx::ex2_approx(y1);
+          ps[e & 3] = ptx::add_f32x2(ps[e & 3], ptx::pack_f32x2(p0, p1));
+          pk[e] = pack_f16(p0, p1);
         }
+        ptx::tmem_st_32x32(s_addr, pk);
         {
           float a0, a1;
           ptx::unpack_f32x2(ptx::add_f32x2(ptx::add_f32x2(ps[0], ps[1]), ptx::add_f32x2(ps[2], ps[3])), a0, a1);
@@ -769,7 +750,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         ptx::tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(B_PREADY + t));
+        if (lane == 0) ptx::mbar_arrive(bar(B_PREADY + 2 * t + h));
       }
       if (!ok) break;
       ++act;
@@ -778,7 +759,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         const int s = seq & (ITEM_SLOTS - 1);
         ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
         if (!ok) break;
-        if ((t == 0 ? sh->items[s].n_kv0 : sh->items[s].n_kv1) > 0 && sh->items[s].n_kv0 >= 0) {
+        if (sh->items[s].n_kv >= 0 && sh->items[s].halves[t] > 0) {
           ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_QRAW + t), act & 1, abort_flag, limit));
           if (!ok) break;
           convert_q<HD>(smem_base + C::Q_OFF + t * C::Q_BYTES, lane_group * 32, sh->row_exp[act & 1][t]);
@@ -787,49 +768,45 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         }
       }
       // ---- it has finished: store the tile's rows
-      ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + t), (step - 1) & 1, abort_flag, limit));
+      ok = wait_product((nh - 1) & 1);
       if (!ok) break;
-      ptx::tc_fence_after();
-      // the whole row first, so that the next item's first product may overwrite O as early as possible
-      uint32_t ov[HD / 32][32];
-#pragma unroll
-      for (int c = 0; c < HD / 32; ++c) ptx::tmem_ld_32x32(t_lane + C::O_COL + c * 32, ov[c]);
-      ptx::tmem_ld_wait();
-      ptx::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(bar(B_OREAD + t));
       // o = O 2^(v_exp) / (sum of 2^7 p); the two factors apart, so that neither leaves the normal range
-      const float unit = exp2_int(v_exp);
-      if (mine && p.n_splits == 1) {
-        const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
-        bf16* dst = p.o + out_row * HD;
-        // a thread owns a row, so every store of a warp touches 32 different lines: 32-byte stores halve their number
+      const float unit = exp2_int(v_exp), inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
+      const size_t part = static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row;
+#pragma unroll 1
+      for (int c0 = 0; c0 < HD; c0 += 64) {
+        uint32_t ov[2][32];
+        ptx::tmem_ld_32x32(t_lane + C::O_COL + c0, ov[0]);
+        ptx::tmem_ld_32x32(t_lane + C::O_COL + c0 + 32, ov[1]);
+        ptx::tmem_ld_wait();
+        if (c0 == HD - 64) {  // the next item's first product may overwrite O
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(B_OREAD + t));
+        }
+        if (mine && p.n_splits == 1) {
+          bf16* dst = p.o + out_row * HD + c0;
+          // a thread owns a row, so every store of a warp touches 32 different lines: 32-byte stores halve their number
 #pragma unroll
-        for (int c = 0; c < HD / 32; ++c) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 16) {
+          for (int e = 0; e < 64; e += 16) {
             uint32_t w[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-              w[q] = ptx::pack_bf16(__uint_as_float(ov[c][e + 2 * q]) * inv * unit, __uint_as_float(ov[c][e + 2 * q + 1]) * inv * unit);
-            ptx::st_global_v8(dst + c * 32 + e, w);
+              w[q] = ptx::pack_bf16(__uint_as_float(ov[e >> 5][(e & 31) + 2 * q]) * inv * unit, __uint_as_float(ov[e >> 5][(e & 31) + 2 * q + 1]) * inv * unit);
+            ptx::st_global_v8(dst + e, w);
           }
-        }
-      } else if (mine) {
-        const size_t part = static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row;
-        float* dst = p.parts.o + part * HD;
+        } else if (mine) {
+          float* dst = p.parts.o + part * HD + c0;
 #pragma unroll
-        for (int c = 0; c < HD / 32; ++c) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+          for (int e = 0; e < 64; e += 8) {
             uint32_t w[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) w[q] = __float_as_uint(__uint_as_float(ov[c][e + q]) * unit);
-            ptx::st_global_v8(dst + c * 32 + e, w);
+            for (int q = 0; q < 8; ++q) w[q] = __float_as_uint(__uint_as_float(ov[e >> 5][(e & 31) + q]) * unit);
+            ptx::st_global_v8(dst + e, w);
           }
         }
-        p.parts.ml[part] = make_float2(m_used, l_sum);
       }
+      if (mine && p.n_splits > 1) p.parts.ml[part] = make_float2(m_used, l_sum);
       __syncwarp();
     }
   }
