@@ -17,12 +17,21 @@
 //     unnormalised fp32 rows with their maximum and sum, and a second kernel joins them.
 //   * Items are handed out by the hardware: the grid has one block per item, a resident block that is done takes over the
 //     next block that has not been started (clusterlaunchcontrol), so there is no counter in memory to share or to reset.
-//   warp 0      : producer     - takes items over, publishes them in a ring, starts the copies of Q, K and V tiles and
-//                 publishes the scales of the pages
-//   warp 1      : MMA issuer   - S = Q K^T, O += P V (P read from tensor memory), whichever is ready
-//   warps 2-5, 6-9 : softmax of row tile 0, 1, one row per thread; they also turn the next item's Q into codes, while the
-//                 last product of the current one runs, and store the output rows
-//   warps 10-11 : V tiles, 64 keys each, from codes to f16
+//   * S, P and both products advance by half a key tile: S of a half is written over the P that a product has just consumed,
+//     while the softmax works on the other half (a prompt of 4096 tokens: 168 us, 208 us by whole tiles; 8192: 547, 720).
+//   * 2^x of one pair of scores in eight is computed with products and sums instead of the special-function unit, which the
+//     rest keeps busy for half of a step (1 x 8192: 547 us, 560 without; one in four is slower again, 577).
+//   warp 0        : producer     - takes items over, publishes them in a ring, starts the copies of Q, K and V tiles and
+//                   publishes the scales of the pages
+//   warps 1, 2    : MMA issuers of row tile 0, 1 - S = Q K^T, O += P V (P read from tensor memory)
+//   warps 4-7, 8-11 : softmax of row tile 0, 1, one row per thread; they also turn the next item's Q into codes, while the
+//                   last product of the current one runs, and store the output rows
+//   warps 12-15   : V tiles, 32 keys each, from codes to f16
+// What bounds it: the issuers.  A half costs a row tile 12 products, 650 cycles of the tensor pipe when back to back, 1300 for
+// both tiles; their thread gets them out at 1000 to 1600 between the other warps of its scheduler, the period of a half is
+// 2150.  So an issuer runs its code as a whole warp (uniform addresses: one lane alone 4 % slower), descriptors are a sum with
+// a constant, and loops that every warp shares the instruction caches with are kept small (roles inlined: 1.4 times the time).
+// Measured: 358 Gflop of 37 chunks at 1000 Tflop/s (fp16 flops of the formula).
 // Every wait is wall-clock bounded and leaves through the common teardown.
 #include <math_constants.h>
 
@@ -34,7 +43,8 @@ namespace {
 constexpr int TQ = 128;                    // rows per row tile
 constexpr int TK = 128;                    // keys per key tile
 constexpr int TH = TK / 2;                 // half a key tile: scores, weights and products advance by it
-constexpr int THREADS = 416;
+constexpr int THREADS = 512;
+constexpr int SOFTMAX_REGS = 168, OTHER_REGS = 88;  // registers of 8 warps each: together what the block is launched with, 16 x 128
 constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr float RESCALE_THRESHOLD = 8.f;   // log2 units
 constexpr float P_SHIFT = 7.f;             // p is kept as 2^7 p: at most 2^15, below f16's 65504
@@ -124,6 +134,34 @@ __device__ __forceinline__ float exp2_int(int e) {  // 2^e, e within -126 .. 127
 }
 __device__ __forceinline__ void sts64(uint32_t addr, uint32_t a, uint32_t b) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+// A wait of a whole warp: one look and one vote where the phase is over, the bounded loop only where it is not.
+__device__ __forceinline__ bool slow_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint64_t limit) {
+  return ptx::mbar_wait_bounded(bar, parity, abort_flag, limit);
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint64_t limit) {
+  if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, slow_wait(bar, parity, abort_flag, limit));
+}
+// 2^y of two numbers with the arithmetic of products and sums: 2^n times a polynomial in f = y - n, n the nearest integer
+// (read off the sum with 1.5 * 2^23), of degree 4 with the smallest largest relative error on [-1/2, 1/2] (found by Remez
+// exchange: 2^-18.5, 2^-7 of a rounding to f16).  Below 2^-126: 2^-126.  A NaN stays one.
+__device__ __forceinline__ void exp2_poly(float y0, float y1, float& p0, float& p1) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(y0) : "f"(-126.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(y1) : "f"(-126.f));
+  auto both = [](float v) { return ptx::pack_f32x2(v, v); };
+  const uint64_t y = ptx::pack_f32x2(y0, y1);
+  const uint64_t r = ptx::add_f32x2(y, both(12582912.f));
+  const uint64_t f = ptx::fma_f32x2(ptx::add_f32x2(r, both(-12582912.f)), both(-1.f), y);
+  uint64_t v = ptx::fma_f32x2(f, both(0.009570102207f), both(0.05591785908f));
+  v = ptx::fma_f32x2(f, v, both(0.2402474433f));
+  v = ptx::fma_f32x2(f, v, both(0.6931217909f));
+  v = ptx::fma_f32x2(f, v, both(0.9999992847f));
+  float r0, r1;
+  ptx::unpack_f32x2(r, r0, r1);
+  const uint64_t n = ptx::pack_f32x2(__uint_as_float((__float_as_uint(r0) << 23) + 0x3f800000u),
+                                     __uint_as_float((__float_as_uint(r1) << 23) + 0x3f800000u));
+  ptx::unpack_f32x2(ptx::mul_f32x2(v, n), p0, p1);
 }
 // Byte offset of 16-byte chunk c (8 features) of a row of a V tile: sub-tiles of 64 features, 128-byte rows, swizzled.
 template <int HD>
@@ -386,92 +424,147 @@ __device__ __noinline__ void producer(const CUtensorMap* tmap_q, const CUtensorM
   }
 }
 
-// ------------------------------------------------------------------------- warps 1, 12: MMA issuers, one per row tile
+// Issued by the lane whose predicate is set; the whole warp runs the code, so that addresses and descriptors are uniform.
+__device__ __forceinline__ void umma_f8_if(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void umma_f16_ts_if(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void commit_if(uint32_t leader, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+               "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
+}
+// The first lane's value, which the compiler then knows to be the whole warp's.
+template <typename T>
+__device__ __forceinline__ T uniform(T v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ void arrive_if(uint32_t leader, uint32_t bar) {
+  __syncwarp();
+  if (leader) ptx::mbar_arrive(bar);
+  __syncwarp();
+}
+// A descriptor whose address lies `bytes` further (addresses stay below 2^18, so nothing carries out of the field).
+__device__ __forceinline__ uint64_t desc_plus(uint64_t desc, uint32_t bytes) {
+  return (desc & 0xffffffff00000000ull) | (static_cast<uint32_t>(desc) + (bytes >> 4));
+}
+// ------------------------------------------------------------------------- warps 1, 2: MMA issuers, one per row tile
 // S of half a key tile, and P V of it, at a time: the half of S that a product has consumed is written again at once, while
 // the softmax works on the other half.
 template <int HD>
-__device__ __noinline__ void mma_issuer(const int t, const uint32_t smem_base, const uint32_t tmem_base, Shared* sh, const uint64_t limit) {
+__device__ __noinline__ void mma_issuer(const int tile, const uint32_t smem_b, const uint32_t tmem_b, Shared* sh, const uint64_t limit) {
   using C = Cfg<HD>;
+  const int t = uniform(tile);
+  const uint32_t smem_base = uniform(smem_b), tmem_base = uniform(tmem_b);
   const uint32_t bar0 = ptx::smem_u32(sh->bars);
   auto bar = [&](int i) { return bar0 + 8u * i; };
   volatile int* abort_flag = &sh->abort_flag;
   constexpr uint32_t idesc_qk = ptx::umma_idesc_e4m3(TQ, TH);
   constexpr uint32_t idesc_pv = idesc_f16(TQ, HD) | (1u << 16);  // V: MN-major
   const uint32_t s_col = tmem_base + t * C::TILE_COLS + C::S_COL, o_col = tmem_base + t * C::TILE_COLS + C::O_COL;
-  const uint32_t sq = smem_base + C::Q_OFF + t * C::Q_BYTES;
-  auto wait = [&](int b, uint32_t parity) { return ptx::mbar_wait_bounded(bar(b), parity, abort_flag, limit); };
-  int seq = 0;       // items taken from the ring so far
-  int base = 0;      // ring position of the current item's first K / V tile
-  int act = 0;       // items with work for this row tile finished so far
-  uint32_t p_ph = 0; // phases of the two p_ready barriers
+  const uint64_t desc_q = code_desc<HD>(smem_base + C::Q_OFF + t * C::Q_BYTES), desc_k = code_desc<HD>(smem_base + C::K_OFF);
+  const uint64_t desc_v = ptx::umma_desc_mn_sw128(smem_base + C::V_OFF, C::V_SUB_BYTES);
+  auto wait = [&](int b, uint32_t parity) { return warp_wait(bar(b), parity, abort_flag, limit); };
+  const uint32_t leader = (threadIdx.x & 31) == 0;
+  int seq = 0;            // items taken from the ring so far
+  int act = 0;            // items with work for this row tile finished so far
+  int kg = 0, vg = 0;     // ring positions of the next K tile and of the next V tile
+  uint32_t p_ph = 0;      // phase of the p_ready barriers
+  const uint32_t sfull = bar(B_SFULL + 2 * t), odone = bar(B_ODONE + 2 * t), pready = B_PREADY + 2 * t;
+  // S of a half = Q K^T (it overwrites the P that aliased it, which a product issued before has consumed)
+  auto issue_s = [&](int h) {
+    const uint64_t dk = desc_plus(desc_k, (kg % K_SLOTS) * C::CODE_BYTES);
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+#pragma unroll
+      for (int kk = 0; kk < HD / 32; ++kk)
+        umma_f8_if(leader, s_col + h * TH, desc_plus(desc_q, part * C::CODE_BYTES + kk * 32), desc_plus(dk, h * (TH * HD) + kk * 32), idesc_qk,
+                   (part > 0 || kk > 0) ? 1u : 0u);
+    }
+    commit_if(leader, sfull + 8 * h);
+  };
+  // O += P V of a half
+  auto issue_pv = [&](int h, uint32_t accumulate) {
+    const uint64_t dv = desc_plus(desc_v, (vg % V_SLOTS) * C::V_BYTES);
+#pragma unroll
+    for (int kk = 0; kk < TH / 16; ++kk) {
+      // 16 keys = 16 rows of 128 bytes further into the V tile; 8 packed columns further into P
+      umma_f16_ts_if(leader, o_col, s_col + h * TH + kk * 8, desc_plus(dv, h * (TH * 128) + kk * 2048), idesc_pv, kk > 0 ? 1u : accumulate);
+    }
+  };
+  auto wait_k = [&] { return wait(B_KFULL + kg % K_SLOTS, (kg / K_SLOTS) & 1); };
+  auto wait_v = [&] { return wait(B_VFULL + vg % V_SLOTS, (vg / V_SLOTS) & 1); };
   while (true) {
     const int s = seq & (ITEM_SLOTS - 1);
     if (!wait(B_IFULL + s, (seq / ITEM_SLOTS) & 1)) return;
-    const int n_kv = sh->items[s].n_kv, nh = sh->items[s].halves[t];
-    ptx::mbar_arrive(bar(B_IEMPTY + s));
+    const int n_kv = uniform(sh->items[s].n_kv), nh = uniform(sh->items[s].halves[t]);
+    arrive_if(leader, bar(B_IEMPTY + s));
     ++seq;
     if (n_kv < 0) return;
-    // S of half i = Q K^T (it overwrites the P that aliased it, which a product issued before has consumed)
-    auto issue_s = [&](int i) {
-      const int h = i & 1, g = base + (i >> 1), slot = g % K_SLOTS;
-      if (h == 0 && !wait(B_KFULL + slot, (g / K_SLOTS) & 1)) return false;
-      ptx::tc_fence_after();
-      const uint32_t sk = smem_base + C::K_OFF + slot * C::CODE_BYTES + h * (TH * HD);
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-#pragma unroll
-        for (int kk = 0; kk < HD / 32; ++kk)
-          ptx::umma_f8(s_col + h * TH, code_desc<HD>(sq + part * C::CODE_BYTES + kk * 32), code_desc<HD>(sk + kk * 32), idesc_qk,
-                       (part > 0 || kk > 0) ? 1u : 0u);
-      }
-      ptx::umma_commit(bar(B_SFULL + 2 * t + h));
-      if (h == 1 || i == nh - 1) ptx::umma_commit(bar(B_KEMPTY + slot));
-      if (i == nh - 1) ptx::umma_commit(bar(B_QEMPTY + t));  // the tile's Q buffer may be refilled
-      return true;
+    int left = nh;       // halves whose S has not been issued
+    auto k_done = [&] {  // the tile's last S
+      commit_if(leader, bar(B_KEMPTY + kg % K_SLOTS));
+      if (left == 0) commit_if(leader, bar(B_QEMPTY + t));  // the tile's Q buffer may be refilled
+      ++kg;
     };
     if (nh > 0) {
-      if (!wait(B_QFULL + t, act & 1)) return;
-      if (!issue_s(0)) return;
-      if (nh > 1 && !issue_s(1)) return;
-    }
-#pragma unroll 1
-    for (int i = 0; i < nh; ++i) {
-      // ---- O += P V of half i
-      const int h = i & 1, g = base + (i >> 1), slot = g % V_SLOTS;
-      if (h == 0 && !wait(B_VFULL + slot, (g / V_SLOTS) & 1)) return;
-      // the first product of an item overwrites O: the previous item's output must have been read out
-      if (i == 0 && act > 0 && !wait(B_OREAD + t, (act - 1) & 1)) return;
-      if (!wait(B_PREADY + 2 * t + h, (p_ph >> h) & 1)) return;
-      p_ph ^= 1u << h;
+      if (!wait(B_QFULL + t, act & 1) || !wait_k()) return;
       ptx::tc_fence_after();
-      const uint32_t sv = smem_base + C::V_OFF + slot * C::V_BYTES + h * (TH * 128);
+      issue_s(0);
+      --left;
+      if (left > 0) { issue_s(1); --left; }
+      k_done();
+    }
+    // Per tile, and the half h of it: O += P V, then S of that half of the next tile.  As little as possible stands between
+    // the products: one that is followed by an S has no barrier of its own.
+#pragma unroll 1
+    for (int todo = nh; todo > 0; todo -= 2) {
+      if (!wait_v()) return;
+      // the first product of an item overwrites O: the previous item's output must have been read out
+      if (todo == nh && act > 0 && !wait(B_OREAD + t, (act - 1) & 1)) return;
 #pragma unroll
-      for (int kk = 0; kk < TH / 16; ++kk) {
-        // 16 keys = 16 rows of 128 bytes further into the V tile; 8 packed columns further into P
-        ptx::umma_bf16_ts(o_col, s_col + h * TH + kk * 8, ptx::umma_desc_mn_sw128(sv + kk * 2048, C::V_SUB_BYTES), idesc_pv,
-                          (i > 0 || kk > 0) ? 1u : 0u);
+      for (int h = 0; h < 2; ++h) {
+        if (h < todo) {
+          if (!wait(pready + h, (p_ph >> h) & 1)) return;
+          p_ph ^= 1u << h;
+          ptx::tc_fence_after();
+          issue_pv(h, h == 0 && todo == nh ? 0u : 1u);
+          if (h == 1 || todo == 1) commit_if(leader, bar(B_VEMPTY + vg % V_SLOTS));
+          if (left > 0) {
+            if (h == 0) {
+              if (!wait_k()) return;
+              ptx::tc_fence_after();
+            }
+            issue_s(h);
+            --left;
+            if (h == 1 || left == 0) k_done();
+          } else {
+            commit_if(leader, odone + 8 * h);
+          }
+        }
       }
-      ptx::umma_commit(bar(B_ODONE + 2 * t + h));
-      if (h == 1 || i == nh - 1) ptx::umma_commit(bar(B_VEMPTY + slot));
-      if (i + 2 < nh && !issue_s(i + 2)) return;
+      ++vg;
     }
     // tiles that only the other row tile works on
 #pragma unroll 1
     for (int j = (nh + 1) / 2; j < n_kv; ++j) {
-      const int g = base + j;
-      if (!wait(B_KFULL + g % K_SLOTS, (g / K_SLOTS) & 1)) return;
-      ptx::mbar_arrive(bar(B_KEMPTY + g % K_SLOTS));
-      if (!wait(B_VFULL + g % V_SLOTS, (g / V_SLOTS) & 1)) return;
-      ptx::mbar_arrive(bar(B_VEMPTY + g % V_SLOTS));
+      if (!wait_k()) return;
+      arrive_if(leader, bar(B_KEMPTY + kg % K_SLOTS));
+      ++kg;
+      if (!wait_v()) return;
+      arrive_if(leader, bar(B_VEMPTY + vg % V_SLOTS));
+      ++vg;
     }
-    base += n_kv;
     if (nh > 0) ++act;
   }
 }
 
-// ------------------------------------------------------------------------------------------- warps 10, 11: V tiles
+// ------------------------------------------------------------------------------------------- warps 12-15: V tiles
 template <int HD>
-__device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_t smem_base, Shared* sh, const int half,
+__device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_t smem_base, Shared* sh, const int part,
                                          const uint64_t limit) {
   using C = Cfg<HD>;
   constexpr int LPR = HD / 16, RPL = 32 / LPR;     // lanes per row (16 codes each), rows at a time
@@ -479,7 +572,7 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
   auto bar = [&](int i) { return bar0 + 8u * i; };
   volatile int* abort_flag = &sh->abort_flag;
   const int lane = threadIdx.x & 31;
-  const int row_lo = half * 64;                    // this warp's rows of a tile
+  const int row_lo = part * (TK / 4);              // this warp's rows of a tile
   // 16 codes are two chunks of a row; lanes of the second half of a 128-feature row store theirs in the other order, so
   // that eight lanes cover all banks
   const int c = (lane % LPR) * 2, odd = HD == 128 ? (lane >> 2) & 1 : 0;
@@ -509,7 +602,7 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
       const uint32_t src = smem_base + C::R_OFF + r * C::CODE_BYTES + lane * 16, dst = smem_base + C::V_OFF + s * C::V_BYTES;
       // codes * 2^(page exponent - unit) -> f16 operand rows
 #pragma unroll 1
-      for (int r0 = row_lo; r0 < row_lo + 64; r0 += 16) {
+      for (int r0 = row_lo; r0 < row_lo + TK / 4; r0 += 16) {
         uint4 v[16 / RPL];
 #pragma unroll
         for (int q = 0; q < 16 / RPL; ++q)
@@ -538,7 +631,7 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
       __syncwarp();
       if (lane == 0) {
         ptx::mbar_arrive(bar(B_REMPTY + r));
-        if (!(p.test_skip_arrive && half == 1 && g == 1)) ptx::mbar_arrive(bar(B_VFULL + s));
+        if (!(p.test_skip_arrive && part == 1 && g == 1)) ptx::mbar_arrive(bar(B_VFULL + s));
       }
     }
   }
@@ -562,13 +655,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
     for (int i = 0; i < N_BARS; ++i) {
       int count = 1;
       if (i >= B_QFULL && i < B_QFULL + 2) count = 4;
-      if (i >= B_VFULL && i < B_VFULL + V_SLOTS) count = 2;         // the two V warps
-      if (i >= B_REMPTY && i < B_REMPTY + R_SLOTS) count = 2;
+      if (i >= B_VFULL && i < B_VFULL + V_SLOTS) count = 4;         // the four V warps
+      if (i >= B_REMPTY && i < B_REMPTY + R_SLOTS) count = 4;
       if (i >= B_KEMPTY && i < B_KEMPTY + K_SLOTS) count = 2;       // the two row tiles
       if (i >= B_VEMPTY && i < B_VEMPTY + V_SLOTS) count = 2;
       if (i >= B_PREADY && i < B_PREADY + 4) count = 4;             // the four softmax warps of the tile
       if (i >= B_OREAD && i < B_OREAD + 2) count = 4;
-      if (i >= B_IEMPTY && i < B_IEMPTY + ITEM_SLOTS) count = 12;   // eight softmax warps, two MMA threads, two V warps
+      if (i >= B_IEMPTY && i < B_IEMPTY + ITEM_SLOTS) count = 14;   // eight softmax warps, two MMA threads, four V warps
       ptx::mbar_init(bar(i), count);
     }
     ptx::fence_barrier_init();
@@ -587,15 +680,19 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
 
-  if (warp == 0) {
-    producer<HD>(&tmap_q, &tmap_k, &tmap_v, p, smem_base, sh, limit);
-  } else if (warp == 1 || warp == 12) {
-    if (lane == 0) mma_issuer<HD>(warp == 12, smem_base, tmem_base, sh, limit);
-  } else if (warp >= 10) {
-    v_converter<HD>(p, smem_base, sh, warp - 10, limit);
+  if (warp < 4 || warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+    if (warp == 0) {
+      producer<HD>(&tmap_q, &tmap_k, &tmap_v, p, smem_base, sh, limit);
+    } else if (warp == 1 || warp == 2) {
+      mma_issuer<HD>(warp - 1, smem_base, tmem_base, sh, limit);
+    } else if (warp >= 12) {
+      v_converter<HD>(p, smem_base, sh, warp - 12, limit);
+    }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     // ---------------------------------------------------------------- softmax
-    const int t = (warp - 2) >> 2;       // row tile of this warpgroup
+    const int t = (warp - 4) >> 2;       // row tile of this warpgroup
     const int lane_group = warp & 3;     // tensor-memory lanes this warp may touch
     const int row = lane_group * 32 + lane;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(lane_group * 32) << 16) + t * C::TILE_COLS;
@@ -603,14 +700,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
     const int row_token = row / group, row_head = row - row_token * group;
     int seq = 0;    // items taken from the ring so far
     int base = 0;   // ring position of the current item's first key tile
-    // Halves of key tiles taken so far from each of the two halves of S, modulo 2: the phases of s_full, and of o_done, which
-    // has two barriers as well: half i of S is seen when the product of half i - 2 has run, but that of i - 1 may not have.
-    uint32_t s_ph = 0;
-    auto wait_product = [&](int h) {  // the last product of P in that half
-      const bool done = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + 2 * t + h), ((s_ph >> h) & 1) ^ 1u, abort_flag, limit));
-      ptx::tc_fence_after();
-      return done;
-    };
+    uint32_t s_ph = 0, o_ph = 0;  // phases of the two s_full and of the two o_done barriers
     int act = 0;    // items with work for this row tile
     bool q_ready = false;  // the next one's q has been converted
     bool ok = true;
@@ -650,7 +740,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
 #pragma unroll 1
       for (int i = 0; i < nh; ++i) {
         const int h = i & 1;
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_SFULL + 2 * t + h), (s_ph >> h) & 1, abort_flag, limit));
+        ok = warp_wait(bar(B_SFULL + 2 * t + h), (s_ph >> h) & 1, abort_flag, limit);
         if (!ok) break;
         s_ph ^= 1u << h;
         ptx::tc_fence_after();
@@ -712,8 +802,11 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         }
         if (__any_sync(0xffffffffu, grow)) {
           // O must be stable: the P V product of the previous half has finished
-          ok = wait_product(h ^ 1);
+          // (S of half i + 1 follows it, the last two products of an item have a barrier)
+          const uint32_t b = i + 1 < nh ? bar(B_SFULL + 2 * t + (h ^ 1)) : bar(B_ODONE + 2 * t + (h ^ 1));
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(b, ((i + 1 < nh ? s_ph : o_ph) >> (h ^ 1)) & 1, abort_flag, limit));
           if (!ok) break;
+          ptx::tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < HD / 32; ++c) {
             uint32_t ov[32];
@@ -737,7 +830,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
           if (e % 8 == 0) sl2 = ptx::pack_f32x2(sl[e / 8], sl[e / 8]);
           float y0, y1;
           ptx::unpack_f32x2(ptx::fma_f32x2(x2, sl2, negm_2), y0, y1);
-          const float p0 = ptx::ex2_approx(y0), p1 = ptx::ex2_approx(y1);
+          float p0, p1;
+          if (e % 8 == 3) {  // (one pair in eight)
+            exp2_poly(y0, y1, p0, p1);
+          } else {
+            p0 = ptx::ex2_approx(y0);
+            p1 = ptx::ex2_approx(y1);
+          }
           ps[e & 3] = ptx::add_f32x2(ps[e & 3], ptx::pack_f32x2(p0, p1));
           pk[e] = pack_f16(p0, p1);
         }
@@ -768,8 +867,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         }
       }
       // ---- it has finished: store the tile's rows
-      ok = wait_product((nh - 1) & 1);
-      if (!ok) break;
+      {
+        const int h = (nh - 1) & 1;
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + 2 * t + h), (o_ph >> h) & 1, abort_flag, limit));
+        if (!ok) break;
+        o_ph ^= nh > 1 ? 3u : 1u;
+      }
+      ptx::tc_fence_after();
       // o = O 2^(v_exp) / (sum of 2^7 p); the two factors apart, so that neither leaves the normal range
       const float unit = exp2_int(v_exp), inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
       const size_t part = static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row;

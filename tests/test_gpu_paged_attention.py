@@ -292,3 +292,21 @@ def test_prefill_replayed(pdlib):
         g.replay()
     torch.cuda.synchronize()
     np.testing.assert_array_equal(from_dev(out), ref)
+
+
+def test_prefill_nan_key_at_every_position(pdlib):
+    """A NaN in the cached K of one key makes the rows that see it NaN and leaves the others alone, wherever the key stands in
+    a tile (the weights of a tile's keys are not all computed in the same way)."""
+    hq, hkv, hd, page_len, new, prefix = 8, 2, 64, 32, 40, 120
+    c = Cache(pdlib, hkv, hd, page_len, [new + prefix], seed=77)
+    c.fill([new + prefix], np.random.default_rng(77), 0.5)
+    clean = c.k.copy()
+    q = gen.normal_bf16(91, gen.S_X, (new, hq, hd), 1.0)
+    for key in list(range(64)) + [prefix - 1, prefix, prefix + 7, prefix + new - 1]:
+        c.k = clean.copy()
+        c.k[c.table[0][key // page_len], 1, key % page_len, key % hd] = 0x7F  # the second KV head: query heads 4 .. 7
+        c.upload()
+        got = np.asarray(prefill(pdlib, c, hq, q, [new], [prefix]), dtype=np.float64).reshape(new, hq, hd)
+        sees = np.arange(new) + prefix >= key
+        assert np.isnan(got[sees][:, 4:]).all(), key
+        assert np.isfinite(got[:, :4]).all() and np.isfinite(got[~sees]).all(), key
