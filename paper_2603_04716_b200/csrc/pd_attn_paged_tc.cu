@@ -24,9 +24,8 @@
 //   warp 0        : producer     - takes items over, publishes them in a ring, starts the copies of Q, K and V tiles and
 //                   publishes the scales of the pages
 //   warps 1, 2    : MMA issuers of row tile 0, 1 - S = Q K^T, O += P V (P read from tensor memory)
-//   warps 4-7, 8-11 : softmax of row tile 0, 1, one row per thread; they also turn the next item's Q into codes, while the
-//                   last product of the current one runs, and store the output rows
-//   warps 12-15   : V tiles, 32 keys each, from codes to f16
+//   warps 4-7, 8-11 : softmax of row tile 0, 1, one row per thread; they also store the output rows
+//   warps 12-15   : 32 rows each - V tiles from codes to f16, Q into two codes (while the item before is finished)
 // What bounds it: the issuers.  A half costs a row tile 12 products, 650 cycles of the tensor pipe when back to back, 1300 for
 // both tiles; their thread gets them out at 1000 to 1600 between the other warps of its scheduler, the period of a half is
 // 2150.  So an issuer runs its code as a whole warp (uniform addresses: one lane alone 4 % slower), descriptors are a sum with
@@ -126,6 +125,16 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t f16x2_to_e4m3x2(uint32_t v) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(v));
+  return r;
+}
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
@@ -210,7 +219,7 @@ __device__ __forceinline__ int tile_rows(const PagedPrefillDev& p, const Item& i
 // q of 32 rows of a row tile, in place: the buffer holds the bf16 rows as TMA has brought them, the first half of the
 // features of a row where the first number of that row goes, the second half where the second goes; they become two E4M3
 // numbers and the rows' exponents.  Four lanes share a row, eight rows at a time.  All lanes of a warp call.  A function of
-// its own (never inlined), like the roles below, so that its registers are allocated apart from the softmax code.
+// its own (never inlined), like the roles below, so that its registers are allocated apart from theirs.
 template <int HD>
 __device__ __noinline__ void convert_q(const uint32_t tile, const int first, int8_t* exps) {
   const int lane = threadIdx.x & 31, quarter = lane & 3;
@@ -219,48 +228,34 @@ __device__ __noinline__ void convert_q(const uint32_t tile, const int first, int
 #pragma unroll 1
   for (int r0 = first; r0 < first + 32; r0 += 8) {
     const int r = r0 + (lane >> 2);
-    uint4 w[NC];
-    float amax = 0.f;
+    uint32_t w[4 * NC], m2 = 0;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[c].x), "=r"(w[c].y), "=r"(w[c].z), "=r"(w[c].w)
+    for (int c = 0; c < NC; ++c)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
                    : "r"(raw + r * HD + c * 16));
-    }
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].x)), fabsf(ptx::bf16_hi(w[c].x)));
-      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].y)), fabsf(ptx::bf16_hi(w[c].y)));
-      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].z)), fabsf(ptx::bf16_hi(w[c].z)));
-      amax = ptx::fmax3(amax, fabsf(ptx::bf16_lo(w[c].w)), fabsf(ptx::bf16_hi(w[c].w)));
-    }
-    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));  // (also: the rows have been read whole)
-    // 2^(e + 7) <= amax < 2^(e + 8), e kept where 2^e and 2^-e are normal
-    const int e2 = min(max(static_cast<int>(__float_as_uint(amax) >> 23) - 127 - 7, -126), 120);
+    for (int e = 0; e < 4 * NC; ++e) m2 = __vmaxu2(m2, w[e] & 0x7fff7fffu);  // magnitudes compare as integers
+    m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
+    m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 2));  // (also: the rows have been read whole)
+    const uint32_t amax = max(m2 & 0xffffu, m2 >> 16);       // bits of the largest magnitude
+    // 2^(e + 7) <= the largest < 2^(e + 8), e kept where 2^e and 2^-e are normal
+    const int e2 = min(max(static_cast<int>(amax >> 7) - 127 - 7, -126), 120);
     const float inv = exp2_int(-e2);
-    const bool finite = amax <= 3.402823466e38f;
+    // a row with an infinity or a NaN: all its scores are NaN (E4M3 has no infinity, and the conversion would saturate)
+    const uint32_t spoilt = amax >= 0x7f80u ? 0x7f7f7f7fu : 0u;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const uint32_t ww[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float h[2], l[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float x = (i ? ptx::bf16_hi(ww[e]) : ptx::bf16_lo(ww[e])) * inv;
-          // an infinite q: E4M3 has no infinity, and the conversion would saturate
-          if (!finite && !(fabsf(x) <= 3.402823466e38f)) x = __int_as_float(0x7fc00000);
-          // h: x rounded to four significant bits (a product with 2^20 + 1 and two differences), l: the rest, exactly
-          const float s = __fmul_rn(x, 1048577.f);
-          h[i] = __fsub_rn(s, __fsub_rn(s, x));
-          l[i] = __fsub_rn(x, h[i]);
-        }
-        hi[e] = ptx::cvt_e4m3x2(h[0], h[1]);
-        lo[e] = ptx::cvt_e4m3x2(l[0], l[1]);
+        // at most 2^8 and of 8 significant bits: f16 holds it exactly down to 2^-14 and within 2^-25 below, and what the
+        // first number leaves as well
+        const uint32_t x = pack_f16(ptx::bf16_lo(w[4 * c + e]) * inv, ptx::bf16_hi(w[4 * c + e]) * inv);
+        hi[e] = f16x2_to_e4m3x2(x);
+        lo[e] = f16x2_to_e4m3x2(sub_f16x2(x, e4m3x2_to_f16x2(static_cast<uint16_t>(hi[e]))));
       }
       const uint32_t at = tile + code_off<HD>(r, quarter * NC + c);
-      sts64(at, hi[0] | (hi[1] << 16), hi[2] | (hi[3] << 16));
+      sts64(at, hi[0] | (hi[1] << 16) | spoilt, hi[2] | (hi[3] << 16) | spoilt);
       sts64(at + Cfg<HD>::CODE_BYTES, lo[0] | (lo[1] << 16), lo[2] | (lo[3] << 16));
     }
     if (quarter == 0) exps[r] = static_cast<int8_t>(e2);
@@ -562,7 +557,7 @@ __device__ __noinline__ void mma_issuer(const int tile, const uint32_t smem_b, c
   }
 }
 
-// ------------------------------------------------------------------------------------------- warps 12-15: V tiles
+// ------------------------------------------------------------------------------------------- warps 12-15: Q and V tiles
 template <int HD>
 __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_t smem_base, Shared* sh, const int part,
                                          const uint64_t limit) {
@@ -576,22 +571,35 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
   // 16 codes are two chunks of a row; lanes of the second half of a 128-feature row store theirs in the other order, so
   // that eight lanes cover all banks
   const int c = (lane % LPR) * 2, odd = HD == 128 ? (lane >> 2) & 1 : 0;
-  int seq = 0, g = 0;  // items taken, tiles converted so far
+  int seq = 0, g = 0;       // items taken, V tiles converted so far
+  int act[2] = {0, 0};      // items with work for a row tile so far
   bool ok = true;
   while (ok) {
-    int n, keys;
+    int n, keys, halves[2];
     {
       const int s = seq & (ITEM_SLOTS - 1);
       ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
       if (!ok) break;
       const Item& it = sh->items[s];
       n = it.n_kv;
+      halves[0] = it.halves[0]; halves[1] = it.halves[1];
       keys = it.pre + it.len - it.jb * TK;  // that the request holds, from the item's first tile on
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B_IEMPTY + s));
       ++seq;
     }
     if (n < 0) break;
+    // q, while the item before is still worked on: its copy started when the last Q K^T of that item had run
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (halves[t] == 0) continue;
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_QRAW + t), act[t] & 1, abort_flag, limit));
+      if (!ok) break;
+      convert_q<HD>(smem_base + C::Q_OFF + t * C::Q_BYTES, part * 32, sh->row_exp[act[t] & 1][t]);
+      if (lane == 0) ptx::mbar_arrive(bar(B_QFULL + t));
+      ++act[t];
+    }
+    if (!ok) break;
 #pragma unroll 1
     for (int j = 0; j < n; ++j, ++g, keys -= TK) {
       const int s = g % V_SLOTS, r = g % R_SLOTS;
@@ -702,7 +710,6 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
     int base = 0;   // ring position of the current item's first key tile
     uint32_t s_ph = 0, o_ph = 0;  // phases of the two s_full and of the two o_done barriers
     int act = 0;    // items with work for this row tile
-    bool q_ready = false;  // the next one's q has been converted
     bool ok = true;
     while (ok) {
       Item it;
@@ -727,13 +734,6 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
           p.parts.ml[static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row] = make_float2(-CUDART_INF_F, 0.f);
         continue;
       }
-      if (!q_ready) {  // (a block's first item, or the one after an item without work for this tile)
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_QRAW + t), act & 1, abort_flag, limit));
-        if (!ok) break;
-        convert_q<HD>(smem_base + C::Q_OFF + t * C::Q_BYTES, lane_group * 32, sh->row_exp[act & 1][t]);
-        if (lane == 0) ptx::mbar_arrive(bar(B_QFULL + t));
-      }
-      q_ready = false;
       const int row_pos = it.pre + token0 + row_token;  // last key the row may see
       float m_used = -CUDART_INF_F, l_sum = 0.f, row_scale = 0.f;
       int v_exp = 0;
@@ -853,20 +853,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
       }
       if (!ok) break;
       ++act;
-      // ---- while the item's last P V product runs: q of the next item (its copy started when the last Q K^T had run)
-      {
-        const int s = seq & (ITEM_SLOTS - 1);
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
-        if (!ok) break;
-        if (sh->items[s].n_kv >= 0 && sh->items[s].halves[t] > 0) {
-          ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_QRAW + t), act & 1, abort_flag, limit));
-          if (!ok) break;
-          convert_q<HD>(smem_base + C::Q_OFF + t * C::Q_BYTES, lane_group * 32, sh->row_exp[act & 1][t]);
-          if (lane == 0) ptx::mbar_arrive(bar(B_QFULL + t));
-          q_ready = true;
-        }
-      }
-      // ---- it has finished: store the tile's rows
+      // ---- the last product: store the tile's rows
       {
         const int h = (nh - 1) & 1;
         ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_ODONE + 2 * t + h), (o_ph >> h) & 1, abort_flag, limit));
