@@ -228,11 +228,12 @@ __device__ __noinline__ void convert_q(const uint32_t tile, const int first, int
 #pragma unroll 1
   for (int r0 = first; r0 < first + 32; r0 += 8) {
     const int r = r0 + (lane >> 2);
+    const int turn = r & (NC - 1);  // rows take their chunks in different orders, so that eight lanes cover all banks
     uint32_t w[4 * NC], m2 = 0;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
       asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
-                   : "r"(raw + r * HD + c * 16));
+                   : "r"(raw + r * HD + (c ^ turn) * 16));
 #pragma unroll
     for (int e = 0; e < 4 * NC; ++e) m2 = __vmaxu2(m2, w[e] & 0x7fff7fffu);  // magnitudes compare as integers
     m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
@@ -254,7 +255,7 @@ __device__ __noinline__ void convert_q(const uint32_t tile, const int first, int
         hi[e] = f16x2_to_e4m3x2(x);
         lo[e] = f16x2_to_e4m3x2(sub_f16x2(x, e4m3x2_to_f16x2(static_cast<uint16_t>(hi[e]))));
       }
-      const uint32_t at = tile + code_off<HD>(r, quarter * NC + c);
+      const uint32_t at = tile + code_off<HD>(r, quarter * NC + (c ^ turn));
       sts64(at, hi[0] | (hi[1] << 16) | spoilt, hi[2] | (hi[3] << 16) | spoilt);
       sts64(at + Cfg<HD>::CODE_BYTES, lo[0] | (lo[1] << 16), lo[2] | (lo[3] << 16));
     }
