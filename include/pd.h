@@ -458,9 +458,8 @@ pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int3
 
 /* pd_prefill_attention over the 8-bit paged cache: row t of request r is the query at position prefix[r] + t and attends to
  * positions 0 .. prefix[r] + t of page_table row r (its own tokens must have been appended).  Serves whole prompts, chunks of
- * prompts and a few drafted tokens per sequence: one of three kernels is taken from the host lengths (a streaming one for few
- * rows, a tensor-memory one on the codes themselves, or the kernel of pd_prefill_attention on a decoded copy for long runs);
- * they agree within the rounding of the softmax weights to 16 bits and of the result.
+ * prompts and a few drafted tokens per sequence: one of two kernels is taken from the host lengths (a streaming one for few
+ * rows, a tensor-memory one otherwise); they agree within the rounding of the softmax weights to f16 and of the result.
  *   q, out        as for pd_prefill_attention (q 16-byte aligned, out 32-byte aligned)
  *   cu_seqlens    device and host copy;  prefix  device and host copy, both or neither (NULL = 0)
  *   workspace     at least pd_paged_prefill_attention_workspace_bytes() bytes for the longest prefix[r] + len_r, 256-byte

@@ -457,28 +457,30 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
   }
 }
 
-// Joins the parts of a row: one block per (token, query head).  Every warp computes the weights of all parts (a part per lane),
-// the warps share the parts' outputs and add up in shared memory.  All loads of up to 32 parts are issued before the first
-// is used; outputs of parts without keys are loaded, too, and left out.
-constexpr int PC_WARPS = 4;
+// Joins the parts of a row = (token, query head).  With few rows or many parts the four warps of a block share a row: each
+// computes the weights of all parts (a part per lane), they divide the parts' outputs and add up in shared memory.  Otherwise
+// every warp has a row (16384 rows of two parts: 8 us, 24 with a block per row).  All loads of a round are issued before the
+// first is used; outputs of parts without keys are loaded, too, and left out.
+constexpr int PJ_WARPS = 4, PJ_PARTS = 8;  // parts per warp and round
 
-template <int HD>
-__global__ void __launch_bounds__(PC_WARPS * 32) paged_join_kernel(const PagedParts p, bf16* o, long long rows, int n_splits) {
-  constexpr int V = HD / 32, NR = 32 / PC_WARPS;  // features per lane, parts per warp and round
+template <int HD, int WARPS_PER_ROW>
+__global__ void __launch_bounds__(PJ_WARPS * 32) paged_join_kernel(const PagedParts p, bf16* o, long long rows, int n_splits) {
+  constexpr int V = HD / 32, ROUND = PJ_PARTS * WARPS_PER_ROW;  // features per lane, parts per round
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const size_t row = blockIdx.x;
-  __shared__ float acc[PC_WARPS][HD];
+  const int share = WARPS_PER_ROW == 1 ? 0 : warp;
+  const long long row = WARPS_PER_ROW == 1 ? 1ll * blockIdx.x * PJ_WARPS + warp : blockIdx.x;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
+  if (row >= rows) return;  // (a whole warp, and only where warps do not meet)
   float m_run = -CUDART_INF_F, l = 0.f, o_sum[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) o_sum[e] = 0.f;
-  for (int s0 = 0; s0 < n_splits; s0 += 32) {
-    const float2 st = s0 + lane < n_splits ? p.ml[static_cast<size_t>(s0 + lane) * rows + row] : make_float2(-CUDART_INF_F, 0.f);
-    float v[NR][V];
+  for (int s0 = 0; s0 < n_splits; s0 += ROUND) {
+    const float2 st = lane < ROUND && s0 + lane < n_splits ? p.ml[static_cast<size_t>(s0 + lane) * rows + row] : make_float2(-CUDART_INF_F, 0.f);
+    float v[PJ_PARTS][V];
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int s = s0 + i * PC_WARPS + warp;
+    for (int i = 0; i < PJ_PARTS; ++i) {
+      const int s = s0 + i * WARPS_PER_ROW + share;
 #pragma unroll
       for (int e = 0; e < V; ++e) v[i][e] = 0.f;
       if (s < n_splits) {
@@ -504,8 +506,8 @@ __global__ void __launch_bounds__(PC_WARPS * 32) paged_join_kernel(const PagedPa
     for (int e = 0; e < V; ++e) o_sum[e] *= corr;
     const uint32_t held_mask = __ballot_sync(0xffffffffu, held);
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int s = i * PC_WARPS + warp;
+    for (int i = 0; i < PJ_PARTS; ++i) {
+      const int s = i * WARPS_PER_ROW + share;
       const float f = __shfl_sync(0xffffffffu, f_lane, s);
       if ((held_mask >> s) & 1u) {
 #pragma unroll
@@ -515,12 +517,22 @@ __global__ void __launch_bounds__(PC_WARPS * 32) paged_join_kernel(const PagedPa
   }
 #pragma unroll
   for (int k = 16; k > 0; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+  if constexpr (WARPS_PER_ROW == 1) {
+    float r[V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) acc[warp][lane * V + e] = o_sum[e];
-  __syncthreads();
-  if (threadIdx.x < HD) {
-    const float sum = (acc[0][threadIdx.x] + acc[1][threadIdx.x]) + (acc[2][threadIdx.x] + acc[3][threadIdx.x]);
-    o[row * HD + threadIdx.x] = __float2bfloat16(l == 0.f ? 0.f : sum / l);  // (no visible entry: zeros)
+    for (int e = 0; e < V; ++e) r[e] = l == 0.f ? 0.f : o_sum[e] / l;  // (no visible entry: zeros)
+    uint32_t* dst = reinterpret_cast<uint32_t*>(o + row * HD + lane * V);
+#pragma unroll
+    for (int e = 0; e < V; e += 2) dst[e / 2] = ptx::pack_bf16(r[e], r[e + 1]);
+  } else {
+    __shared__ float acc[PJ_WARPS][HD];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[warp][lane * V + e] = o_sum[e];
+    __syncthreads();
+    if (threadIdx.x < HD) {
+      const float sum = (acc[0][threadIdx.x] + acc[1][threadIdx.x]) + (acc[2][threadIdx.x] + acc[3][threadIdx.x]);
+      o[row * HD + threadIdx.x] = __float2bfloat16(l == 0.f ? 0.f : sum / l);
+    }
   }
 }
 
@@ -572,9 +584,11 @@ Split decode_split(int batch, int n_kv_heads, int max_kv_len) {
 
 pd_status launch_paged_join(const PagedParts& parts, bf16* o, long long rows, int n_splits, int head_dim, cudaStream_t s) {
   if (rows > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
-  const dim3 grid(static_cast<unsigned>(rows)), block(PC_WARPS * 32);
-  PD_CUDA_TRY(head_dim == 128 ? launch_pdl(paged_join_kernel<128>, grid, block, 0, s, parts, o, rows, n_splits)
-                              : launch_pdl(paged_join_kernel<64>, grid, block, 0, s, parts, o, rows, n_splits));
+  const bool few = n_splits <= PJ_PARTS && rows > 2048;  // (blocks enough for the whole GPU either way)
+  const dim3 grid(static_cast<unsigned>(few ? (rows + PJ_WARPS - 1) / PJ_WARPS : rows)), block(PJ_WARPS * 32);
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, s, parts, o, rows, n_splits); };
+  PD_CUDA_TRY(head_dim == 128 ? (few ? go(paged_join_kernel<128, 1>) : go(paged_join_kernel<128, 4>))
+                              : (few ? go(paged_join_kernel<64, 1>) : go(paged_join_kernel<64, 4>)));
   count_launch();
   return PD_OK;
 }

@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("which", [0, 1])
 def test_each_kernel_on_all_cases(pdlib, which):
     res = subprocess.run([sys.executable, "-m", "pytest", "tests/test_gpu_paged_attention.py", "-k", "prefill", "-x", "-q", "-m", "gpu"],
                          cwd=ROOT, env={**os.environ, "PD_PAGED_PREFILL": str(which)}, capture_output=True, text=True, timeout=600)
