@@ -466,6 +466,8 @@ pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int3
  *                 aligned, not shared by calls that can overlap on the GPU
  *   err_word      optional device int32: 1 if a bounded wait gave up, 2 if a page number lies outside the pool (the output
  *                 of that request is then not meaningful, that of the others is)
+ * A NaN in a cached row of k makes the rows that see it NaN, one in v their values of that feature; rows before it are not
+ * touched.
  * Page scales within a sequence may differ by 2^15 without loss; V values of pages further below the largest lose low bits
  * first.  Only enqueues work. */
 pd_status pd_paged_prefill_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t n_req, int32_t max_kv_len,

@@ -109,6 +109,7 @@ struct Shared {
   int8_t row_exp[2][2][TQ];   // [items with work & 1][row tile][row]: exponent that q of the row was divided by
   uint4 clc;                  // the answer to a request for another block
   uint32_t tmem;
+  int v_nan[8];               // [item & 7]: number of an item with a NaN that not all its rows see
   int abort_flag;
 };
 static_assert(sizeof(Shared) <= 2048, "AUX area");
@@ -266,6 +267,21 @@ __device__ __noinline__ void convert_q(const uint32_t tile, const int first, int
   }
   ptx::fence_proxy_async();
   __syncwarp();
+}
+
+// NaN where a row sees a key (of first .. last) whose NaN codes were left out of the products.
+template <int HD>
+__device__ __noinline__ void put_nans(const PagedPrefillDev& p, int req, int kvh, int first, int last, bf16* out, float* part) {
+  const int32_t* table = p.c.table + static_cast<size_t>(req) * p.c.table_ld;
+  for (int key = first; key <= last; ++key) {
+    const uint8_t* v = v_row(p.c, table, p.n_kv_heads, kvh, HD, key);
+    if (!v) continue;
+    for (int d = 0; d < HD; ++d) {
+      if ((v[d] & 0x7f) != 0x7f) continue;
+      if (out) out[d] = __float2bfloat16(CUDART_NAN_F);
+      else part[d] = CUDART_NAN_F;
+    }
+  }
 }
 
 // --------------------------------------------------------------------------------------------- warp 0: producer
@@ -578,7 +594,7 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
   int act[2] = {0, 0};      // items with work for a row tile so far
   bool ok = true;
   while (ok) {
-    int n, keys, halves[2];
+    int n, keys, seen_by_all, halves[2];
     {
       const int s = seq & (ITEM_SLOTS - 1);
       ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_IFULL + s), (seq / ITEM_SLOTS) & 1, abort_flag, limit));
@@ -586,6 +602,7 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
       const Item& it = sh->items[s];
       n = it.n_kv;
       halves[0] = it.halves[0]; halves[1] = it.halves[1];
+      seen_by_all = it.pre + it.t0 - it.jb * TK;  // the last key that all rows see
       keys = it.pre + it.len - it.jb * TK;  // that the request holds, from the item's first tile on
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B_IEMPTY + s));
@@ -604,7 +621,7 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
     }
     if (!ok) break;
 #pragma unroll 1
-    for (int j = 0; j < n; ++j, ++g, keys -= TK) {
+    for (int j = 0; j < n; ++j, ++g, keys -= TK, seen_by_all -= TK) {
       const int s = g % V_SLOTS, r = g % R_SLOTS;
       ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar(B_RFULL + r), (g / R_SLOTS) & 1, abort_flag, limit));
       if (!ok) break;
@@ -624,6 +641,16 @@ __device__ __noinline__ void v_converter(const PagedPrefillDev& p, const uint32_
         const uint32_t m2 = pack_f16(m, m);
         // rows past the last key, and rows of a page that does not exist, become zeros: 0 * (whatever) must stay 0
         const int valid = d == kNoRows ? 0 : keys;
+        if (r0 + 15 > seen_by_all) {
+          bool seen = false;
+#pragma unroll
+          for (int q = 0; q < 16 / RPL; ++q) {
+            const int row = r0 + q * RPL + lane / LPR;
+            if (row > seen_by_all && row < valid)
+              v[q] = make_uint4(drop_nans(v[q].x, seen), drop_nans(v[q].y, seen), drop_nans(v[q].z, seen), drop_nans(v[q].w, seen));
+          }
+          if (seen) *const_cast<volatile int*>(&sh->v_nan[seq & 7]) = seq;
+        }
 #pragma unroll
         for (int q = 0; q < 16 / RPL; ++q) {
           const int row = r0 + q * RPL + lane / LPR;
@@ -663,6 +690,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     *abort_flag = 0;
+    for (int i = 0; i < 8; ++i) sh->v_nan[i] = 0;
     for (int i = 0; i < N_BARS; ++i) {
       int count = 1;
       if (i >= B_QFULL && i < B_QFULL + 2) count = 4;
@@ -901,6 +929,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
         }
       }
       if (mine && p.n_splits > 1) p.parts.ml[part] = make_float2(m_used, l_sum);
+      if (mine && *const_cast<volatile int*>(&sh->v_nan[seq & 7]) == seq)
+        put_nans<HD>(p, it.req, it.kvh, max(it.pre + it.t0 + 1, it.jb * TK), min(row_pos, (it.jb + it.n_kv) * TK - 1), p.n_splits == 1 ? p.o + out_row * HD : nullptr, p.parts.o + part * HD);
       __syncwarp();
     }
   }

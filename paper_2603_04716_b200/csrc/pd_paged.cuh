@@ -133,6 +133,21 @@ pd_status launch_paged_tiles(const PagedRuns& r, const PagedParts& parts, cudaSt
 size_t paged_tiles_part_rows();
 int paged_tiles_splits(long long items, int max_kv);  // parts that the key ranges of `items` row blocks are cut into
 
+// A key that some row of a block does not see meets that row with a weight of 0, and 0 * NaN is NaN: V rows of such keys enter
+// the products without their NaN codes, and the rows that do see the key are given their NaN at the end.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t drop_nans(uint32_t codes, bool& seen) {
+  const uint32_t m = nan_bytes(codes);
+  seen |= m != 0;
+  return codes & ~((m >> 7) * 0xffu);
+}
+// V row of a key of the sequence with page table row `table`; NULL: its page number lies outside the pool.
+__device__ __forceinline__ const uint8_t* v_row(const PagedCache& c, const int32_t* table, int n_kv_heads, int kvh, int head_dim, int key) {
+  const int id = table[key >> c.log2_page];
+  if (static_cast<unsigned>(id) >= static_cast<unsigned>(c.n_pages)) return nullptr;
+  return c.v + (((static_cast<size_t>(id) * n_kv_heads + kvh) << c.log2_page) + (key & ((1 << c.log2_page) - 1))) * head_dim;
+}
+
 // Two E4M3 codes (bits 0-15) -> two halves, exactly.
 __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t c) {
   uint32_t r;

@@ -263,6 +263,7 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
     l_sum[c][0] = l_sum[c][1] = 0.f;
   }
   float unit = 0.f;  // o_acc counts in this V scale, the largest so far
+  bool nan_seen = false;
 
   for (int i = 0; i < my_tiles; ++i) {
     const int stage = i % PA_STAGES;
@@ -380,6 +381,15 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
         vw[r][0] = v.x; vw[r][1] = v.y;
       }
     }
+    if (RUNS && key0 + PA_KEYS - 1 > pos0) {  // not every token of the block sees all keys
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (key0 + (r >> 1) * 8 + key_of<HD>(t4 * 2 + (r & 1)) > pos0) {
+#pragma unroll
+          for (int e = 0; e < HD / 32; ++e) vw[r][e] = drop_nans(vw[r][e], nan_seen);
+        }
+      }
+    }
     auto product = [&](auto accumulate) {
 #pragma unroll
       for (int j = 0; j < HD / 32; ++j) {
@@ -435,7 +445,7 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
       }
     }
   }
-  __syncthreads();
+  const bool nans = RUNS ? __syncthreads_or(nan_seen) : (__syncthreads(), false);
   for (int idx = tid; idx < n_cols * HD; idx += PA_THREADS) {
     const int r = idx / HD, d = idx - r * HD;
     float m = -CUDART_INF_F;
@@ -451,6 +461,12 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
       o += src[d] * f;
     }
     const size_t row = out_row(r);
+    if (RUNS && nans) {
+      for (int key = max(pos0 + 1, k_begin); key <= min(pos0 + token_of(r), k_end - 1); ++key) {
+        const uint8_t* v = v_row(a.c, table, a.n_kv_heads, kvh, HD, key);
+        if (v && (v[d] & 0x7f) == 0x7f) o = CUDART_NAN_F;
+      }
+    }
     if (a.n_splits == 1) {
       a.o[row * HD + d] = __float2bfloat16(l == 0.f ? 0.f : o / l);  // (no visible entry: zeros)
     } else {

@@ -310,3 +310,29 @@ def test_prefill_nan_key_at_every_position(pdlib):
         sees = np.arange(new) + prefix >= key
         assert np.isnan(got[sees][:, 4:]).all(), key
         assert np.isfinite(got[:, :4]).all() and np.isfinite(got[~sees]).all(), key
+
+
+@pytest.mark.parametrize("hq,hkv,hd,new,prefix", [(8, 2, 64, [40, 3, 16], [120, 0, 37]), (32, 8, 128, [70, 1, 130], [0, 5, 300]),
+                                                  (4, 4, 128, [4, 2, 1], [500, 30, 0])])
+def test_prefill_nan_value_reaches_only_the_rows_that_see_it(pdlib, hq, hkv, hd, new, prefix):
+    """NaN entries of V make their feature NaN in the rows that see the key; a row before it is left alone, although it shares
+    a tile with the key (its weight there is 0)."""
+    c = Cache(pdlib, hkv, hd, 32, [a + b for a, b in zip(new, prefix)], seed=hd + hq)
+    c.fill([a + b for a, b in zip(new, prefix)], np.random.default_rng(hd), 0.5)
+    clean = c.v.copy()
+    q = gen.normal_bf16(92, gen.S_X, (sum(new), hq, hd), 1.0, sub=hq)
+    want = np.asarray(prefill(pdlib, c.upload(), hq, q, new, prefix), dtype=np.float64).reshape(sum(new), hq, hd)
+    start = np.cumsum([0] + new)
+    for step in (1, 5, 29):
+        c.v = clean.copy()
+        bad = np.zeros((sum(new), hq, hd), bool)
+        for s, (n, pre) in enumerate(zip(new, prefix)):
+            for i, key in enumerate(range(pre + n - 1, max(pre - 20, -1), -step)):
+                head, d = i % hkv, (7 * i + 3) % hd
+                c.v[c.table[s][key // 32], head, key % 32, d] = 0xFF if i % 2 else 0x7F
+                rows = start[s] + np.arange(n)[pre + np.arange(n) >= key]
+                bad[np.ix_(rows, np.arange(head * hq // hkv, (head + 1) * hq // hkv), [d])] = True
+        c.upload()
+        got = np.asarray(prefill(pdlib, c, hq, q, new, prefix), dtype=np.float64).reshape(sum(new), hq, hd)
+        np.testing.assert_array_equal(np.isnan(got), bad)
+        np.testing.assert_array_equal(got[~bad], want[~bad])
