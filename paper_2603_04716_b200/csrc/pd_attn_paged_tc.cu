@@ -13,8 +13,9 @@
 //     two octaves to spare when it does), and O is rescaled when it grows; a page's scale relative to it multiplies the
 //     codes, exact down to 2^-15 of the unit.  p is kept as 2^7 p; the row reference of the exponent may lag the maximum by
 //     2^8.  There is no decoded copy of the cache in global memory.
-//   * When there are fewer items than SMs, the key range of every item is cut into equal parts, the parts write
-//     unnormalised fp32 rows with their maximum and sum, and a second kernel joins them.
+//   * When there are fewer items than SMs, or few left over behind the last full turn of the SMs, key ranges are cut into
+//     equal parts (paged_tiles_plan); the parts write unnormalised fp32 rows with their maximum and sum, and a second kernel
+//     joins them.
 //   * Items are handed out by the hardware: the grid has one block per item, a resident block that is done takes over the
 //     next block that has not been started (clusterlaunchcontrol), so there is no counter in memory to share or to reset.
 //   * S, P and both products advance by half a key tile: S of a half is written over the P that a product has just consumed,
@@ -36,6 +37,9 @@
 // Every wait is wall-clock bounded and leaves through the common teardown.
 #include <math_constants.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include "pd_paged.cuh"
 
 namespace pd {
@@ -52,7 +56,8 @@ constexpr float P_SHIFT = 7.f;             // p is kept as 2^7 p: at most 2^15, 
 constexpr int K_SLOTS = 4, V_SLOTS = 2, R_SLOTS = 2, ITEM_SLOTS = 4, INFO_SLOTS = 8;
 constexpr int kNoPage = static_cast<int>(0x80000000u);  // beyond the keys of a tile
 constexpr int kNoRows = -1000;
-constexpr int MAX_SPLIT_ITEMS = 148;       // parts of items while there are splits (sizes the workspace)
+constexpr int SMS = 148;
+constexpr int MAX_PARTS = 2 * SMS;         // parts of key ranges that a call may have (sizes the workspace)
 
 template <int HD>
 struct Cfg {
@@ -82,19 +87,22 @@ struct PagedPrefillDev {
   bf16* o;
   const int32_t* cu_seqlens;
   const int32_t* prefix;
-  PagedParts parts;        // used when n_splits > 1
+  PagedParts parts;        // used when split_slots > 0
   int* err_word;
   PagedCache c;
   int ldq, n_req, n_tokens, n_q_heads, n_kv_heads;
   int tile_tokens;         // tokens of a row tile: 128 / group
-  int n_slots, n_splits;   // items = n_slots x n_splits x n_kv_heads
+  int n_slots;             // blocks of tokens
+  int split_slots, n_splits;  // of these, the first split_slots are n_splits items per KV head, the others one
+  long long part_rows;     // (token, head) rows of the split ones
   unsigned long long wait_limit_ns;
   int test_skip_arrive;    // test hook: the second V warp leaves out one arrival
 };
 
 // A work item as warp 0 publishes it.
 struct Item {
-  int kvh, start, len, t0, pre, req, jb, split;
+  int kvh, start, len, t0, pre, req, jb;
+  int split;      // part of the key range; -1: the whole
   int n_kv;       // key tiles; -1: no more items
   int halves[2];  // half key tiles that a row tile works on
 };
@@ -192,22 +200,28 @@ __device__ __forceinline__ uint64_t code_desc(uint32_t addr) {
 }
 
 // ------------------------------------------------------------------------------------------------ items
-// Item `idx` of the grid: KV head fastest, then the part of the key range, then slots from the last one down (of a request
-// the rows with the longest key ranges come first).  All lanes of a warp call; false: nothing to do.
+// Item `idx` of the grid: KV head fastest, then the part of the key range where it is cut, then slots from the last one down
+// (of a request the rows with the longest key ranges come first).  All lanes of a warp call; false: nothing to do.
 __device__ __forceinline__ bool decode_item(const PagedPrefillDev& p, int idx, Item& it) {
-  const int tb = 2 * p.tile_tokens;
-  const int per_slot = p.n_kv_heads * p.n_splits;
-  const int rest = idx % per_slot;
-  const TokenBlock b = find_block(p.cu_seqlens, p.prefix, p.n_req, p.n_tokens, p.n_slots - 1 - idx / per_slot, tb);
-  it.kvh = rest % p.n_kv_heads;
-  it.split = rest / p.n_kv_heads;
+  const int tb = 2 * p.tile_tokens, whole = (p.n_slots - p.split_slots) * p.n_kv_heads;
+  int slot;
+  if (idx < whole) {
+    slot = p.n_slots - 1 - idx / p.n_kv_heads;
+    it.split = -1;
+  } else {
+    const int per_slot = p.n_kv_heads * p.n_splits;
+    slot = p.split_slots - 1 - (idx - whole) / per_slot;
+    it.split = (idx - whole) % per_slot / p.n_kv_heads;
+  }
+  it.kvh = (idx < whole ? idx : idx - whole) % p.n_kv_heads;
+  const TokenBlock b = find_block(p.cu_seqlens, p.prefix, p.n_req, p.n_tokens, slot, tb);
   it.req = b.req; it.start = b.start; it.len = b.len; it.pre = b.pre; it.t0 = b.t0;
   if (it.t0 >= it.len) return false;
   const int h0 = (it.pre + min(it.len, it.t0 + p.tile_tokens) + TH - 1) / TH;
   const int h1 = it.t0 + p.tile_tokens < it.len ? (it.pre + min(it.len, it.t0 + tb) + TH - 1) / TH : 0;
   const int n_all = (max(h0, h1) + 1) / 2;
-  it.jb = static_cast<int>(1ll * n_all * it.split / p.n_splits);
-  const int je = static_cast<int>(1ll * n_all * (it.split + 1) / p.n_splits);
+  it.jb = it.split < 0 ? 0 : static_cast<int>(1ll * n_all * it.split / p.n_splits);
+  const int je = it.split < 0 ? n_all : static_cast<int>(1ll * n_all * (it.split + 1) / p.n_splits);
   it.n_kv = je - it.jb;
   it.halves[0] = max(0, min(h0, 2 * je) - 2 * it.jb);
   it.halves[1] = max(0, min(h1, 2 * je) - 2 * it.jb);
@@ -761,8 +775,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
       const bool mine = row < tile_rows(p, it, t, group);
       const size_t out_row = static_cast<size_t>(it.start + token0 + row_token) * p.n_q_heads + it.kvh * group + row_head;
       if (nh == 0) {  // no rows, or no keys in this part of the range
-        if (p.n_splits > 1 && mine)
-          p.parts.ml[static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row] = make_float2(-CUDART_INF_F, 0.f);
+        if (it.split >= 0 && mine)
+          p.parts.ml[it.split * p.part_rows + out_row] = make_float2(-CUDART_INF_F, 0.f);
         continue;
       }
       const int row_pos = it.pre + token0 + row_token;  // last key the row may see
@@ -894,7 +908,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
       ptx::tc_fence_after();
       // o = O 2^(v_exp) / (sum of 2^7 p); the two factors apart, so that neither leaves the normal range
       const float unit = exp2_int(v_exp), inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
-      const size_t part = static_cast<size_t>(it.split) * p.n_tokens * p.n_q_heads + out_row;
+      const size_t part = max(it.split, 0) * p.part_rows + out_row;
 #pragma unroll 1
       for (int c0 = 0; c0 < HD; c0 += 64) {
         uint32_t ov[2][32];
@@ -906,7 +920,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar(B_OREAD + t));
         }
-        if (mine && p.n_splits == 1) {
+        if (mine && it.split < 0) {
           bf16* dst = p.o + out_row * HD + c0;
           // a thread owns a row, so every store of a warp touches 32 different lines: 32-byte stores halve their number
 #pragma unroll
@@ -928,9 +942,9 @@ __global__ void __launch_bounds__(THREADS, 1) paged_prefill_kernel(const __grid_
           }
         }
       }
-      if (mine && p.n_splits > 1) p.parts.ml[part] = make_float2(m_used, l_sum);
+      if (mine && it.split >= 0) p.parts.ml[part] = make_float2(m_used, l_sum);
       if (mine && *const_cast<volatile int*>(&sh->v_nan[seq & 7]) == seq)
-        put_nans<HD>(p, it.req, it.kvh, max(it.pre + it.t0 + 1, it.jb * TK), min(row_pos, (it.jb + it.n_kv) * TK - 1), p.n_splits == 1 ? p.o + out_row * HD : nullptr, p.parts.o + part * HD);
+        put_nans<HD>(p, it.req, it.kvh, max(it.pre + it.t0 + 1, it.jb * TK), min(row_pos, (it.jb + it.n_kv) * TK - 1), it.split < 0 ? p.o + out_row * HD : nullptr, p.parts.o + part * HD);
       __syncwarp();
     }
   }
@@ -956,32 +970,61 @@ pd_status launch(const PagedPrefillDev& p, long long items, cudaStream_t s) {
   PD_TRY(make_tmap_u8(&tv, p.c.v, rows, HD, HD, 1u << p.c.log2_page, 0));
   PD_CUDA_TRY(launch_pdl(paged_prefill_kernel<HD>, dim3(static_cast<unsigned>(items)), dim3(THREADS), Cfg<HD>::SMEM_BYTES, s, tq, tk, tv, p));
   count_launch();
-  if (p.n_splits > 1) return launch_paged_join(p.parts, p.o, 1ll * p.n_tokens * p.n_q_heads, p.n_splits, HD, s);
+  if (p.split_slots > 0) return launch_paged_join(p.parts, p.o, p.part_rows, p.n_splits, HD, s);
   return PD_OK;
 }
 
 }  // namespace
 
-size_t paged_tiles_part_rows() { return static_cast<size_t>(MAX_SPLIT_ITEMS) * 2 * TQ; }
+size_t paged_tiles_part_rows() { return static_cast<size_t>(MAX_PARTS) * 2 * TQ; }
 
-// Key ranges are cut while the parts still fit the SMs together, into parts of at least two key tiles.
-int paged_tiles_splits(long long items, int max_kv) {
-  long long want = MAX_SPLIT_ITEMS / items;
-  const long long most = (max_kv + TK - 1) / TK / 2;
-  if (want > most) want = most;
-  return want > 1 ? static_cast<int>(want) : 1;
+// Up to half as many items as SMs: every key range is cut, as often as the parts still fit the SMs together, into parts of at
+// least two key tiles.  Otherwise the items that are left over when every SM has had the same number may be cut in two to four:
+// items of equal length would leave most SMs idle behind the last full turn.  It is done where the time saved (2.35 us a key
+// tile, 0.7 of it for heads of 64) exceeds that of writing and joining the parts: 4 x 1000 tokens over 5000 keys 390 -> 381 us.
+PagedTilesPlan paged_tiles_plan(const PagedRuns& r, const int32_t* cu, const int32_t* prefix) {
+  const int group = r.n_q_heads / r.n_kv_heads, tb = 2 * (TQ / group);
+  const long long items = r.tile_blocks * r.n_kv_heads, all_rows = 1ll * r.n_tokens * r.n_q_heads;
+  const PagedTilesPlan uncut{0, 1, 0};
+  if (items <= SMS / 2) {
+    const int want = static_cast<int>(std::min<long long>(SMS / items, (r.max_kv + TK - 1) / TK / 2));
+    return want > 1 ? PagedTilesPlan{first_slot(r.n_tokens, r.n_req, tb), want, all_rows} : uncut;
+  }
+  int blocks = static_cast<int>((items % SMS + r.n_kv_heads - 1) / r.n_kv_heads);  // per KV head
+  if (blocks == 0) return uncut;
+  const double cut_items = 1.0 * blocks * r.n_kv_heads;
+  PagedTilesPlan plan = uncut;
+  int steps = 0;  // key tiles of the longest of them
+  for (int i = 0; i < r.n_req && blocks > 0; ++i) {
+    const int len = cu[i + 1] - cu[i], pre = prefix ? prefix[i] : 0, take = std::min(blocks, (len + tb - 1) / tb);
+    if (take == 0) continue;
+    const int tokens = std::min(len, take * tb);
+    steps = std::max(steps, (pre + tokens + TK - 1) / TK);
+    plan.split_slots = first_slot(cu[i], i, tb) + take;
+    plan.part_rows = 1ll * (cu[i] + tokens) * r.n_q_heads;
+    blocks -= take;
+  }
+  const double step_us = r.head_dim == 128 ? 2.35 : 1.65;
+  double best = 0;
+  for (int k = 2; k <= 4; ++k) {
+    if (cut_items * k > MAX_PARTS || steps / k < 4) continue;
+    const double saved = (1 - std::ceil(cut_items * k / SMS) / k) * steps * step_us;
+    const double gain = saved - 6 - cut_items * 2 * TQ * k * r.head_dim * 8 / 4e6;
+    if (gain > best) { best = gain; plan.n_splits = k; }
+  }
+  return plan.n_splits > 1 ? plan : uncut;
 }
 
-pd_status launch_paged_tiles(const PagedRuns& r, const PagedParts& parts, cudaStream_t s) {
+pd_status launch_paged_tiles(const PagedRuns& r, const PagedTilesPlan& plan, const PagedParts& parts, cudaStream_t s) {
   // rows of K are addressed with 32-bit numbers
   if ((static_cast<long long>(r.c.n_pages) * r.n_kv_heads << r.c.log2_page) > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
   PagedPrefillDev p{};
   p.q = r.q; p.o = r.o; p.cu_seqlens = r.cu_seqlens; p.prefix = r.prefix; p.parts = parts; p.err_word = r.err_word; p.c = r.c;
   p.ldq = r.ldq; p.n_req = r.n_req; p.n_tokens = r.n_tokens; p.n_q_heads = r.n_q_heads; p.n_kv_heads = r.n_kv_heads;
   p.tile_tokens = TQ / (r.n_q_heads / r.n_kv_heads);
-  p.n_splits = paged_tiles_splits(r.tile_blocks * r.n_kv_heads, r.max_kv);
+  p.split_slots = plan.split_slots; p.n_splits = plan.n_splits; p.part_rows = plan.part_rows;
   p.n_slots = first_slot(r.n_tokens, r.n_req, 2 * p.tile_tokens);
-  const long long items = 1ll * p.n_slots * p.n_splits * r.n_kv_heads;
+  const long long items = (p.n_slots + 1ll * p.split_slots * (p.n_splits - 1)) * r.n_kv_heads;
   if (items > 0x3fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
   p.wait_limit_ns = 4000000000ull;
   {

@@ -128,10 +128,15 @@ pd_status launch_paged_join(const PagedParts& parts, bf16* o, long long rows, in
 int paged_rows_block(int group, int longest_run);
 pd_status launch_paged_rows(const PagedRuns& r, int longest_run, const PagedParts& parts, cudaStream_t s);
 size_t paged_rows_part_rows();  // rows of partial results that the launch may need
-// The tensor-memory kernel.
-pd_status launch_paged_tiles(const PagedRuns& r, const PagedParts& parts, cudaStream_t s);
+// The tensor-memory kernel.  The rows of the first split_slots blocks of tokens (all of them, or as many as are left when the
+// SMs have had their last full turn) have their key range cut into n_splits parts.
+struct PagedTilesPlan {
+  int split_slots, n_splits;
+  long long part_rows;  // (token, head) rows of those blocks, the first of the call
+};
+PagedTilesPlan paged_tiles_plan(const PagedRuns& r, const int32_t* cu_host, const int32_t* prefix_host);
+pd_status launch_paged_tiles(const PagedRuns& r, const PagedTilesPlan& plan, const PagedParts& parts, cudaStream_t s);
 size_t paged_tiles_part_rows();
-int paged_tiles_splits(long long items, int max_kv);  // parts that the key ranges of `items` row blocks are cut into
 
 // A key that some row of a block does not see meets that row with a weight of 0, and 0 * NaN is NaN: V rows of such keys enter
 // the products without their NaN codes, and the rows that do see the key are given their NaN at the end.

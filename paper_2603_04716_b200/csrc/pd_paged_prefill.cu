@@ -21,7 +21,7 @@ namespace {
 // at 8 x 1000; its copy of n_req * max_kv_len rows was the price.)
 enum class Path { ROWS, TILES };
 
-Path choose_path(const PagedRuns& r, const int32_t* cu, const int32_t* prefix, int longest) {
+Path choose_path(const PagedRuns& r, const PagedTilesPlan& plan, const int32_t* cu, const int32_t* prefix, int longest) {
   const int group = r.n_q_heads / r.n_kv_heads;
   const int row_tokens = paged_rows_block(group, longest), tile_tokens = 2 * (128 / group);
   double rows_steps = 0, tile_steps = 0;  // 16 keys of a row block; 128 keys of a tile block
@@ -37,7 +37,7 @@ Path choose_path(const PagedRuns& r, const int32_t* cu, const int32_t* prefix, i
     tile_steps += r.n_kv_heads * steps(len, pre, tile_tokens, 128);
   }
   const double sms = 148, hd = r.head_dim == 128 ? 1.0 : 0.7, items = static_cast<double>(r.tile_blocks) * r.n_kv_heads;
-  const double splits = paged_tiles_splits(r.tile_blocks * r.n_kv_heads, r.max_kv);
+  const double splits = plan.part_rows == 1ll * r.n_tokens * r.n_q_heads ? plan.n_splits : 1;  // (of all key ranges)
   const double t_rows = 8 + 0.9e-3 * std::fmin(rows_steps, 8000) + 0.85e-3 * std::fmax(rows_steps - 8000, 0);
   const double tile_step = 1.0 * longest * group <= 128 ? 2.0 : 2.35;  // one row tile of a block in use, or both
   const double t_tiles = 11 + hd * tile_step * std::fmax(tile_steps / sms, std::ceil(r.max_kv / 128.0) / splits) + 2.5 * items * splits / sms +
@@ -108,10 +108,11 @@ extern "C" pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const v
   for (int i = 0; i < n_req; ++i) r.tile_blocks += (cu_host[i + 1] - cu_host[i] + tile_tokens - 1) / tile_tokens;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_ATTN_PREFILL, st);
-  const Path path = choose_path(r, cu_host, prefix_host, longest);
+  const PagedTilesPlan plan = paged_tiles_plan(r, cu_host, prefix_host);
+  const Path path = choose_path(r, plan, cu_host, prefix_host, longest);
   const size_t part_rows = path == Path::ROWS ? paged_rows_part_rows() : paged_tiles_part_rows();
   PagedParts parts;
   parts.o = static_cast<float*>(workspace);
   parts.ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + paged_parts_ml_offset(part_rows, cfg->head_dim));
-  return path == Path::ROWS ? launch_paged_rows(r, longest, parts, st) : launch_paged_tiles(r, parts, st);
+  return path == Path::ROWS ? launch_paged_rows(r, longest, parts, st) : launch_paged_tiles(r, plan, parts, st);
 }

@@ -111,3 +111,19 @@ def test_gradually_growing_values_lose_nothing(pdlib):
     want = rows[:, 2 + hkv:]
     step = ap.c.vs[ap.c.table[0, 0]][:, None] * 2.0 ** -9
     assert np.all(np.abs(got - want) <= 2.0 ** -4 * np.abs(want) + step)
+
+
+@pytest.mark.parametrize("hq,hkv,hd,new,prefix", [
+    (16, 8, 128, [1400], [3500]),                         # 88 blocks of rows and heads for 148 SMs: all cut
+    (16, 8, 64, [2600], [1900]),                          # 168: the first three blocks of tokens cut
+    (16, 8, 128, [200, 0, 1000, 1500], [3000, 5, 0, 900]),
+    (12, 6, 64, [130, 1, 129, 3000], [2500, 2600, 40, 0])])
+def test_key_ranges_cut_behind_the_last_full_turn(pdlib, hq, hkv, hd, new, prefix):
+    total = [a + b for a, b in zip(new, prefix)]
+    c = Cache(pdlib, hkv, hd, 128, total, seed=hd + len(new))
+    c.fill(total, np.random.default_rng(8), 0.5, pages=1.0)
+    c.upload()
+    q = gen.normal_bf16(97, gen.S_X, (sum(new), hq, hd), 1.0, sub=hd)
+    got = prefill(pdlib, c, hq, q, new, prefix)
+    check_prefill(c, hq, q, new, prefix, got, rows=10)
+    np.testing.assert_array_equal(got, prefill(pdlib, c, hq, q, new, prefix, pad=8))
