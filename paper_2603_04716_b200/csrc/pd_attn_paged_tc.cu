@@ -32,7 +32,7 @@
 // 2150.  So an issuer runs its code as a whole warp (uniform addresses: one lane alone 4 % slower), descriptors are a sum with
 // a constant, and loops that every warp shares the instruction caches with are kept small (roles inlined: 1.4 times the time).
 // (Counters at 4 x 1000 tokens over 5000 keys: tensor pipe 66 % of the cycles, special functions 43 %, issue slots 53 %.)
-// Measured: 37 chunks, 358 Gflop, in 387 us = 0.92 Pflop/s, 55 % of a library product's rate; a prompt of 4096 tokens (137 Gflop)
+// Measured: 37 chunks, 358 Gflop, in 382 us = 0.94 Pflop/s, 56 % of a library product's rate; a prompt of 4096 tokens (137 Gflop)
 // in 159 us, of 8192 in 526 us = 1.05 Pflop/s.
 // Every wait is wall-clock bounded and leaves through the common teardown.
 #include <math_constants.h>
