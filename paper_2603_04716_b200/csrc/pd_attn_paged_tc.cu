@@ -1,16 +1,16 @@
 // Prefill attention over the 8-bit paged KV cache on the 5th-generation tensor cores (tcgen05 + tensor memory).
 //
 // The tile structure is that of pd_attn_prefill_tc.cu: a block works on two row tiles of 128 rows whose softmax and products
-// ping-pong over key tiles of 128, S / P and O live in tensor memory, one thread issues the products.  What differs:
+// ping-pong over key tiles of 128, S / P and O live in tensor memory.  What differs:
 //   * Rows are (token, query head of the group) pairs, the head fastest: a key tile is read and decoded once for all heads
 //     that share it, and a short run of tokens still fills the rows (16 tokens of a group of 8 are one row tile).
 //   * S = Q K^T takes the K codes as they are: a key tile is copied from its pages by TMA and multiplied as E4M3.  q goes in
 //     as the sum of two E4M3 numbers, scaled per row by a power of two to a largest entry in [128, 256): the products are
 //     exact, the second number leaves an error of at most 2^-10, 2^-17 of the row's largest entry.  Two 8-bit products take
 //     the time of one 16-bit product.  The K scales of the pages multiply the scores in the softmax, per 16 keys.
-//   * O += P V has both operands in f16.  V codes come by TMA as well, two warps turn them into f16 operand rows (exact, one
-//     instruction for two codes).  V counts in a unit that only grows over the key tiles of an item (with
-//     two octaves to spare when it does), and O is rescaled when it grows; a page's scale relative to it multiplies the
+//   * O += P V has both operands in f16.  V codes come by TMA as well, four warps turn them into f16 operand rows (exact, one
+//     instruction for two codes).  V counts in a unit that only grows over the key tiles of an item (with two octaves to spare
+//     when it does), and O is rescaled when it grows; a page's scale relative to it multiplies the
 //     codes, exact down to 2^-15 of the unit.  p is kept as 2^7 p; the row reference of the exponent may lag the maximum by
 //     2^8.  There is no decoded copy of the cache in global memory.
 //   * When there are fewer items than SMs, or few left over behind the last full turn of the SMs, key ranges are cut into

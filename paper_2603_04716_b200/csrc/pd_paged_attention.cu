@@ -281,6 +281,18 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
     __syncwarp();
     const uint32_t sk = ring + stage * 2 * SM::TILE, sv = sk + SM::TILE;
     const int key0 = k_begin + (i * PA_WARPS + warp) * PA_KEYS;
+    if (RUNS && key0 + PA_KEYS - 1 > pos0) {  // not every token of the block sees all keys (in place: registers are short)
+#pragma unroll 1
+      for (int o = lane * 16; o < SM::TILE; o += 512) {
+        if (key0 + o / HD <= pos0) continue;
+        const uint4 w = lds128(sv + o);
+        bool seen = false;
+        const uint4 d = make_uint4(drop_nans(w.x, seen), drop_nans(w.y, seen), drop_nans(w.z, seen), drop_nans(w.w, seen));
+        if (seen) asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(sv + o), "r"(d.x), "r"(d.y), "r"(d.z), "r"(d.w) : "memory");
+        nan_seen |= seen;
+      }
+      __syncwarp();
+    }
 
     // ---- S^T = K Q^T: rows are keys key_of(g) and 8 + key_of(g), columns heads
     float st[NC][2][4];
@@ -379,15 +391,6 @@ __global__ void __launch_bounds__(PA_THREADS, WIDE ? 1 : 2) paged_decode_kernel(
       } else {
         const uint2 v = lds64(sv + chunk_off<HD>(row, g >> 1) + (g & 1) * 8);
         vw[r][0] = v.x; vw[r][1] = v.y;
-      }
-    }
-    if (RUNS && key0 + PA_KEYS - 1 > pos0) {  // not every token of the block sees all keys
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (key0 + (r >> 1) * 8 + key_of<HD>(t4 * 2 + (r & 1)) > pos0) {
-#pragma unroll
-          for (int e = 0; e < HD / 32; ++e) vw[r][e] = drop_nans(vw[r][e], nan_seen);
-        }
       }
     }
     auto product = [&](auto accumulate) {
