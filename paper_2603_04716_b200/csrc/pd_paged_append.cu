@@ -118,11 +118,11 @@ __global__ void __launch_bounds__(AD_WARPS * 32) append_decode_kernel(const Appe
   const int pos = a.kv_len[req];
   if (pos < 0) return;  // a padding row of the batch
   const int pi = pos >> a.c.log2_page;
-  if (pos >= a.max_pos || pi >= a.c.table_ld) {
+  if (pos >= a.max_pos) {
     if (lane == 0) report(a.err_word);
     return;
   }
-  const int page = a.c.table[static_cast<size_t>(req) * a.c.table_ld + pi];
+  const int page = pi < a.c.table_ld ? a.c.table[static_cast<size_t>(req) * a.c.table_ld + pi] : -1;
   const bf16* row = a.qkv + static_cast<size_t>(req) * a.ldqkv;
   const float2* rope = a.rope + static_cast<size_t>(pos) * (HD / 2);
   const int j = lane % J;
