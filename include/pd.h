@@ -459,7 +459,7 @@ pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int3
 /* pd_prefill_attention over the 8-bit paged cache: row t of request r is the query at position prefix[r] + t and attends to
  * positions 0 .. prefix[r] + t of page_table row r (its own tokens must have been appended).  Serves whole prompts, chunks of
  * prompts and a few drafted tokens per sequence: one of two kernels is taken from the host lengths (a streaming one for few
- * rows, a tensor-memory one otherwise); they agree within the rounding of the softmax weights to f16 and of the result.
+ * rows, a tensor-memory one otherwise); they agree within the roundings below and that of the result.
  *   q, out        as for pd_prefill_attention (q 16-byte aligned, out 32-byte aligned)
  *   cu_seqlens    device and host copy;  prefix  device and host copy, both or neither (NULL = 0)
  *   workspace     at least pd_paged_prefill_attention_workspace_bytes() bytes for the longest prefix[r] + len_r, 256-byte
@@ -468,8 +468,11 @@ pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int3
  *                 of that request is then not meaningful, that of the others is)
  * A NaN in a cached row of k makes the rows that see it NaN, one in v their values of that feature; rows before it are not
  * touched.
- * Page scales within a sequence may differ by 2^15 without loss; V values of pages further below the largest lose low bits
- * first.  Only enqueues work. */
+ * Roundings, of this call and of pd_paged_decode_attention: a weight of the softmax is off by 2^-11 of itself, or by 2^-32 of its
+ * row's largest where that is more (2^-22 on a page whose V scale is 1 / 2 to 1 / 1024 of the largest of the sequence).  V is exact
+ * while the page scales of a sequence lie within 2^110 of each other, whatever the pages weigh.  q is exact down to 2^-24
+ * of its row's largest entry in the streaming kernel and down to 2^-17 of it in the tensor-memory kernel.  Sums are fp32.
+ * Only enqueues work. */
 pd_status pd_paged_prefill_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t n_req, int32_t max_kv_len,
                                                      size_t* out_bytes);
 pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const void* q, int32_t ldq, void* out,
