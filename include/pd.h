@@ -440,7 +440,7 @@ pd_status pd_paged_kv_append(const pd_layer_cfg* cfg, const void* qkv, int32_t l
                              const int32_t* kv_len_dev, const pd_paged_kv_cache* cache, int32_t* err_word, void* stream);
 
 /* pd_decode_attention over the 8-bit paged cache: sequence b attends to entries 0 .. kv_len[b] of page_table row b.
- *   q, out        device bf16 [B, ldq] / [B, Hq*hd], q 16-byte aligned, ldq a multiple of 8
+ *   q, out        device bf16 [B, ldq] / [B, Hq*hd], q 16-byte aligned, out only as its elements are, ldq a multiple of 8
  *   kv_len_dev    device int32[B]; a sequence with kv_len[b] < 0 gets an all-zero row; entries beyond the table are left out
  *   max_kv_len    host upper bound of kv_len[b] + 1, at most table_ld * page_len (it sizes the split of the key range; a
  *                 longer sequence is still computed whole)

@@ -606,7 +606,9 @@ Split decode_split(int batch, int n_kv_heads, int max_kv_len) {
 
 pd_status launch_paged_join(const PagedParts& parts, bf16* o, long long rows, int n_splits, int head_dim, cudaStream_t s) {
   if (rows > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
-  const bool few = n_splits <= PJ_PARTS && rows > 2048;  // (blocks enough for the whole GPU either way)
+  // (blocks enough for the whole GPU either way; a warp per row stores pairs of values, so a result that starts between two
+  // 4-byte words takes the other form, which stores single ones)
+  const bool few = n_splits <= PJ_PARTS && rows > 2048 && (reinterpret_cast<uintptr_t>(o) & 3u) == 0;
   const dim3 grid(static_cast<unsigned>(few ? (rows + PJ_WARPS - 1) / PJ_WARPS : rows)), block(PJ_WARPS * 32);
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, s, parts, o, rows, n_splits); };
   PD_CUDA_TRY(head_dim == 128 ? (few ? go(paged_join_kernel<128, 1>) : go(paged_join_kernel<128, 4>))

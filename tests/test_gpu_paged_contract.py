@@ -2,10 +2,12 @@
 import numpy as np
 import pytest
 
-from gpu_util import from_dev
+import pd_inputs as gen
+from gpu_util import empty_bf16, from_dev, i32_dev, to_dev
 from oracle import paged
-from paged_util import BF16
+from paged_util import BF16, Cache
 from test_gpu_paged_append import THETA, Appender, qkv_rows
+from test_gpu_paged_attention import check_decode, decode
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +28,34 @@ def test_append_beyond_the_table_still_writes_q(pdlib, hq, hkv, hd, runs):
     half = np.abs(rows[:, :hq, :hd // 2]) + np.abs(rows[:, :hq, hd // 2:])
     bound = BF16 * np.abs(ref) + 2.0 ** -21 * np.concatenate([half, half], -1)
     assert np.all(np.abs(from_dev(q[:3]).reshape(ref.shape) - ref) <= bound)
+
+
+@pytest.mark.parametrize("hq,hkv,hd,page_len,batch,max_kv,launches", [
+    (16, 1, 128, 16, 130, 600, 2),      # two parts of 2080 rows: the join with a warp per row
+    (64, 8, 64, 32, 33, 8192, 2),       # the same, parts cut for the length bound
+    (32, 8, 128, 64, 2, 1500, 2),       # few rows: the join with a block per row
+    (32, 8, 128, 64, 40, 250, 1)])      # one part
+def test_decode_result_at_any_address(pdlib, hq, hkv, hd, page_len, batch, max_kv, launches):
+    """`out` starts between two 4-byte words: the same bits as at an aligned address, and nothing in front of it or behind."""
+    import torch
+    rng = np.random.default_rng(batch)
+    kv_len = [int(v) for v in rng.integers(-1, min(max_kv, 400), batch)]
+    c = Cache(pdlib, hkv, hd, page_len, [n + 1 for n in kv_len], seed=batch, extra_cols=max_kv // page_len + 1)
+    c.fill([n + 1 for n in kv_len], rng, 0.5)
+    c.upload()
+    q = gen.normal_bf16(103, gen.S_X, (batch, hq, hd), 1.0, sub=batch)
+    want = decode(pdlib, c, hq, q, kv_len, max_kv=max_kv)
+    check_decode(c, hq, q[:9], kv_len[:9], want)
+    cfg = pdlib.LayerConfig(hq * hd, hq, hkv, hd, 64)
+    need = pdlib.pd_paged_decode_attention_workspace_bytes(cfg, batch, max_kv)
+    ws = torch.empty(max(256, need), dtype=torch.uint8, device="cuda")
+    for shift in (1, 2, 3):
+        buf = empty_bf16(batch * hq * hd + 8)
+        out = buf[shift:shift + batch * hq * hd]
+        assert out.data_ptr() % 8 == 2 * shift
+        before = pdlib.pd_launch_count()
+        pdlib.pd_paged_decode_attention(cfg, to_dev(q.reshape(batch, -1)), hq * hd, out, i32_dev(kv_len), batch, max_kv, c.struct, ws, need)
+        torch.cuda.synchronize()
+        assert pdlib.pd_launch_count() - before == launches
+        np.testing.assert_array_equal(from_dev(out).reshape(want.shape), want)
+        assert not buf[:shift].any() and not buf[shift + batch * hq * hd:].any()
