@@ -445,7 +445,8 @@ pd_status pd_paged_kv_append(const pd_layer_cfg* cfg, const void* qkv, int32_t l
  *   max_kv_len    host upper bound of kv_len[b] + 1, at most table_ld * page_len (it sizes the split of the key range; a
  *                 longer sequence is still computed whole)
  *   workspace     at least pd_paged_decode_attention_workspace_bytes() bytes, 256-byte aligned (may be NULL where that is
- *                 0); calls that can overlap on the GPU, captured graphs included, need one each
+ *                 0); what is asked for the largest B and max_kv_len serves every smaller call; calls that can overlap on
+ *                 the GPU, captured graphs included, need one each
  *   err_word      optional device int32, set to 2 where kv_len reaches past the table or a page number lies outside the
  *                 pool (the keys of such a page are left out)
  * Only the head counts and head_dim of cfg are used.  Only enqueues work. */

@@ -602,6 +602,18 @@ Split decode_split(int batch, int n_kv_heads, int max_kv_len) {
                     batch > 1 ? std::max(4096, max_kv_len / 16) : max_kv_len);
 }
 
+// (part, sequence) pairs that any call of up to `batch` sequences and a bound of up to max_kv_len has at most, where it has
+// parts at all: a buffer of that size serves every smaller call, too.  Parts made to fill the GPU are at most as many as
+// decode_split asks for, of at least PA_MIN_CHUNK keys; parts made for their length are as many as the bound allows.
+long long decode_most_parts(int batch, int n_kv_heads, int max_kv_len) {
+  if (batch <= 0 || max_kv_len <= PA_MIN_CHUNK) return 0;
+  const long long fill = (1ll * batch * n_kv_heads <= 148 ? PA_RESIDENT : PA_RESIDENT * 3 / 2) / n_kv_heads;
+  const long long most = std::min(fill, 1ll * batch * ((max_kv_len + PA_MIN_CHUNK - 1) / PA_MIN_CHUNK));
+  // (17: of max_kv_len / 16 keys, rounded down, and what is left)
+  const long long length = batch > 1 ? std::min(17, (max_kv_len + 4095) / 4096) : 1;
+  return std::max(most > 1 ? most : 0, length > 1 ? length * batch : 0);
+}
+
 }  // namespace
 
 pd_status launch_paged_join(const PagedParts& parts, bf16* o, long long rows, int n_splits, int head_dim, cudaStream_t s) {
@@ -642,8 +654,8 @@ extern "C" pd_status pd_paged_decode_attention_workspace_bytes(const pd_layer_cf
                                                                size_t* out_bytes) {
   PD_TRY(pd::check_paged_heads(cfg));
   if (!out_bytes || B < 0 || max_kv_len < 0) return PD_ERR_INVALID_ARG;
-  const int splits = pd::decode_split(B, cfg->n_kv_heads, max_kv_len).n;
-  *out_bytes = splits > 1 ? pd::paged_parts_bytes(static_cast<size_t>(splits) * B * cfg->n_q_heads, cfg->head_dim) : 0;
+  const long long parts = pd::decode_most_parts(B, cfg->n_kv_heads, max_kv_len);
+  *out_bytes = parts ? pd::paged_parts_bytes(static_cast<size_t>(parts) * cfg->n_q_heads, cfg->head_dim) : 0;
   return PD_OK;
 }
 
