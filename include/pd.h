@@ -428,7 +428,7 @@ pd_status pd_rope_table(const pd_layer_cfg* cfg, float* table_host);
  *   cu_seqlens   as for pd_prefill_layer (device and host copy); both NULL: one row per request (a decode step)
  *   kv_len_dev   device int32[n_req]: tokens that sequence r holds already; its rows take positions kv_len[r],
  *                kv_len[r] + 1, ...  A negative value leaves the request out (padding of a captured batch): none of its rows
- *                is read, written or cached.  kv_len itself is not modified.
+ *                is read, written or cached.  kv_len itself is not modified.  n_req at most 2^20 with cu_seqlens
  *   err_word     optional device int32, set to 2 where a row has no place: a position beyond the table, or a page
  *                number outside the pool (q is still written, k and v are left out); a position beyond max_pos (the row is left out)
  * k is rotated in fp32 and rounded once, to its code.  An infinite or NaN element is stored as NaN and takes no part in
@@ -442,6 +442,7 @@ pd_status pd_paged_kv_append(const pd_layer_cfg* cfg, const void* qkv, int32_t l
 /* pd_decode_attention over the 8-bit paged cache: sequence b attends to entries 0 .. kv_len[b] of page_table row b.
  *   q, out        device bf16 [B, ldq] / [B, Hq*hd], q 16-byte aligned, out only as its elements are, ldq a multiple of 8
  *   kv_len_dev    device int32[B]; a sequence with kv_len[b] < 0 gets an all-zero row; entries beyond the table are left out
+ *   B             at most 65535
  *   max_kv_len    host upper bound of kv_len[b] + 1, at most table_ld * page_len (it sizes the split of the key range; a
  *                 longer sequence is still computed whole)
  *   workspace     at least pd_paged_decode_attention_workspace_bytes() bytes, 256-byte aligned (may be NULL where that is
@@ -462,7 +463,9 @@ pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int3
  * prompts and a few drafted tokens per sequence: one of two kernels is taken from the host lengths (a streaming one for few
  * rows, a tensor-memory one otherwise); they agree within the roundings below and that of the result.
  *   q, out        as for pd_prefill_attention (q 16-byte aligned, out 32-byte aligned)
- *   cu_seqlens    device and host copy;  prefix  device and host copy, both or neither (NULL = 0)
+ *   cu_seqlens    device and host copy;  prefix  device and host copy, both or neither (NULL = 0); at most 4095 requests.  A
+ *                 request that brings no row may have any prefix (the -1 of a padded batch, say); with rows a negative
+ *                 one is refused, as is one whose rows reach past the table
  *   workspace     at least pd_paged_prefill_attention_workspace_bytes() bytes for the longest prefix[r] + len_r, 256-byte
  *                 aligned, not shared by calls that can overlap on the GPU
  *   err_word      optional device int32: 1 if a bounded wait gave up, 2 if a page number lies outside the pool (the output

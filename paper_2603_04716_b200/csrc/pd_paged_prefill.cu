@@ -88,9 +88,11 @@ extern "C" pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const v
   for (int i = 0; i < n_req; ++i) {
     const long long len = 1ll * cu_host[i + 1] - cu_host[i];
     const int pre = prefix_host ? prefix_host[i] : 0;
-    if (len < 0 || pre < 0 || pre + len > cap) return PD_ERR_INVALID_ARG;
+    if (len < 0) return PD_ERR_INVALID_ARG;
+    if (len == 0) continue;  // (its prefix plays no role)
+    if (pre < 0 || pre + len > cap) return PD_ERR_INVALID_ARG;
     if (len > longest) longest = static_cast<int>(len);
-    if (len > 0 && pre + len > r.max_kv) r.max_kv = static_cast<int>(pre + len);
+    if (pre + len > r.max_kv) r.max_kv = static_cast<int>(pre + len);
   }
   r.n_tokens = cu_host[n_req];
   if (r.n_tokens == 0) return PD_OK;

@@ -7,7 +7,7 @@ from gpu_util import empty_bf16, from_dev, i32_dev, to_dev
 from oracle import paged
 from paged_util import BF16, Cache
 from test_gpu_paged_append import THETA, Appender, qkv_rows
-from test_gpu_paged_attention import check_decode, decode
+from test_gpu_paged_attention import check_decode, check_prefill, decode, prefill
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +59,17 @@ def test_decode_result_at_any_address(pdlib, hq, hkv, hd, page_len, batch, max_k
         assert pdlib.pd_launch_count() - before == launches
         np.testing.assert_array_equal(from_dev(out).reshape(want.shape), want)
         assert not buf[:shift].any() and not buf[shift + batch * hq * hd:].any()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,new,prefix", [(8, 2, 64, [0, 3, 0, 2], [-1, 40, -1, 0]), (32, 8, 128, [0, 70, 0, 130, 0], [-7, 100, -1, 5, 1 << 30])])
+def test_prefill_of_a_padded_batch(pdlib, hq, hkv, hd, new, prefix):
+    """Requests without rows may have any prefix: the others get what they get without them."""
+    rng = np.random.default_rng(hd)
+    total = [a + b if a else 1 for a, b in zip(new, prefix)]
+    c = Cache(pdlib, hkv, hd, 32, total, seed=hd)
+    c.fill(total, rng, 0.5)
+    c.upload()
+    q = gen.normal_bf16(104, gen.S_X, (sum(new), hq, hd), 1.0, sub=hd)
+    got = prefill(pdlib, c, hq, q, new, prefix)
+    check_prefill(c, hq, q, new, prefix, got, rows=8)
+    np.testing.assert_array_equal(got, prefill(pdlib, c, hq, q, new, [b if a else 0 for a, b in zip(new, prefix)]))

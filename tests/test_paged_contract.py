@@ -35,3 +35,22 @@ def test_decode_call_takes_the_workspace_of_a_larger_call(pdlib, hq, hkv, hd, mo
         with pytest.raises(pdlib.PdError) as e:
             pdlib.pd_paged_decode_attention(cfg, ptr, hq * hd, ptr, ptr, batch, n, k, ptr, room, stream=0)
         assert e.value.status == pdlib.PD_ERR_CUDA, (batch, n)
+
+
+def test_prefill_ignores_the_prefix_of_a_request_without_rows(pdlib):
+    """A padded batch that shares its length array with the append (-1: left out) is no error as long as such a request brings no
+    row; with rows it still is."""
+    if torch.cuda.is_available():
+        pytest.skip("the pointers of this test are not to reach a GPU")
+    ptr = 1 << 20
+    cfg = pdlib.LayerConfig(512, 8, 2, 64, 64)
+    k = pdlib.paged_kv_cache_struct(ptr, ptr, ptr, ptr, ptr, 8, 64, 4, 4)
+    need = pdlib.pd_paged_prefill_attention_workspace_bytes(cfg, 3, 256)
+    call = lambda cu, pre: pdlib.pd_paged_prefill_attention(cfg, ptr, 512, ptr, ptr, cu, ptr, pre, k, ptr, need, stream=0)  # noqa: E731
+    call([0, 0, 0], [-1, 5])                                  # no rows at all: nothing to do
+    call([0, 0, 0], [1 << 20, -(1 << 31)])
+    for cu, pre, status in [([0, 0, 7, 7], [-1, 3, -5], pdlib.PD_ERR_CUDA), ([0, 7, 7, 9], [0, 1000, 100], pdlib.PD_ERR_CUDA),
+                            ([0, 1, 7, 9], [-1, 3, 0], pdlib.PD_ERR_INVALID_ARG), ([0, 1, 7, 7], [256, 3, 0], pdlib.PD_ERR_INVALID_ARG)]:
+        with pytest.raises(pdlib.PdError) as e:
+            call(cu, pre)
+        assert e.value.status == status, (cu, pre)
