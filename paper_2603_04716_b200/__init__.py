@@ -270,16 +270,17 @@ class LayerConfig:
     fp8_projections: bool = False
 
     def c_struct(self) -> pd_layer_cfg:
-        """The C struct, made once per configuration (the library only reads it)."""
-        made = self.__dict__.get("_c_struct")
-        if made is None:
-            made = self._make_c_struct()
-            object.__setattr__(self, "_c_struct", made)
-        return made
-
-    def _make_c_struct(self) -> pd_layer_cfg:
+        """A C struct of this configuration, the caller's own."""
         return pd_layer_cfg(C.sizeof(pd_layer_cfg), self.d_model, self.n_q_heads, self.n_kv_heads, self.head_dim,
                             self.d_ff, self.rms_eps, self.rope_theta, self.max_pos, int(self.fp8_projections))
+
+    def _c_ref(self):
+        """A reference to the struct that the calls of this module pass, made once (the library only reads it)."""
+        made = self.__dict__.get("_made")
+        if made is None:
+            made = self.c_struct()
+            object.__setattr__(self, "_made", made)
+        return C.byref(made)
 
     @property
     def n_qkv(self) -> int:
@@ -316,7 +317,7 @@ def pd_trace_end() -> dict:
 
 def pd_workspace_bytes(cfg: LayerConfig, max_tokens: int, max_batch: int, max_kv_len: int) -> int:
     out = C.c_size_t(0)
-    _check(_lib.pd_workspace_bytes(C.byref(cfg.c_struct()), max_tokens, max_batch, max_kv_len, C.byref(out)),
+    _check(_lib.pd_workspace_bytes(cfg._c_ref(), max_tokens, max_batch, max_kv_len, C.byref(out)),
            "pd_workspace_bytes")
     return out.value
 
@@ -329,7 +330,7 @@ class Layer:
         w = pd_layer_weights(C.sizeof(pd_layer_weights), *[_ptr(weights[k]) for k in
                              ("w_qkv", "w_o", "w_gate", "w_up", "w_down", "g_attn", "g_mlp")])
         h = _P()
-        _check(_lib.pd_layer_create(C.byref(cfg.c_struct()), C.byref(w), _stream_ptr(stream), C.byref(h)),
+        _check(_lib.pd_layer_create(cfg._c_ref(), C.byref(w), _stream_ptr(stream), C.byref(h)),
                "pd_layer_create")
         self.handle = h
 
@@ -376,14 +377,14 @@ def pd_decode_layer(layer: Layer, x, out, kv_len_dev, batch: int, max_kv_len: in
 
 def pd_decode_attention_workspace_bytes(cfg: LayerConfig, batch: int, max_kv_len: int) -> int:
     out = C.c_size_t(0)
-    _check(_lib.pd_decode_attention_workspace_bytes(C.byref(cfg.c_struct()), batch, max_kv_len, C.byref(out)),
+    _check(_lib.pd_decode_attention_workspace_bytes(cfg._c_ref(), batch, max_kv_len, C.byref(out)),
            "pd_decode_attention_workspace_bytes")
     return out.value
 
 
 def pd_decode_attention(cfg: LayerConfig, q, ldq: int, out, kv_len_dev, batch: int, max_kv_len: int,
                         cache: pd_kv_cache, workspace, workspace_bytes: int, stream=None):
-    _check(_lib.pd_decode_attention(C.byref(cfg.c_struct()), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch,
+    _check(_lib.pd_decode_attention(cfg._c_ref(), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch,
                                     max_kv_len, C.byref(cache), _ptr(workspace), workspace_bytes,
                                     _stream_ptr(stream)), "pd_decode_attention")
 
@@ -392,7 +393,7 @@ def pd_prefill_attention(cfg: LayerConfig, q, ldq: int, out, cu_seqlens_dev, cu_
                          prefix_dev=None, prefix_host=None, slots_dev=None, err_word=None, stream=None):
     cu = _i32_array(cu_seqlens_host)
     pre = _i32_array(prefix_host) if prefix_host is not None else None
-    _check(_lib.pd_prefill_attention(C.byref(cfg.c_struct()), _ptr(q), ldq, _ptr(out), _ptr(cu_seqlens_dev), cu,
+    _check(_lib.pd_prefill_attention(cfg._c_ref(), _ptr(q), ldq, _ptr(out), _ptr(cu_seqlens_dev), cu,
                                      len(cu_seqlens_host) - 1, _ptr(prefix_dev), pre, _ptr(slots_dev),
                                      C.byref(cache), _ptr(err_word), _stream_ptr(stream)), "pd_prefill_attention")
 
@@ -406,7 +407,7 @@ def pd_decode_attention_noalloc(cfg: LayerConfig, q, ldq: int, out, kv_len_dev, 
     device memory: the split partials live in a fixed NOALLOC_SCRATCH_BYTES array inside the
     library.  Raises PdError(PD_ERR_WORKSPACE_TOO_SMALL) when the problem does not fit it.
     Calls on one device share that array, so keep them on one stream."""
-    _check(_lib.pd_decode_attention_noalloc(C.byref(cfg.c_struct()), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev),
+    _check(_lib.pd_decode_attention_noalloc(cfg._c_ref(), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev),
                                             batch, max_kv_len, C.byref(cache), _stream_ptr(stream)),
            "pd_decode_attention_noalloc")
 
@@ -518,7 +519,7 @@ def pd_gemm_bf16_ws(a, b, c, m: int, n: int, k: int, workspace, workspace_bytes:
 def pd_workspace_offsets(cfg: LayerConfig, tokens: int) -> dict:
     """Byte offsets of the intermediates a layer pass over `tokens` rows leaves in its workspace."""
     out = pd_workspace_layout(C.sizeof(pd_workspace_layout))
-    _check(_lib.pd_workspace_offsets(C.byref(cfg.c_struct()), tokens, C.byref(out)), "pd_workspace_offsets")
+    _check(_lib.pd_workspace_offsets(cfg._c_ref(), tokens, C.byref(out)), "pd_workspace_offsets")
     return {n: int(getattr(out, n)) for n in ("norm", "qkv", "attn_o", "resid", "act")}
 
 
@@ -571,7 +572,7 @@ def pd_rope_table(cfg: LayerConfig):
     if cfg.max_pos <= 0 or cfg.head_dim <= 0:
         raise PdError(PD_ERR_INVALID_ARG, "pd_rope_table")
     out = np.empty((cfg.max_pos, cfg.head_dim // 2, 2), dtype=np.float32)
-    _check(_lib.pd_rope_table(C.byref(cfg.c_struct()), out.ctypes.data), "pd_rope_table")
+    _check(_lib.pd_rope_table(cfg._c_ref(), out.ctypes.data), "pd_rope_table")
     return out
 
 
@@ -583,28 +584,28 @@ def pd_paged_kv_append(cfg: LayerConfig, qkv, ldqkv: int, q_out, rope_tab, cache
         if len(cu_seqlens_host) != n_req + 1:
             raise ValueError("cu_seqlens has one entry more than there are requests")
         cu = _i32_array(cu_seqlens_host)
-    _check(_lib.pd_paged_kv_append(C.byref(cfg.c_struct()), _ptr(qkv), ldqkv, _ptr(q_out), _ptr(rope_tab),
+    _check(_lib.pd_paged_kv_append(cfg._c_ref(), _ptr(qkv), ldqkv, _ptr(q_out), _ptr(rope_tab),
                                    _ptr(cu_seqlens_dev), cu, n_req, _ptr(kv_len_dev), C.byref(cache), _ptr(err_word),
                                    _stream_ptr(stream)), "pd_paged_kv_append")
 
 
 def pd_paged_decode_attention_workspace_bytes(cfg: LayerConfig, batch: int, max_kv_len: int) -> int:
     out = C.c_size_t(0)
-    _check(_lib.pd_paged_decode_attention_workspace_bytes(C.byref(cfg.c_struct()), batch, max_kv_len, C.byref(out)),
+    _check(_lib.pd_paged_decode_attention_workspace_bytes(cfg._c_ref(), batch, max_kv_len, C.byref(out)),
            "pd_paged_decode_attention_workspace_bytes")
     return out.value
 
 
 def pd_paged_decode_attention(cfg: LayerConfig, q, ldq: int, out, kv_len_dev, batch: int, max_kv_len: int,
                               cache: pd_paged_kv_cache, workspace, workspace_bytes: int, err_word=None, stream=None):
-    _check(_lib.pd_paged_decode_attention(C.byref(cfg.c_struct()), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch,
+    _check(_lib.pd_paged_decode_attention(cfg._c_ref(), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch,
                                           max_kv_len, C.byref(cache), _ptr(workspace), workspace_bytes, _ptr(err_word),
                                           _stream_ptr(stream)), "pd_paged_decode_attention")
 
 
 def pd_paged_prefill_attention_workspace_bytes(cfg: LayerConfig, n_req: int, max_kv_len: int) -> int:
     out = C.c_size_t(0)
-    _check(_lib.pd_paged_prefill_attention_workspace_bytes(C.byref(cfg.c_struct()), n_req, max_kv_len, C.byref(out)),
+    _check(_lib.pd_paged_prefill_attention_workspace_bytes(cfg._c_ref(), n_req, max_kv_len, C.byref(out)),
            "pd_paged_prefill_attention_workspace_bytes")
     return out.value
 
@@ -618,7 +619,7 @@ def pd_paged_prefill_attention(cfg: LayerConfig, q, ldq: int, out, cu_seqlens_de
         if len(prefix_host) != len(cu_seqlens_host) - 1:
             raise ValueError("one prefix per request")
         pre = _i32_array(prefix_host)
-    _check(_lib.pd_paged_prefill_attention(C.byref(cfg.c_struct()), _ptr(q), ldq, _ptr(out), _ptr(cu_seqlens_dev), cu,
+    _check(_lib.pd_paged_prefill_attention(cfg._c_ref(), _ptr(q), ldq, _ptr(out), _ptr(cu_seqlens_dev), cu,
                                            len(cu_seqlens_host) - 1, _ptr(prefix_dev), pre, C.byref(cache),
                                            _ptr(workspace), workspace_bytes, _ptr(err_word), _stream_ptr(stream)),
            "pd_paged_prefill_attention")
@@ -639,7 +640,7 @@ def pd_measure(cfg: LayerConfig, *, n_layers_run: int, n_layers_model: int, warm
                        l_arr, len(l_in), b_arr, len(batch_sizes), kv_len_start, n_steps, step_stride, mix, vocab,
                        chunk_tokens, g_arr, len(l_in_grid))
     out = pd_measurement()
-    _check(_lib.pd_measure(C.byref(cfg.c_struct()), C.byref(m), peak_bf16_flops, peak_hbm_bytes_s, C.byref(out)),
+    _check(_lib.pd_measure(cfg._c_ref(), C.byref(m), peak_bf16_flops, peak_hbm_bytes_s, C.byref(out)),
            "pd_measure")
     n = out.n_points
     return {

@@ -54,3 +54,18 @@ def test_prefill_ignores_the_prefix_of_a_request_without_rows(pdlib):
         with pytest.raises(pdlib.PdError) as e:
             call(cu, pre)
         assert e.value.status == status, (cu, pre)
+
+
+def test_every_c_struct_is_the_callers_own(pdlib):
+    """A caller may change the struct that c_struct() returns; the configuration and its later calls do not notice."""
+    import copy
+    import pickle
+    cfg = pdlib.LayerConfig(512, 8, 2, 64, 64, max_pos=4)
+    want = pdlib.pd_rope_table(cfg)                       # (a call that has used the configuration's struct)
+    mine = cfg.c_struct()
+    mine.max_pos, mine.head_dim = 0, 7
+    assert cfg.c_struct().max_pos == 4 and cfg.c_struct().head_dim == 64
+    np.testing.assert_array_equal(pdlib.pd_rope_table(cfg), want)
+    for other in (copy.copy(cfg), copy.deepcopy(cfg), pickle.loads(pickle.dumps(cfg))):
+        assert other == cfg and hash(other) == hash(cfg)
+        np.testing.assert_array_equal(pdlib.pd_rope_table(other), want)
