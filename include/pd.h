@@ -375,7 +375,9 @@ pd_status pd_gemm_fp8_blockwise(const void* a_codes, const float* a_scales, cons
  *   h = bf16(x + residual),  n = h * rsqrt(mean(h^2) + eps) * gain  (fp32, from the rounded h),
  *   s = max|n| / 448 (1 for an all-zero block; never below the smallest normal float),  code = E4M3(n / s)
  * with one s per row and 128 channels (group = 128, d a multiple of 128) or per row (group = 0, d a multiple of 16).  The
- * codes are those of the fp32 n: there is no bf16 rounding between the norm and the quantiser.
+ * codes are those of the fp32 n: there is no bf16 rounding between the norm and the quantiser.  s and n / s are formed with
+ * products and an approximate reciprocal, right to 2^-22: a code whose quotient lies closer than that to the middle of two is
+ * one of the two (pd_quantize_fp8_groups divides, and of the norm rounded to bf16: its codes and scales differ).
  *   x, residual   device bf16 [rows, d], row pitches ldx and ldr elements (multiples of 8); residual may be NULL (h = x)
  *   gain          device bf16 [d]
  *   sum_out       h, device bf16 [rows, d] contiguous, or NULL; may alias x or residual where that one's pitch is d
