@@ -477,7 +477,8 @@ pd_status pd_paged_decode_attention(const pd_layer_cfg* cfg, const void* q, int3
  * Roundings, of this call and of pd_paged_decode_attention: a weight of the softmax is off by 2^-11 of itself, or by 2^-32 of its
  * row's largest where that is more (2^-22 on a page whose V scale is 1 / 2 to 1 / 1024 of the largest of the sequence).  V is exact
  * while the page scales of a sequence lie within 2^110 of each other, whatever the pages weigh.  q is exact down to 2^-24
- * of its row's largest entry in the streaming kernel and down to 2^-17 of it in the tensor-memory kernel.  Sums are fp32.
+ * of its row's largest entry in the streaming kernel and down to 2^-17 of it in the tensor-memory kernel.  Sums are fp32 and
+ * unnormalised: 2^7 times the number of keys times the largest |v| has to stay below 3e38.
  * Only enqueues work. */
 pd_status pd_paged_prefill_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t n_req, int32_t max_kv_len,
                                                      size_t* out_bytes);

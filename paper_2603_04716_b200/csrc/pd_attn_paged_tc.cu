@@ -15,7 +15,7 @@
 //     row gets does not depend on the size of pages that weigh nothing for it or that only other rows see.  Every role has a
 //     second copy of its code (ANY) that takes items of either kind, with the same arithmetic, which a block goes on with from
 //     its first far item to its end.  (Measured against the kernel without far items: calls of hundreds of us 1.5 to 3 %, of
-//     25 us 1.4 us more; a branch per tile in one copy of the roles 5 to 9 %.)
+//     25 us 1.4 us more; a branch per tile in one copy of the roles 5 to 9 %.  Far items take 1.3 to 1.7 times as long.)
 //   * p is kept as 2^7 p; the row reference of the exponent may lag the maximum by 2^8.  There is no decoded copy of the cache in
 //     global memory.
 //   * When there are fewer items than SMs, or few left over behind the last full turn of the SMs, key ranges are cut into
@@ -32,13 +32,14 @@
 //   warps 1, 2    : MMA issuers of row tile 0, 1 - S = Q K^T, O += P V (P read from tensor memory)
 //   warps 4-7, 8-11 : softmax of row tile 0, 1, one row per thread; they also store the output rows
 //   warps 12-15   : 32 rows each - V tiles from codes to f16, Q into two codes (while the item before is finished)
-// What bounds it: the issuers.  A half costs a row tile 12 products, 650 cycles of the tensor pipe when back to back, 1300 for
-// both tiles; their thread gets them out at 1000 to 1600 between the other warps of its scheduler, the period of a half is
-// 2150.  So an issuer runs its code as a whole warp (uniform addresses: one lane alone 4 % slower), descriptors are a sum with
+// What bounds it: two chains of about equal length, the products and the softmax.  A half costs a row tile 12 products, 650 cycles of the
+// tensor pipe when back to back (8 of S, each of which reads 6 KB of shared memory, 48 cycles where the arithmetic is 32; 4 of P V, 64
+// each), 1300 for both tiles; their thread gets them out at 1000 to 1600 between the other warps of its scheduler, the period
+// of a half is 2150.  So an issuer runs its code as a whole warp (uniform addresses: one lane alone 4 % slower), descriptors are a sum with
 // a constant, and loops that every warp shares the instruction caches with are kept small (roles inlined: 1.4 times the time).
-// (Counters at 4 x 1000 tokens over 5000 keys: tensor pipe 66 % of the cycles, special functions 43 %, issue slots 53 %.)
-// Measured: 37 chunks, 358 Gflop, in 382 us = 0.94 Pflop/s, 56 % of a library product's rate; a prompt of 4096 tokens (137 Gflop)
-// in 159 us, of 8192 in 526 us = 1.05 Pflop/s.
+// (Counters at 4 x 1000 tokens over 5000 keys: tensor pipe 62 % of the cycles, special functions 42 %, issue slots 50 %.)
+// Measured: 37 chunks, 358 Gflop, in 385 us = 0.93 Pflop/s, 56 % of a library product's rate; a prompt of 4096 tokens (137 Gflop)
+// in 160 us, of 8192 in 533 us = 1.03 Pflop/s.
 // Every wait is wall-clock bounded and leaves through the common teardown.
 #include <math_constants.h>
 

@@ -15,8 +15,8 @@
 // that they are free of bank conflicts.  q is scaled by a power of two per head into f16 range.  The reference of the
 // exponent follows the maximum lazily, so a tile costs one vote instead of a reduction over its keys.  Softmax statistics
 // and O are fp32; K's scale is applied to the scores, V's to the weights, relative to the largest V scale so far.
-// Measured: 256 sequences of 2304 keys (1.13 GB) in 171 us = 103 % of a copy's rate; one sequence of 32768 keys (67 MB) in 19 us,
-// 24 of 100 to 4351 keys (103 MB) in 29 us, 53 %: launch, first lookups, ramp of the rings and the join do not shrink with it.
+// Measured: 256 sequences of 2304 keys (1.13 GB) in 170 us = 103 % of a copy's rate, repeated on one cache, and 176 to 187 us = 94 to 100 % as a
+// call among caches that change; one sequence of 32768 keys (67 MB) in 19 us, 24 of 100 to 4351 keys (103 MB) in 29 us, 53 %: launch, first lookups, ramp of the rings and the join do not shrink with it.
 #include <math_constants.h>
 
 #include <algorithm>

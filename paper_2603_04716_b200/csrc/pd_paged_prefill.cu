@@ -13,9 +13,10 @@ namespace {
 //   TILES  tensor-memory tiles of 128 (token, head) rows
 // Estimated times in microseconds, fitted to measurements (32 query and 8 KV heads of 128, one to 37 requests, 1 to 8192 fresh
 // tokens, up to 16000 cached): the fixed part, the steps of the busiest SM, the row blocks, the join.  Heads of 64 take
-// about 0.7 of a tile step.  Examples, measured (ROWS / TILES): 1 x 8 tokens over 2000 keys 11 / 15, 1 x 32 17 / 16, 1 x 64 20 / 22, 1 x 128 38 / 25,
-// 4 x 16 over 5000 40 / 36, 8 x 64 over 4096 221 / 62, 32 x 4 over 2000 39 / 81, a prompt of 4096 tokens 989 / 160.
-// Of 38 measured calls the estimates miss the faster kernel in two, by 1.4 and 2.5 us.
+// about 0.7 of a tile step.  Examples, measured (ROWS / TILES): 1 x 8 tokens over 2000 keys 11 / 15, 1 x 32 16 / 19, 1 x 64 21 / 25, 1 x 128 40 / 26,
+// 4 x 16 over 5000 41 / 38, 8 x 64 over 4096 231 / 63, 32 x 4 over 2000 41 / 84, a prompt of 4096 tokens 989 / 160.
+// Of 24 measured calls around the border the estimates miss the faster kernel in four: 1 x 64 (by 4 us), 8 x 16 over 200 keys (2) and
+// prompts without a prefix, whose short key ranges the streaming kernel's fixed cost outweighs: 1 x 200 20 / 14, 4 x 100 36 / 13.
 // (A third way, pages decoded to a contiguous bf16 copy for the kernel of pd_prefill_attention, took 303 us for 1 x 512 over
 // 16000 keys where TILES take 162, 165 for the prompt, and was ahead only for short prompts without a prefix, 131 against 142
 // at 8 x 1000; its copy of n_req * max_kv_len rows was the price.)
