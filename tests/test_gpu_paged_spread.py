@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 
 import pd_inputs as gen
+from gpu_util import empty_bf16, from_dev, i32_dev, to_dev
 from oracle import paged
 from paged_util import F16, Cache, assert_within, attention_bound
 from test_gpu_paged_attention import decode, prefill
@@ -151,6 +152,53 @@ def test_nan_values_among_far_pages(pdlib, hq, hkv, hd, page_len):
     got = prefill(pdlib, c.upload(), hq, q, new, prefix).reshape(-1, hq, hd)
     np.testing.assert_array_equal(np.isnan(got), bad)
     np.testing.assert_array_equal(got[~bad], want[~bad])
+
+
+def test_wait_timeout_among_far_pages(pdlib):
+    """One arrival left out while the second copy of the roles is at work: the error word says so and the next call is right."""
+    import torch
+    hq, hkv, hd, page_len, n, pre = 32, 8, 128, 64, 128, 2000
+    c = scaled_cache(pdlib, hkv, hd, page_len, [n + pre], lambda s, i: 30 if i % 9 == 0 else 0, np.random.default_rng(5))
+    q = gen.normal_bf16(107, gen.S_X, (n, hq, hd), 1.0)
+    cfg = pdlib.LayerConfig(hq * hd, hq, hkv, hd, 64)
+    need = pdlib.pd_paged_prefill_attention_workspace_bytes(cfg, 1, n + pre)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out, err = empty_bf16(n, hq * hd), torch.zeros(1, dtype=torch.int32, device="cuda")
+    pdlib.pd_test_inject_wait_timeout(pdlib.INJECT_ATTN_PAGED, 20_000_000)
+    try:
+        pdlib.pd_paged_prefill_attention(cfg, to_dev(q.reshape(n, -1)), hq * hd, out, i32_dev([0, n]), [0, n], i32_dev([pre]), [pre], c.struct,
+                                         ws, need, err_word=err)
+        torch.cuda.synchronize()
+    finally:
+        pdlib.pd_test_inject_wait_timeout(pdlib.INJECT_NONE, 0)
+    if os.environ.get("PD_PAGED_PREFILL") != "0":      # (the streaming kernel waits for nothing)
+        assert int(err.item()) == 1
+    check(c, hq, q, pre, n, 0, prefill(pdlib, c, hq, q, [n], [pre]), "after it")
+
+
+def test_far_pages_in_a_replayed_graph(pdlib):
+    """Whether pages are far apart is seen on the device: a captured call follows the scales of its replay."""
+    import torch
+    hq, hkv, hd, page_len, n, pre = 32, 8, 128, 64, 200, 300
+    c = scaled_cache(pdlib, hkv, hd, page_len, [n + pre], lambda s, i: 0, np.random.default_rng(6))
+    q = gen.normal_bf16(108, gen.S_X, (n, hq, hd), 1.0)
+    usual = prefill(pdlib, c, hq, q, [n], [pre])
+    cfg = pdlib.LayerConfig(hq * hd, hq, hkv, hd, 64)
+    need = pdlib.pd_paged_prefill_attention_workspace_bytes(cfg, 1, n + pre)
+    ws, dq, out = torch.empty(need, dtype=torch.uint8, device="cuda"), to_dev(q.reshape(n, -1)), empty_bf16(n, hq * hd)
+    cu, dpre, s, g = i32_dev([0, n]), i32_dev([pre]), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        pdlib.pd_paged_prefill_attention(cfg, dq, hq * hd, out, cu, [0, n], dpre, [pre], c.struct, ws, need)
+    for page, factor in ((2, 2.0 ** 35), (2, 2.0 ** -35), (6, 2.0 ** -50)):
+        c.vs[c.table[0, page]] *= np.float32(factor)
+        c.dvs.copy_(torch.from_numpy(c.vs))
+        g.replay()
+        torch.cuda.synchronize()
+        got = from_dev(out)
+        check(c, hq, q, pre, n, 0, got, f"page {page}")
+        if factor == 2.0 ** -35:
+            np.testing.assert_array_equal(got, usual)
 
 
 @pytest.mark.parametrize("which", [0, 1])
