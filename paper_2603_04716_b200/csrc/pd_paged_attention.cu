@@ -608,9 +608,9 @@ Split decode_split(int batch, int n_kv_heads, int max_kv_len) {
 long long decode_most_parts(int batch, int n_kv_heads, int max_kv_len) {
   if (batch <= 0 || max_kv_len <= PA_MIN_CHUNK) return 0;
   const long long fill = (1ll * batch * n_kv_heads <= 148 ? PA_RESIDENT : PA_RESIDENT * 3 / 2) / n_kv_heads;
-  const long long most = std::min(fill, 1ll * batch * ((max_kv_len + PA_MIN_CHUNK - 1) / PA_MIN_CHUNK));
+  const long long most = std::min(fill, batch * ((max_kv_len + (PA_MIN_CHUNK - 1ll)) / PA_MIN_CHUNK));
   // (17: of max_kv_len / 16 keys, rounded down, and what is left)
-  const long long length = batch > 1 ? std::min(17, (max_kv_len + 4095) / 4096) : 1;
+  const long long length = batch > 1 ? std::min(17ll, (max_kv_len + 4095ll) / 4096) : 1;
   return std::max(most > 1 ? most : 0, length > 1 ? length * batch : 0);
 }
 

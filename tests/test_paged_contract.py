@@ -12,7 +12,7 @@ def test_decode_workspace_of_the_largest_call_serves_smaller_ones(pdlib, hq, hkv
     need = lambda b, n: pdlib.pd_paged_decode_attention_workspace_bytes(cfg, b, n)  # noqa: E731
     rng = np.random.default_rng(hq)
     batches = sorted({0, 1, 2, 3, 8, 18, 19, 37, 74, 75, 148, 149, 256, 1000, 65535} | set(int(v) for v in rng.integers(1, 400, 20)))
-    lengths = sorted({0, 1, 255, 256, 257, 2304, 4096, 4097, 8192, 9472, 9473, 32768, 65535, 65536, 65551, 1 << 20, (1 << 27) + 5} |
+    lengths = sorted({0, 1, 255, 256, 257, 2304, 4096, 4097, 8192, 9472, 9473, 32768, 65535, 65536, 65551, 1 << 20, (1 << 27) + 5, (1 << 31) - 300, (1 << 31) - 1} |
                      set(int(v) for v in np.exp(rng.uniform(3, 15, 30))))
     table = np.array([[need(b, n) for n in lengths] for b in batches], dtype=np.int64)
     assert (np.diff(table, axis=0) >= 0).all() and (np.diff(table, axis=1) >= 0).all()
