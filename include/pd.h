@@ -488,6 +488,157 @@ pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const void* q, int
                                      const pd_paged_kv_cache* cache, void* workspace, size_t workspace_bytes,
                                      int32_t* err_word, void* stream);
 
+/* ------------------------------------------------------ 4-bit paged KV cache */
+
+/* Rotary positions as models for long contexts vary them, norms of the q and k heads, and a paged KV cache in 4 bits (the paper
+ * hands the KV cache of a request from a prefill to a decode instance and keeps it there for the request's life; 0.5625 bytes
+ * per element instead of 2, or 1 of the 8-bit cache, are moved, kept and read.  The paper fixes neither a cache format nor the
+ * attention of the models it deploys).
+ *
+ * Frequencies f_i, i = 0 .. rot_dim/2 - 1, start from theta^(-2 i / rot_dim) and are scaled by
+ *   PD_ROPE_SCALE_NONE    nothing
+ *   PD_ROPE_SCALE_LINEAR  f_i / factor
+ *   PD_ROPE_SCALE_BASE    theta replaced by theta * factor^(rot_dim / (rot_dim - 2))
+ *   PD_ROPE_SCALE_TURNS   w f_i + (1 - w) f_i / factor, w = (n_i - low) / (high - low) within 0 .. 1, where
+ *                         n_i = trained_len * f_i / (2 pi) is how often pair i turns within the trained length
+ *   PD_ROPE_SCALE_INDEX   the same with w = 1 - (i - a) / (b - a) within 0 .. 1, where a = max(floor(I(high)), 0),
+ *                         b = min(ceil(I(low)), rot_dim/2 - 1), I(n) = rot_dim ln(trained_len / (2 pi n)) / (2 ln theta) is the
+ *                         (fractional) pair that turns n times; b - a below 0.001 counts as 0.001
+ * and the table holds magnitude * cos and magnitude * sin of position * f_i. */
+enum { PD_ROPE_SCALE_NONE = 0, PD_ROPE_SCALE_LINEAR = 1, PD_ROPE_SCALE_BASE = 2, PD_ROPE_SCALE_TURNS = 3, PD_ROPE_SCALE_INDEX = 4 };
+typedef struct {
+  uint32_t struct_size;
+  int32_t rot_dim;     /* features of a head that are rotated, the first ones: a multiple of 16, at most 128 */
+  int32_t scaling;     /* PD_ROPE_SCALE_* */
+  int32_t trained_len; /* TURNS, INDEX: context length of the training, at least 1 */
+  double theta;        /* above 1 */
+  double factor;       /* all but NONE: at least 1 */
+  double low, high;    /* TURNS, INDEX: 0 < low < high */
+  double magnitude;    /* above 0 (1: plain rotation) */
+} pd_rope_cfg;
+
+/* Table rows of positions first_pos .. first_pos + n_pos - 1: device fp32 [n_pos, rot_dim / 2, 2], 8-byte aligned.  Angles and
+ * their cos and sin are computed in double and rounded once (right to 2^-24 + position * 2^-50, relative to magnitude).  first_pos +
+ * n_pos below 2^31.  Enqueues one kernel; n_pos = 0 does nothing. */
+pd_status pd_rope_table_scaled(const pd_rope_cfg* rope, int32_t first_pos, int32_t n_pos, float* table, void* stream);
+
+/* What happens to the q and k heads of a projection before attention: x = x * rsqrt(mean(x^2) + eps) * gain over the features
+ * of a head (where there is a gain), then the rotation of its first rot_dim features,
+ * (a, b) -> (a cos - b sin, b cos + a sin), of the pairs (x_i, x_{i + rot_dim/2}) (PD_ROPE_HALVES) or (x_2i, x_{2i+1})
+ * (PD_ROPE_PAIRS).  The other features pass unrotated. */
+enum { PD_ROPE_HALVES = 0, PD_ROPE_PAIRS = 1 };
+typedef struct {
+  uint32_t struct_size;
+  int32_t layout;      /* PD_ROPE_HALVES or PD_ROPE_PAIRS */
+  int32_t rot_dim;     /* a multiple of 16, at most head_dim; not used without a table */
+  int32_t n_pos;       /* rows of the table: positions 0 .. n_pos - 1 */
+  const float* table;  /* device fp32 [n_pos, rot_dim / 2, 2], 16-byte aligned; NULL: no rotation, any position */
+  const void* q_gain;  /* device bf16 [head_dim], 16-byte aligned; NULL: q is not normalised */
+  const void* k_gain;  /* the same for k */
+  double eps;          /* at least 0 */
+} pd_qk_transform;
+
+/* Normalises and rotates the q and k heads of projection rows.
+ *   qkv        device bf16 [T, ldqkv]: q heads, k heads (v heads) of a row; ldqkv a multiple of 8, at least (Hq + Hkv) * hd
+ *   q_out      device bf16 [T, ldq_out], Hq * hd columns written; NULL: q is left alone.  May be qkv with ldq_out = ldqkv
+ *   k_out      device bf16 [T, ldk_out], Hkv * hd columns written; NULL: k is left alone.  May be qkv + Hq * hd with
+ *              ldk_out = ldqkv
+ *   positions  device int32 [T]; a negative one leaves its row out (it is neither read nor written)
+ *   err_word   optional device int32, set to 2 where a position lies beyond the table (the row is left out)
+ * Outputs that overlap qkv in any other way, or each other, are undefined.  Tensors start on 16-byte boundaries, pitches are
+ * multiples of 8.  fp32 arithmetic, rounded once; the squares of a head must sum to less than 3e38.  Only head_dim and the head counts of cfg
+ * are used.  Enqueues one kernel; T = 0 does nothing. */
+pd_status pd_qk_norm_rope(const pd_layer_cfg* cfg, const pd_qk_transform* transform, const void* qkv, int32_t ldqkv, void* q_out,
+                          int32_t ldq_out, void* k_out, int32_t ldk_out, const int32_t* positions, int32_t T, int32_t* err_word,
+                          void* stream);
+
+/* KV cache of fixed-size pages in 4 bits.
+ *   k_codes, v_codes    device uint8 [n_pages, Hkv, page_len, hd / 2], 16-byte aligned: E2M1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a
+ *                       sign), feature 2 i in bits 0-3 and feature 2 i + 1 in bits 4-7 of byte i
+ *   k_scales, v_scales  device uint8 [n_pages, Hkv, page_len, hd / 16], 16-byte aligned: one E4M3 scale per 16 features
+ *   k_exp, v_exp        device int32 [Hkv], a power of two per head, from a calibration; NULL: 0.  Held to -30 .. 30
+ *   page_table          device int32 [n_seqs, table_ld]: position p of sequence s lies in page page_table[s][p / page_len], row
+ *                       p % page_len.  Entries of pages that hold no token are not used (they may be read).
+ *   page_len            16, 32, 64 or 128;  table_ld * page_len below 2^31
+ * value = code * scale * 2^exp[head].  Of 16 neighbouring features x, in units of 2^exp: scale = E4M3(max|x| / 6), saturating at
+ * 448, code = E2M1(x / scale), saturating at 6, both rounded to nearest even from the exact quotient; a scale of 0 has codes of
+ * 0.  So magnitudes from 2^-10 to 2688 times 2^exp are represented, and 16 features none of which exceeds 6 * 2^-10 times 2^exp are
+ * stored as zeros.  16 features of which one is infinite or NaN are stored as
+ * NaN (a scale of NaN).  A row has scales of its own: appending touches no other row, and rows may be appended again, in any
+ * order.  A value has six significant bits: reading back to bf16 is exact.
+ * All buffers are the caller's; they need no initialisation.  A sequence's pages are its own while it is appended to; full
+ * pages may be shared for reading. */
+typedef struct {
+  uint32_t struct_size;
+  void* k_codes;
+  void* v_codes;
+  void* k_scales;
+  void* v_scales;
+  const int32_t* k_exp;
+  const int32_t* v_exp;
+  const int32_t* page_table;
+  int32_t n_pages, page_len, n_seqs, table_ld;
+} pd_paged_kv4_cache;
+
+/* Normalises and rotates fresh q and k heads and appends k and v to the cache.
+ *   qkv          device bf16 [T, ldqkv]: q heads, k heads, v heads of a row as the QKV projection leaves them; ldqkv a multiple of 8
+ *   q_out        transformed q, device bf16 [T, Hq*hd] contiguous, not overlapping qkv; NULL: only the cache is written
+ *   cu_seqlens   as for pd_prefill_layer (device and host copy); both NULL: one row per request (a decode step)
+ *   kv_len_dev   device int32[n_req]: tokens that sequence r holds already; its rows take positions kv_len[r],
+ *                kv_len[r] + 1, ...  A negative value leaves the request out: none of its rows is read, written or cached.
+ *                kv_len itself is not modified
+ *   err_word     optional device int32, set to 2 where a row has no place: a position beyond the page table or a page number
+ *                outside the pool (q is still written, k and v are left out); a position beyond the rotation table (the row is left out)
+ * k is transformed in double, so that its codes are those of the exact values up to 2^-45; q in fp32, as in pd_qk_norm_rope.  Two
+ * rows of one call must not be the same position of the same page.  Only head_dim and the head counts of cfg are used.  Only enqueues
+ * work; one kernel; no workspace. */
+pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_transform* transform, const void* qkv, int32_t ldqkv, void* q_out,
+                              const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, int32_t n_req,
+                              const int32_t* kv_len_dev, const pd_paged_kv4_cache* cache, int32_t* err_word, void* stream);
+
+/* Between a bf16 cache of the layer calls (pd_kv_cache) and the 4-bit pages, positions begin[s] .. end[s] - 1 of sequences
+ * s < n_seqs: pd_paged_kv4_write quantises (what a prefill instance computed on its way into the pages), pd_paged_kv4_read reads
+ * back (a prefix in front of pd_prefill_attention, or on its way to an instance that keeps bf16).
+ *   begin, end   device int32[n_seqs]; begin NULL: 0; end <= begin: nothing
+ *   max_len      host upper bound of end[s] - begin[s] (it sizes the grid; what lies behind is left out)
+ *   slots        device int32[n_seqs]: the bf16 cache sequence that belongs to sequence s; NULL: s
+ *   origin       device int32[n_seqs]: position p is row p - origin[s] of the bf16 cache; NULL: 0
+ *   err_word     optional device int32, set to 2 where a position is negative, lies beyond the page table or has a page number
+ *                outside the pool, or where a slot or a row lies outside the bf16 cache; such rows are left out
+ * Rows outside the range are left as they were.  k and v of the bf16 cache start on 16-byte boundaries.  n_seqs at most 65535 and
+ * the n_seqs of the page table.  Only enqueues work; one kernel; no workspace. */
+pd_status pd_paged_kv4_write(const pd_layer_cfg* cfg, const pd_paged_kv4_cache* cache, const int32_t* begin, const int32_t* end,
+                             int32_t n_seqs, int32_t max_len, const pd_kv_cache* in, const int32_t* slots, const int32_t* origin,
+                             int32_t* err_word, void* stream);
+pd_status pd_paged_kv4_read(const pd_layer_cfg* cfg, const pd_paged_kv4_cache* cache, const int32_t* begin, const int32_t* end,
+                            int32_t n_seqs, int32_t max_len, const pd_kv_cache* out, const int32_t* slots, const int32_t* origin,
+                            int32_t* err_word, void* stream);
+
+/* pd_decode_attention over the 4-bit paged cache, for n_new tokens per sequence (1: a decode step; more: drafted tokens that are
+ * verified together).  Row b * n_new + j is the query of sequence b at position kv_len[b] + j and attends to entries
+ * 0 .. kv_len[b] + j of page_table row b (its own tokens must have been appended).
+ *   q, out        device bf16 [B * n_new, ldq] / [B * n_new, Hq*hd], q 16-byte aligned, out only as its elements are, ldq a
+ *                 multiple of 8
+ *   kv_len_dev    device int32[B]; a sequence with kv_len[b] < 0 gets all-zero rows; entries beyond the table are left out
+ *   n_new         at least 1; B * ceil(n_new / t) at most 65535, t = n_new if group * n_new <= 8, else floor(16 / group).  Every t
+ *                 tokens read the cache once
+ *   max_kv_len    host upper bound of kv_len[b] + n_new, at most table_ld * page_len (it sizes the split of the key range; a
+ *                 longer sequence is still computed whole)
+ *   workspace     at least pd_paged_kv4_decode_attention_workspace_bytes() bytes, 256-byte aligned (may be NULL where that is
+ *                 0); what is asked for the largest B, n_new and max_kv_len serves every smaller call; calls that can overlap
+ *                 on the GPU, captured graphs included, need one each
+ *   err_word      optional device int32, set to 2 where a sequence reaches past the table or a page number lies outside the pool
+ *                 (the keys of such a page are left out)
+ * A key stored as NaN makes the rows that see it NaN, a value their 16 features of it; rows in front of it are not touched.
+ * Roundings: K, V and q are exact (q down to 2^-24 of its row's largest entry; |q| below 2^90); a weight of the softmax is off by
+ * 2^-11 of itself, or by 2^-32 of its row's largest where that is more; sums are fp32.  The result does not depend on the order in which the GPU does the work.
+ * Only the head counts and head_dim of cfg are used.  Only enqueues work. */
+pd_status pd_paged_kv4_decode_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t B, int32_t n_new, int32_t max_kv_len,
+                                                        size_t* out_bytes);
+pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, const void* q, int32_t ldq, void* out, const int32_t* kv_len_dev,
+                                        int32_t B, int32_t n_new, int32_t max_kv_len, const pd_paged_kv4_cache* cache,
+                                        void* workspace, size_t workspace_bytes, int32_t* err_word, void* stream);
+
 /* Failure-detection test hook.  Every wait inside the tensor-core kernels (on a tile load, an accumulator, a
  * partner block) is bounded by wall clock (4 s); when a wait gives up, the block raises its abort flag, leaves
  * through the normal teardown (tensor memory freed, cluster barrier of a CTA pair passed) and sets the error

@@ -44,6 +44,8 @@ EXPORTS = [
     "pd_quantize_fp8_groups", "pd_quantize_fp8_blocks", "pd_gemm_fp8_blockwise",
     "pd_add_rmsnorm_fp8", "pd_rope_table", "pd_paged_kv_append", "pd_paged_decode_attention_workspace_bytes",
     "pd_paged_decode_attention", "pd_paged_prefill_attention_workspace_bytes", "pd_paged_prefill_attention",
+    "pd_rope_table_scaled", "pd_qk_norm_rope", "pd_paged_kv4_append", "pd_paged_kv4_write", "pd_paged_kv4_read",
+    "pd_paged_kv4_decode_attention_workspace_bytes", "pd_paged_kv4_decode_attention",
 ]
 
 TRACE_CLASSES = ["gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "attn_prefill", "attn_decode", "rmsnorm",
@@ -88,6 +90,22 @@ class pd_kv_cache(C.Structure):
 class pd_paged_kv_cache(C.Structure):
     _fields_ = ([("struct_size", C.c_uint32)] +
                 [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales", "page_table")] +
+                [(n, C.c_int32) for n in ("n_pages", "page_len", "n_seqs", "table_ld")])
+
+
+class pd_rope_cfg(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32), ("rot_dim", C.c_int32), ("scaling", C.c_int32), ("trained_len", C.c_int32)] +
+                [(n, C.c_double) for n in ("theta", "factor", "low", "high", "magnitude")])
+
+
+class pd_qk_transform(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32), ("layout", C.c_int32), ("rot_dim", C.c_int32), ("n_pos", C.c_int32)] +
+                [(n, C.c_void_p) for n in ("table", "q_gain", "k_gain")] + [("eps", C.c_double)])
+
+
+class pd_paged_kv4_cache(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32)] +
+                [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales", "k_exp", "v_exp", "page_table")] +
                 [(n, C.c_int32) for n in ("n_pages", "page_len", "n_seqs", "table_ld")])
 
 
@@ -198,6 +216,18 @@ _lib.pd_paged_prefill_attention_workspace_bytes.argtypes = [C.POINTER(pd_layer_c
                                                             C.POINTER(C.c_size_t)]
 _lib.pd_paged_prefill_attention.argtypes = [C.POINTER(pd_layer_cfg), _P, C.c_int32, _P, _P, C.POINTER(C.c_int32), C.c_int32,
                                             _P, C.POINTER(C.c_int32), C.POINTER(pd_paged_kv_cache), _P, C.c_size_t, _P, _P]
+_lib.pd_rope_table_scaled.argtypes = [C.POINTER(pd_rope_cfg), C.c_int32, C.c_int32, _P, _P]
+_lib.pd_qk_norm_rope.argtypes = [C.POINTER(pd_layer_cfg), C.POINTER(pd_qk_transform), _P, C.c_int32, _P, C.c_int32, _P, C.c_int32,
+                                 _P, C.c_int32, _P, _P]
+_lib.pd_paged_kv4_append.argtypes = [C.POINTER(pd_layer_cfg), C.POINTER(pd_qk_transform), _P, C.c_int32, _P, _P,
+                                     C.POINTER(C.c_int32), C.c_int32, _P, C.POINTER(pd_paged_kv4_cache), _P, _P]
+for _f in (_lib.pd_paged_kv4_write, _lib.pd_paged_kv4_read):
+    _f.argtypes = [C.POINTER(pd_layer_cfg), C.POINTER(pd_paged_kv4_cache), _P, _P, C.c_int32, C.c_int32, C.POINTER(pd_kv_cache),
+                   _P, _P, _P, _P]
+_lib.pd_paged_kv4_decode_attention_workspace_bytes.argtypes = [C.POINTER(pd_layer_cfg), C.c_int32, C.c_int32, C.c_int32,
+                                                               C.POINTER(C.c_size_t)]
+_lib.pd_paged_kv4_decode_attention.argtypes = [C.POINTER(pd_layer_cfg), _P, C.c_int32, _P, _P, C.c_int32, C.c_int32, C.c_int32,
+                                               C.POINTER(pd_paged_kv4_cache), _P, C.c_size_t, _P, _P]
 _lib.pd_model_create.argtypes = [C.POINTER(_P), C.c_int32, C.POINTER(pd_model_weights), _P, C.POINTER(_P)]
 _lib.pd_model_destroy.argtypes = [_P]
 _lib.pd_model_check.argtypes = [_P, _P]
@@ -623,6 +653,94 @@ def pd_paged_prefill_attention(cfg: LayerConfig, q, ldq: int, out, cu_seqlens_de
                                            len(cu_seqlens_host) - 1, _ptr(prefix_dev), pre, C.byref(cache),
                                            _ptr(workspace), workspace_bytes, _ptr(err_word), _stream_ptr(stream)),
            "pd_paged_prefill_attention")
+
+
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_TURNS, ROPE_SCALE_INDEX = range(5)
+ROPE_HALVES, ROPE_PAIRS = range(2)
+
+
+@dataclass(frozen=True)
+class RopeConfig:
+    """Rotary frequencies of the first rot_dim features of a head and how they are scaled for long contexts."""
+    rot_dim: int
+    theta: float = 1e4
+    scaling: int = ROPE_SCALE_NONE
+    factor: float = 1.0
+    trained_len: int = 4096
+    low: float = 1.0
+    high: float = 32.0
+    magnitude: float = 1.0
+
+    def c_struct(self) -> pd_rope_cfg:
+        return pd_rope_cfg(C.sizeof(pd_rope_cfg), self.rot_dim, self.scaling, self.trained_len, self.theta, self.factor,
+                           self.low, self.high, self.magnitude)
+
+
+def pd_rope_table_scaled(rope: RopeConfig, first_pos: int, n_pos: int, table, stream=None):
+    """table: device fp32 [n_pos, rot_dim / 2, 2] -> cos and sin of positions first_pos .. first_pos + n_pos - 1."""
+    _check(_lib.pd_rope_table_scaled(C.byref(rope.c_struct()), first_pos, n_pos, _ptr(table), _stream_ptr(stream)),
+           "pd_rope_table_scaled")
+
+
+def qk_transform_struct(table, n_pos: int, rot_dim: int, layout: int = ROPE_HALVES, q_gain=None, k_gain=None,
+                        eps: float = 1e-6) -> pd_qk_transform:
+    """Norms (gains bf16 [head_dim], None: none) and rotation (table None: none) of q and k heads."""
+    return pd_qk_transform(C.sizeof(pd_qk_transform), layout, rot_dim, n_pos, _ptr(table), _ptr(q_gain), _ptr(k_gain), eps)
+
+
+def pd_qk_norm_rope(cfg: LayerConfig, transform: pd_qk_transform, qkv, ldqkv: int, q_out, ldq_out: int, k_out, ldk_out: int,
+                    positions_dev, rows: int, err_word=None, stream=None):
+    """q_out, k_out: device bf16 rows, None to leave q or k alone; qkv itself (k: behind its q heads) with ldqkv for in place."""
+    _check(_lib.pd_qk_norm_rope(cfg._c_ref(), C.byref(transform), _ptr(qkv), ldqkv, _ptr(q_out), ldq_out, _ptr(k_out), ldk_out,
+                                _ptr(positions_dev), rows, _ptr(err_word), _stream_ptr(stream)), "pd_qk_norm_rope")
+
+
+def paged_kv4_cache_struct(k_codes, v_codes, k_scales, v_scales, page_table, n_pages: int, page_len: int, n_seqs: int,
+                           table_ld: int, k_exp=None, v_exp=None) -> pd_paged_kv4_cache:
+    """codes: device uint8 [n_pages, Hkv, page_len, head_dim / 2]; scales: uint8 [n_pages, Hkv, page_len, head_dim / 16]."""
+    return pd_paged_kv4_cache(C.sizeof(pd_paged_kv4_cache), _ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales),
+                              _ptr(k_exp), _ptr(v_exp), _ptr(page_table), n_pages, page_len, n_seqs, table_ld)
+
+
+def pd_paged_kv4_append(cfg: LayerConfig, transform: pd_qk_transform, qkv, ldqkv: int, q_out, cache: pd_paged_kv4_cache, kv_len_dev,
+                        n_req: int, cu_seqlens_dev=None, cu_seqlens_host=None, err_word=None, stream=None):
+    """Without cu_seqlens every request brings one row (a decode step)."""
+    cu = None
+    if cu_seqlens_host is not None:
+        if len(cu_seqlens_host) != n_req + 1:
+            raise ValueError("cu_seqlens has one entry more than there are requests")
+        cu = _i32_array(cu_seqlens_host)
+    _check(_lib.pd_paged_kv4_append(cfg._c_ref(), C.byref(transform), _ptr(qkv), ldqkv, _ptr(q_out), _ptr(cu_seqlens_dev), cu, n_req,
+                                    _ptr(kv_len_dev), C.byref(cache), _ptr(err_word), _stream_ptr(stream)), "pd_paged_kv4_append")
+
+
+def pd_paged_kv4_write(cfg: LayerConfig, cache: pd_paged_kv4_cache, begin_dev, end_dev, n_seqs: int, max_len: int,
+                       kv_in: pd_kv_cache, slots_dev=None, origin_dev=None, err_word=None, stream=None):
+    """Positions begin .. end - 1 of every sequence from a bf16 cache into the 4-bit pages."""
+    _check(_lib.pd_paged_kv4_write(cfg._c_ref(), C.byref(cache), _ptr(begin_dev), _ptr(end_dev), n_seqs, max_len, C.byref(kv_in),
+                                   _ptr(slots_dev), _ptr(origin_dev), _ptr(err_word), _stream_ptr(stream)), "pd_paged_kv4_write")
+
+
+def pd_paged_kv4_read(cfg: LayerConfig, cache: pd_paged_kv4_cache, begin_dev, end_dev, n_seqs: int, max_len: int,
+                      kv_out: pd_kv_cache, slots_dev=None, origin_dev=None, err_word=None, stream=None):
+    """Positions begin .. end - 1 of every sequence from the 4-bit pages into a bf16 cache, exactly."""
+    _check(_lib.pd_paged_kv4_read(cfg._c_ref(), C.byref(cache), _ptr(begin_dev), _ptr(end_dev), n_seqs, max_len, C.byref(kv_out),
+                                  _ptr(slots_dev), _ptr(origin_dev), _ptr(err_word), _stream_ptr(stream)), "pd_paged_kv4_read")
+
+
+def pd_paged_kv4_decode_attention_workspace_bytes(cfg: LayerConfig, batch: int, n_new: int, max_kv_len: int) -> int:
+    out = C.c_size_t(0)
+    _check(_lib.pd_paged_kv4_decode_attention_workspace_bytes(cfg._c_ref(), batch, n_new, max_kv_len, C.byref(out)),
+           "pd_paged_kv4_decode_attention_workspace_bytes")
+    return out.value
+
+
+def pd_paged_kv4_decode_attention(cfg: LayerConfig, q, ldq: int, out, kv_len_dev, batch: int, n_new: int, max_kv_len: int,
+                                  cache: pd_paged_kv4_cache, workspace, workspace_bytes: int, err_word=None, stream=None):
+    """Row b * n_new + j of q and out: token j of sequence b, at position kv_len[b] + j."""
+    _check(_lib.pd_paged_kv4_decode_attention(cfg._c_ref(), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch, n_new, max_kv_len,
+                                              C.byref(cache), _ptr(workspace), workspace_bytes, _ptr(err_word),
+                                              _stream_ptr(stream)), "pd_paged_kv4_decode_attention")
 
 
 def pd_measure(cfg: LayerConfig, *, n_layers_run: int, n_layers_model: int, warmup: int = 3, reps: int = 10,

@@ -1,0 +1,631 @@
+// Attention over the 4-bit paged KV cache for one or a few query tokens per sequence (pd_paged_kv4_decode_attention).
+//
+// o = softmax(q K^T / sqrt(hd)) V per query head over the sequence's pages; K and V are E2M1 codes times an E4M3 scale per 16
+// features.  HBM-bound: 0.5625 bytes per element, read once (by every block of tokens).  One block per (part of the key range,
+// KV head, sequence and block of tokens); every warp streams its own 32-key tiles through a private cp.async ring.
+//   S^T = K Q^T    m16n8k16 in f16: rows are 16 keys, columns 8 (token, head of the group) pairs.
+//   O^T = V^T P^T  m16n8k16: rows are features.
+// A code times its scale has six significant bits and lies in 2^-10 .. 2688: exact in f16.  The contraction order of a product
+// is free, so a lane takes hd / 4 neighbouring features of a K row as its share of all k-steps and hd / 8 neighbouring features of
+// four V rows per 16 keys: its scales are a byte or two per row.  Features of two V rows are paired by shifts and masks on whole
+// words before they are converted.  q is scaled by a power of two per head into f16 range.  The reference of the exponent
+// follows the maximum lazily, so a tile costs one vote instead of a reduction over its keys.  Softmax statistics and O are fp32.
+#include <math_constants.h>
+
+#include <algorithm>
+
+#include "pd_kv4.cuh"
+#include "pd_paged.cuh"
+
+namespace pd {
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct Kv4DecodeArgs {
+  const bf16* q;              // [B * n_new, ldq]
+  bf16* o;                    // [B * n_new, Hq*hd]
+  const int32_t* kv_len;      // [B] position of the first row
+  PagedParts parts;           // used when n_splits > 1
+  int* err_word;
+  Kv4Cache c;
+  int ldq, rows, n_new, n_q_heads, n_kv_heads;
+  int block_tokens, seq_blocks;  // tokens of a block: block_tokens * group columns; blocks of a sequence
+  int n_splits, chunk;           // block x covers keys x * chunk .. (the last one whatever lies behind); chunk is a multiple of 64
+};
+
+constexpr int KA_WARPS = 8;
+constexpr int KA_THREADS = KA_WARPS * 32;
+constexpr int KA_KEYS = 32;                     // of a tile: two halves of 16, each within a page
+constexpr int KA_STAGES = 3;
+// p is kept as 2^7 p relative to a reference that may lag the running maximum by 2^8: at most 2^15, below f16's 65504.
+constexpr float P_SHIFT = 7.f, P_SLACK = 8.f, P_UNIT = 1.f / 128.f;
+constexpr int KA_MIN_CHUNK = 256;               // keys of a part at least
+constexpr int KA_RESIDENT = 296;                // blocks that run together (half as many WIDE ones)
+
+template <int HD>
+struct Kv4Smem {
+  static constexpr int CODES = KA_KEYS * HD / 2, SCALES = KA_KEYS * HD / 16;  // bytes of a tile's K (or V)
+  static constexpr int STAGE = 2 * (CODES + SCALES);                          // K codes, V codes, K scales, V scales
+  static constexpr int RING = KA_WARPS * KA_STAGES * STAGE;
+  static constexpr int MERGE = KA_WARPS * 16 * (HD + 2) * 4;
+  static constexpr int BYTES = RING > MERGE ? RING : MERGE;
+};
+
+// Key that row n of an 8-key group of S^T holds.  A lane reads V rows key_of(2 t), key_of(2 t + 1): four neighbouring rows each
+// over the lanes.
+__device__ __forceinline__ int key_of(int n) { return (n >> 1) | ((n & 1) << 2); }
+// Where 16-byte chunk c of key r lies in a tile.  K rows lie in the order in which they are read (8 rows x 4 lanes side by
+// side); V rows of 64 bytes swap their halves in every other pair, so that four rows x 32 bytes fill all banks.
+template <int HD>
+__device__ __forceinline__ uint32_t k_chunk(int r, int c) {
+  return static_cast<uint32_t>(((r & ~7) | ((r & 3) << 1) | ((r >> 2) & 1)) * (HD / 2) + c * 16);
+}
+template <int HD>
+__device__ __forceinline__ uint32_t v_chunk(int r, int c) {
+  return static_cast<uint32_t>(r * (HD / 2) + (HD == 128 ? c ^ (r & 2) : c) * 16);
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// The transpose of an 8 x 8 matrix of halves held one row per four lanes.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Eight E2M1 codes -> eight halves in order, exactly.
+__device__ __forceinline__ void e2m1_to_f16(uint32_t codes, uint32_t (&h)[4]) {
+  asm("{ .reg .b8 b0, b1, b2, b3; mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b0; cvt.rn.f16x2.e2m1x2 %1, b1; cvt.rn.f16x2.e2m1x2 %2, b2; cvt.rn.f16x2.e2m1x2 %3, b3; }"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t addr) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
+}
+// 16 bytes to shared memory, of which the first `bytes` are read and the others become zeros.
+__device__ __forceinline__ void cp_async_part(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// WIDE: 9 to 16 columns (two column groups in both products).  MULTI: blocks of several tokens, or of sequences with several.
+template <int HD, bool WIDE, bool MULTI>
+__global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(const Kv4DecodeArgs a) {
+  using SM = Kv4Smem<HD>;
+  constexpr int KS = HD / 16;          // k-steps of K Q^T
+  constexpr int MT = HD / 16;          // 16-feature tiles of O^T
+  constexpr int NC = WIDE ? 2 : 1;     // column groups of 8 (token, head) pairs
+  constexpr int W = HD / 32;           // words of codes a lane has of a K row, and 2 W of V rows
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int split = blockIdx.x, kvh = blockIdx.y;
+  const int group = a.n_q_heads / a.n_kv_heads;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = lane >> 2, t4 = lane & 3;
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+
+  const int l2p = a.c.log2_page, cap = a.c.table_ld << l2p;
+  const int b = MULTI ? blockIdx.z / a.seq_blocks : blockIdx.z;
+  const int tok0 = MULTI ? (blockIdx.z - b * a.seq_blocks) * a.block_tokens : 0;
+  const int n_tok = MULTI ? min(a.block_tokens, a.n_new - tok0) : 1;
+  const int row0 = (MULTI ? b * a.n_new : b) + tok0;
+  const int n_cols = n_tok * group;
+  // Page numbers of the halves of 32 tiles of this warp at a time, a tile per lane.  The first 32 are read before the sequence's
+  // length is known: entries behind its last page are read, too, but not used.
+  const int32_t* table = a.c.table + static_cast<size_t>(b) * a.c.table_ld;
+  const long long split_begin = 1ll * split * a.chunk;
+  auto fetch_pages = [&](int first, int (&id)[2]) {
+    const long long key = split_begin + (1ll * (first + lane) * KA_WARPS + warp) * KA_KEYS;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const long long page = (key + 16 * h) >> l2p;
+      id[h] = (h == 1 && l2p > 4) ? id[0] : page < a.c.table_ld ? table[page] : -1;
+    }
+  };
+  int id_cur[2], id_nxt[2] = {-1, -1};
+  fetch_pages(0, id_cur);
+  // Column c * 8 + j is token (c * 8 + j) / group, head (c * 8 + j) % group.  q of column c * 8 + g: this lane's share of all
+  // k-steps, features t4 * hd / 4 ..
+  const uint32_t inv_group = 65536u / group + 1u;
+  auto token_of = [&](int col) { return MULTI ? static_cast<int>((col * inv_group) >> 16) : 0; };
+  uint4 qw[NC][KS / 2];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int tok = token_of(c * 8 + g), head = c * 8 + g - tok * group;
+    const bf16* src = a.q + static_cast<size_t>(row0 + tok) * a.ldq + (kvh * group + head) * HD + t4 * (HD / 4);
+#pragma unroll
+    for (int s = 0; s < KS / 2; ++s)
+      qw[c][s] = c * 8 + g < n_cols ? *reinterpret_cast<const uint4*>(src + s * 8) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  const int len = a.kv_len[b];
+  // position of the block's first token; a negative length: a padding sequence, none of its rows sees a key
+  const int pos0 = len < 0 ? -0x40000000 : static_cast<int>(min(1ll * len + tok0, static_cast<long long>(cap)));
+  if (split == 0 && kvh == 0 && tid == 0 && a.err_word && 1ll * len + tok0 + n_tok > cap) atomicExch(a.err_word, 2);
+  const int total = static_cast<int>(max(min(1ll * pos0 + n_tok, static_cast<long long>(cap)), 0ll));  // keys that the last token sees
+  const int k_begin = static_cast<int>(min(1ll * total, split_begin));
+  const int k_end = split == a.n_splits - 1 ? total : static_cast<int>(min(1ll * total, 1ll * k_begin + a.chunk));
+  // the row of column `col` among the partial results, and among the outputs (split 0)
+  auto out_row = [&](int col) {
+    const int tok = token_of(col);
+    return static_cast<size_t>(row0 + tok) * a.n_q_heads + kvh * group + col - tok * group;
+  };
+  const size_t part_row0 = static_cast<size_t>(split) * a.rows * a.n_q_heads;
+  if (split > 0 && k_begin == k_end) {
+    if (tid < n_cols) a.parts.ml[part_row0 + out_row(tid)] = make_float2(-CUDART_INF_F, 0.f);
+    return;
+  }
+  const int n_tiles_blk = static_cast<int>((static_cast<uint32_t>(k_end - k_begin) + KA_KEYS - 1) / KA_KEYS);
+  const int my_tiles = (n_tiles_blk > warp) ? (n_tiles_blk - warp + KA_WARPS - 1) / KA_WARPS : 0;
+  const uint32_t ring = ptx::smem_u32(smem) + warp * (KA_STAGES * SM::STAGE);
+  auto key_begin = [&](int tile) { return k_begin + (tile * KA_WARPS + warp) * KA_KEYS; };
+  // Of a batch of 32 tiles: -1 for a half behind the end or on a page that does not exist (its keys are left out).
+  auto check_pages = [&](int first, int (&id)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (first + lane >= my_tiles || key_begin(first + lane) + 16 * h >= k_end) {
+        id[h] = -1;
+      } else if (static_cast<unsigned>(id[h]) >= static_cast<unsigned>(a.c.n_pages)) {
+        id[h] = -1;
+        if (a.err_word) atomicExch(a.err_word, 2);
+      }
+    }
+  };
+  check_pages(0, id_cur);
+  // the next batch is fetched a batch ahead
+  if (my_tiles > 32) { fetch_pages(32, id_nxt); check_pages(32, id_nxt); }
+
+  // The codes of 16 keys of a page are HD * 8 contiguous bytes, their scales HD.  All rows of a page can be read; keys that do
+  // not count (behind the end, pages that do not exist) get scales of zero instead of whatever is there.
+  constexpr int NLD = HD / 64;
+  uint32_t dst_k[NLD], dst_v[NLD];
+#pragma unroll
+  for (int i = 0; i < NLD; ++i) {
+    const int ch = lane + 32 * i, r = ch / (HD / 32), c = ch % (HD / 32);
+    dst_k[i] = k_chunk<HD>(r, c);
+    dst_v[i] = SM::CODES + v_chunk<HD>(r, c);
+  }
+  // scales: a chunk of 16 bytes per lane, [half][K or V][chunk]
+  constexpr int SC = HD / 16;
+  const int sc_half = lane / (2 * SC), sc_kv = (lane / SC) & 1, sc_chunk = lane % SC;
+  const uint8_t* sc_src = (sc_kv ? a.c.v_scale : a.c.k_scale) + sc_chunk * 16;
+  const uint32_t dst_s = 2 * SM::CODES + sc_kv * SM::SCALES + sc_half * HD + sc_chunk * 16;
+  uint32_t valid = 0;  // of the tiles in flight, two bits each (the newest in bits 0-1): halves with keys
+  auto load_tile = [&](int i, int stage) {
+    if (i > 0 && (i & 31) == 0) { id_cur[0] = id_nxt[0]; id_cur[1] = id_nxt[1]; }
+    const int id0 = __shfl_sync(0xffffffffu, id_cur[0], i & 31), id1 = __shfl_sync(0xffffffffu, id_cur[1], i & 31);
+    const int key0 = key_begin(i);
+    const uint32_t to = ring + stage * SM::STAGE;
+    valid = (valid << 2) | (id0 >= 0 ? 1u : 0u) | (id1 >= 0 ? 2u : 0u);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int id = h ? id1 : id0, key = key0 + 16 * h;
+      const size_t row = ((static_cast<size_t>(max(id, 0)) * a.n_kv_heads + kvh) << l2p) + (key & ((1 << l2p) - 1));
+      const size_t at = row * (HD / 2) + lane * 16;
+#pragma unroll
+      for (int n = 0; n < NLD; ++n) {
+        ptx::cp_async_16(to + h * (HD * 8) + dst_k[n], a.c.k + at + 512 * n, true);
+        ptx::cp_async_16(to + h * (HD * 8) + dst_v[n], a.c.v + at + 512 * n, true);
+      }
+      if (sc_half == h) cp_async_part(to + dst_s, sc_src + row * (HD / 16), id < 0 ? 0 : min(max((k_end - key) * (HD / 16) - sc_chunk * 16, 0), 16));
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < KA_STAGES - 1; ++s) {
+    if (s < my_tiles) load_tile(s, s); else valid <<= 2;
+    ptx::cp_async_commit();
+  }
+
+  // Q^T as f16 operand fragments, every head scaled by a power of two so that its largest entry lies in [1, 2)
+  uint32_t qb[NC][KS][2];
+  float q_scale[NC];  // of the scores of head c * 8 + g, in log2 units
+  const float k_unit = pow2f(kv4_exp(a.c.k_exp, kvh));
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    float x[KS / 2][8], amax = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS / 2; ++s) {
+      unpack8(qw[c][s], x[s]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[s][e]));
+    }
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+    // 2^e <= amax < 2^(e+1), e kept where 2^e and 2^-e are normal (an infinite q stays infinite)
+    const int e = min(max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -126), 126);
+    const float inv = pow2f(-e);
+    q_scale[c] = rsqrtf(static_cast<float>(HD)) * LOG2E * pow2f(e) * k_unit;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        qb[c][s][p] = pack_f16(x[s / 2][(s & 1) * 4 + 2 * p] * inv, x[s / 2][(s & 1) * 4 + 2 * p + 1] * inv);
+    }
+  }
+  // This lane's columns of S^T and O^T are c * 8 + 2 t4 + h, h = 0, 1.
+  float f_head[NC][2];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    f_head[c][0] = __shfl_sync(0xffffffffu, q_scale[c], t4 * 8);
+    f_head[c][1] = __shfl_sync(0xffffffffu, q_scale[c], t4 * 8 + 4);
+  }
+
+  float o_acc[NC][MT][4];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) o_acc[c][i][0] = o_acc[c][i][1] = o_acc[c][i][2] = o_acc[c][i][3] = 0.f;
+  // reference of the exponent (uniform over the lanes of a head; -inf: no key yet) and this lane's share of the sum
+  float m_ref[NC][2], l_sum[NC][2];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m_ref[c][0] = m_ref[c][1] = -CUDART_INF_F;
+    l_sum[c][0] = l_sum[c][1] = 0.f;
+  }
+  bool nan_seen = false;
+
+  for (int i = 0; i < my_tiles; ++i) {
+    const int stage = i % KA_STAGES;
+    {
+      const int nxt = i + KA_STAGES - 1;
+      if (i > 0 && (i & 31) == 0 && i + 32 < my_tiles) { fetch_pages(i + 32, id_nxt); check_pages(i + 32, id_nxt); }
+      if (nxt < my_tiles) load_tile(nxt, nxt % KA_STAGES); else valid <<= 2;
+      ptx::cp_async_commit();
+    }
+    ptx::cp_async_wait<KA_STAGES - 1>();
+    __syncwarp();
+    const uint32_t sk = ring + stage * SM::STAGE, sv = sk + SM::CODES, ssk = sv + SM::CODES, ssv = ssk + SM::SCALES;
+    const int key0 = key_begin(i), halves = static_cast<int>((valid >> (2 * (KA_STAGES - 1))) & 3u);
+    if (MULTI && pos0 - key0 < KA_KEYS - 1) {
+      // Not every token of the block sees all keys, and 0 * NaN is NaN: scales of V that are NaN become 0 where not all see the
+      // key, and the rows that do see it are given their NaN at the end.  A key per lane.
+      if (key0 + lane > pos0) {
+#pragma unroll
+        for (int n = 0; n < HD / 64; ++n) {
+          const uint32_t at = ssv + lane * (HD / 16) + 4 * n, w = lds32(at);
+          bool seen = false;
+          const uint32_t d = drop_nans(w, seen);
+          if (seen) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(d) : "memory");
+          nan_seen |= seen;
+        }
+      }
+      __syncwarp();
+    }
+
+    // ---- S^T = K Q^T: rows are keys key_of(g) and 8 + key_of(g) of each half, columns (token, head) pairs
+    float x[2][NC][4];  // [half][column group][key half][column] = (e >> 1, e & 1)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float st[NC][2][4];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st[c][0][e] = st[c][1][e] = 0.f;
+      uint32_t w[2][W], sc[2][2];  // rows g, g + 8: codes and scales (as pairs of equal halves)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t row = sk + (16 * h + 8 * r + g) * (HD / 2), srow = ssk + (16 * h + 8 * r + key_of(g)) * (HD / 16);
+        if (HD == 128) {
+          const uint4 v = lds128(row + t4 * 16);
+          w[r][0] = v.x; w[r][1] = v.y; w[r][W - 2] = v.z; w[r][W - 1] = v.w;
+          const uint32_t s2 = e4m3x2_to_f16x2(static_cast<uint16_t>(lds16(srow + t4 * 2)));
+          sc[r][0] = __byte_perm(s2, 0, 0x1010);
+          sc[r][1] = __byte_perm(s2, 0, 0x3232);
+        } else {
+          const uint2 v = lds64(row + t4 * 8);
+          w[r][0] = v.x; w[r][1] = v.y;
+          const uint32_t s1 = lds8(srow + t4);
+          sc[r][0] = sc[r][1] = e4m3x2_to_f16x2(static_cast<uint16_t>(s1 | (s1 << 8)));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        uint32_t a0[4], a1[4];
+        e2m1_to_f16(w[0][j], a0);
+        e2m1_to_f16(w[1][j], a1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a0[e] = mul_f16x2(a0[e], sc[0][j / 2]);
+          a1[e] = mul_f16x2(a1[e], sc[1][j / 2]);
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            mma_f16(st[c][p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], qb[c][2 * j + p][0], qb[c][2 * j + p][1]);
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[h][c][e] = (st[c][0][e] + st[c][1][e]) * f_head[c][e & 1];
+    }
+    // ---- softmax
+    const bool masked = (MULTI ? min(k_end, pos0 + 1) : k_end) - key0 < KA_KEYS || halves != 3;
+    if (masked) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          // the last key of the tile that the column's token sees
+          const int last = (MULTI ? min(pos0 + token_of(c * 8 + 2 * t4 + e), k_end - 1) : k_end - 1) - key0;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int lim = (halves >> h) & 1 ? last - 16 * h : -1;
+            if (key_of(g) > lim) x[h][c][e] = -CUDART_INF_F;
+            if (8 + key_of(g) > lim) x[h][c][2 + e] = -CUDART_INF_F;
+          }
+        }
+      }
+    }
+    // the reference follows the maximum only when that has grown by more than P_SLACK (always at the first key)
+    float mx[NC][2];
+    bool grow = false;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        mx[c][e] = fmaxf(fmaxf(x[0][c][e], x[0][c][2 + e]), fmaxf(x[1][c][e], x[1][c][2 + e]));
+        grow |= mx[c][e] > m_ref[c][e] + P_SLACK;
+      }
+    }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float m = mx[c][e];
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+          const float m_new = fmaxf(m_ref[c][e], m);
+          const float corr = m_new == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][e] - m_new);
+          m_ref[c][e] = m_new;
+          l_sum[c][e] *= corr;
+#pragma unroll
+          for (int n = 0; n < MT; ++n) { o_acc[c][n][e] *= corr; o_acc[c][n][2 + e] *= corr; }
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t pb[NC][2];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float (&y)[4] = x[h][c];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float ref = (m_ref[c][e] == -CUDART_INF_F ? 0.f : m_ref[c][e]) - P_SHIFT;  // (no key yet: every p is 0)
+          y[e] = ptx::ex2_approx(y[e] - ref);
+          y[2 + e] = ptx::ex2_approx(y[2 + e] - ref);
+          l_sum[c][e] += y[e] + y[2 + e];
+        }
+        // P^T as an operand: the transpose of the accumulator's 8 x 8 blocks
+        pb[c][0] = transpose8x8(pack_f16(y[0], y[1]));
+        pb[c][1] = transpose8x8(pack_f16(y[2], y[3]));
+      }
+      // ---- O^T += V^T P^T: this lane's keys are key_of(2 t4), key_of(2 t4 + 1) = t4, t4 + 4 of both 8-key groups, its features
+      // g * hd / 8 ..; two keys share a word's nibbles, low and high
+      uint32_t vw[4][W / 2], sv2[2];
+      uint32_t sb[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * h + (r >> 1) * 8 + t4 + (r & 1) * 4;
+        if (HD == 128) {
+          const uint2 v = lds64(sv + v_chunk<HD>(row, g >> 1) + (g & 1) * 8);
+          vw[r][0] = v.x; vw[r][W / 2 - 1] = v.y;
+        } else {
+          vw[r][0] = lds32(sv + row * (HD / 2) + g * 4);
+        }
+        sb[r] = lds8(ssv + row * (HD / 16) + (HD == 128 ? g : g >> 1));
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) sv2[k] = e4m3x2_to_f16x2(static_cast<uint16_t>(sb[2 * k] | (sb[2 * k + 1] << 8)));
+#pragma unroll
+      for (int j = 0; j < W / 2; ++j) {
+        uint32_t even[2][4], odd[2][4];  // [8-key group]: features 8 j + 2 n and 8 j + 2 n + 1 of two keys
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t w0 = vw[2 * k][j], w1 = vw[2 * k + 1][j];
+          e2m1_to_f16((w0 & 0x0f0f0f0fu) | ((w1 << 4) & 0xf0f0f0f0u), even[k]);
+          e2m1_to_f16(((w0 >> 4) & 0x0f0f0f0fu) | (w1 & 0xf0f0f0f0u), odd[k]);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) { even[k][n] = mul_f16x2(even[k][n], sv2[k]); odd[k][n] = mul_f16x2(odd[k][n], sv2[k]); }
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) mma_f16(o_acc[c][4 * j + n], even[0][n], odd[0][n], even[1][n], odd[1][n], pb[c][0], pb[c][1]);
+      }
+    }
+    __syncwarp();  // every lane has read this stage before it is refilled
+  }
+  ptx::cp_async_wait<0>();
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) l_sum[c][h] += __shfl_xor_sync(0xffffffffu, l_sum[c][h], o);
+  __syncthreads();  // every warp has left its ring: the memory is reused for the merge
+
+  float* mrg = reinterpret_cast<float*>(smem);
+  constexpr int RS = HD + 2;
+  const float o_unit = P_UNIT * pow2f(kv4_exp(a.c.v_exp, kvh));
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int col = c * 8 + t4 * 2 + h;
+      if (col < n_cols) {
+        float* dst_row = mrg + (warp * 16 + col) * RS;
+#pragma unroll
+        for (int n = 0; n < MT; ++n) {
+          dst_row[g * (HD / 8) + 2 * n] = o_acc[c][n][h] * o_unit;
+          dst_row[g * (HD / 8) + 2 * n + 1] = o_acc[c][n][2 + h] * o_unit;
+        }
+        if (g == 0) { dst_row[HD] = m_ref[c][h]; dst_row[HD + 1] = l_sum[c][h] * P_UNIT; }
+      }
+    }
+  }
+  const bool nans = MULTI ? __syncthreads_or(nan_seen) : (__syncthreads(), false);
+  for (int idx = tid; idx < n_cols * HD; idx += KA_THREADS) {
+    const int r = idx / HD, d = idx - r * HD;
+    float m = -CUDART_INF_F;
+#pragma unroll
+    for (int w = 0; w < KA_WARPS; ++w) m = fmaxf(m, mrg[(w * 16 + r) * RS + HD]);
+    const float m_use = m == -CUDART_INF_F ? 0.f : m;
+    float l = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < KA_WARPS; ++w) {
+      const float* src = mrg + (w * 16 + r) * RS;
+      const float f = exp2f(src[HD] - m_use);  // 0 for a warp that saw no key
+      l += src[HD + 1] * f;
+      o += src[d] * f;
+    }
+    const size_t row = out_row(r);
+    if (MULTI && nans) {
+      for (int key = max(pos0 + 1, k_begin); key <= min(pos0 + token_of(r), k_end - 1); ++key) {
+        const int id = table[key >> l2p];
+        if (static_cast<unsigned>(id) >= static_cast<unsigned>(a.c.n_pages)) continue;
+        const size_t at = ((static_cast<size_t>(id) * a.n_kv_heads + kvh) << l2p) + (key & ((1 << l2p) - 1));
+        if ((a.c.v_scale[at * (HD / 16) + d / 16] & 0x7f) == 0x7f) o = CUDART_NAN_F;
+      }
+    }
+    if (a.n_splits == 1) {
+      a.o[row * HD + d] = __float2bfloat16(l == 0.f ? 0.f : o / l);  // (no visible entry: zeros)
+    } else {
+      a.parts.o[(part_row0 + row) * HD + d] = o;
+      if (d == 0) a.parts.ml[part_row0 + row] = make_float2(m, l);
+    }
+  }
+}
+
+template <int HD, bool WIDE, bool MULTI>
+pd_status launch_kv4(const Kv4DecodeArgs& a, int slots, cudaStream_t s) {
+  using SM = Kv4Smem<HD>;
+  static PerDeviceInt smem_opt_in;
+  PD_TRY(opt_in_smem(smem_opt_in, kv4_decode_kernel<HD, WIDE, MULTI>, SM::BYTES));
+  PD_CUDA_TRY(launch_pdl(kv4_decode_kernel<HD, WIDE, MULTI>, dim3(a.n_splits, a.n_kv_heads, slots), dim3(KA_THREADS), SM::BYTES, s, a));
+  count_launch();
+  if (a.n_splits > 1) return launch_paged_join(a.parts, a.o, 1ll * a.rows * a.n_q_heads, a.n_splits, HD, s);
+  return PD_OK;
+}
+template <int HD>
+pd_status launch_kv4(const Kv4DecodeArgs& a, int slots, cudaStream_t s) {
+  const bool wide = a.block_tokens * (a.n_q_heads / a.n_kv_heads) > 8;
+  if (a.n_new > 1) return wide ? launch_kv4<HD, true, true>(a, slots, s) : launch_kv4<HD, false, true>(a, slots, s);
+  return wide ? launch_kv4<HD, true, false>(a, slots, s) : launch_kv4<HD, false, false>(a, slots, s);
+}
+
+// Tokens of a block: eight columns where the tokens of a sequence fit them (half the registers), else sixteen.
+int kv4_block_tokens(int group, int n_new) { return group * n_new <= 8 ? n_new : std::min(n_new, 16 / group); }
+
+// Key ranges are cut into equal parts while there are fewer blocks than run together, into parts of at least KA_MIN_CHUNK keys
+// and at most `longest` keys.  The sequences of a batch may differ in length, which the host does not know, so a part is at most
+// 4096 keys, and from about one block per SM on half as many parts again as run together even the lengths out.  No more
+// than 16 parts are made for the length alone, since max_kv_len may be a capacity far above the lengths.
+struct Split { int n, chunk; };
+int kv4_most_blocks(long long blocks) { return blocks <= 148 ? KA_RESIDENT : KA_RESIDENT * 3 / 2; }
+Split kv4_split(long long slots, int n_kv_heads, int max_kv_len) {
+  const long long blocks = slots * n_kv_heads;
+  const long long want = std::max(1ll, kv4_most_blocks(blocks) / blocks);
+  long long chunk = (max_kv_len + want - 1) / want;
+  chunk = std::min(chunk, slots > 1 ? std::max(4096ll, max_kv_len / 16ll) : static_cast<long long>(max_kv_len));
+  chunk = std::min((std::max<long long>(chunk, KA_MIN_CHUNK) + 63) / 64 * 64, 0x7fffffc0ll);
+  return {static_cast<int>((max_kv_len + chunk - 1) / chunk), static_cast<int>(chunk)};
+}
+// (part, row) pairs, row = (token, query head), that any call of up to these sizes has at most, where it has parts at all: a
+// buffer of that size serves every smaller call, too.  Parts made to fill the GPU are at most as many as kv4_split asks for,
+// of at least KA_MIN_CHUNK keys and at most 16 rows; parts made for their length are as many as the bound allows.
+long long kv4_most_part_rows(int batch, int n_new, int n_q_heads, int n_kv_heads, int max_kv_len) {
+  if (batch <= 0 || n_new <= 0 || max_kv_len <= KA_MIN_CHUNK) return 0;
+  const int group = n_q_heads / n_kv_heads;
+  const long long tokens = std::min(n_new, std::max(16 / group, 1));   // of a block at most
+  const long long by_length = (max_kv_len + (KA_MIN_CHUNK - 1ll)) / KA_MIN_CHUNK;
+  const long long fill = std::min(KA_RESIDENT * 3ll / 2 / n_kv_heads * tokens, by_length * batch * n_new);
+  // (17: of max_kv_len / 16 keys, rounded down, and what is left)
+  const long long length = std::min(17ll, (max_kv_len + 4095ll) / 4096);
+  return std::max(fill, length > 1 ? length * batch * n_new : 0) * n_q_heads;
+}
+
+}  // namespace
+}  // namespace pd
+
+extern "C" pd_status pd_paged_kv4_decode_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t B, int32_t n_new, int32_t max_kv_len,
+                                                                   size_t* out_bytes) {
+  PD_TRY(pd::check_kv4_heads(cfg));
+  if (!out_bytes || B < 0 || n_new < 1 || max_kv_len < 0) return PD_ERR_INVALID_ARG;
+  const long long rows = pd::kv4_most_part_rows(B, n_new, cfg->n_q_heads, cfg->n_kv_heads, max_kv_len);
+  *out_bytes = rows ? pd::paged_parts_bytes(static_cast<size_t>(rows), cfg->head_dim) : 0;
+  return PD_OK;
+}
+
+extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, const void* q, int32_t ldq, void* out,
+                                                   const int32_t* kv_len_dev, int32_t B, int32_t n_new, int32_t max_kv_len,
+                                                   const pd_paged_kv4_cache* cache, void* workspace, size_t workspace_bytes,
+                                                   int32_t* err_word, void* stream) {
+  using namespace pd;
+  PD_TRY(check_kv4_heads(cfg));
+  Kv4DecodeArgs a{};
+  PD_TRY(kv4_cache_view(cache, &a.c));
+  if (B < 0 || B > cache->n_seqs || n_new < 1) return PD_ERR_INVALID_ARG;
+  if (B == 0) return PD_OK;
+  if (!q || !out || !kv_len_dev || ldq < 1ll * cfg->n_q_heads * cfg->head_dim || ldq % 8 != 0) return PD_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(q) & 15u) || (reinterpret_cast<uintptr_t>(out) & 1u)) return PD_ERR_INVALID_ARG;
+  if (max_kv_len < n_new || max_kv_len > (cache->table_ld << a.c.log2_page)) return PD_ERR_INVALID_ARG;
+  a.block_tokens = kv4_block_tokens(cfg->n_q_heads / cfg->n_kv_heads, n_new);
+  a.seq_blocks = (n_new + a.block_tokens - 1) / a.block_tokens;
+  const long long slots = 1ll * B * a.seq_blocks;
+  if (slots > 65535) return PD_ERR_UNSUPPORTED_SHAPE;
+  a.rows = B * n_new;
+  const Split sp = kv4_split(slots, cfg->n_kv_heads, max_kv_len);
+  a.n_splits = sp.n; a.chunk = sp.chunk;
+  if (a.n_splits > 1) {
+    const size_t part_rows = static_cast<size_t>(a.n_splits) * a.rows * cfg->n_q_heads;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PD_ERR_INVALID_ARG;
+    if (workspace_bytes < paged_parts_bytes(part_rows, cfg->head_dim)) return PD_ERR_WORKSPACE_TOO_SMALL;
+    a.parts.o = static_cast<float*>(workspace);
+    a.parts.ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + paged_parts_ml_offset(part_rows, cfg->head_dim));
+  }
+  a.q = static_cast<const bf16*>(q); a.o = static_cast<bf16*>(out); a.kv_len = kv_len_dev; a.err_word = err_word;
+  a.ldq = ldq; a.n_new = n_new; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  TraceScope ts(PD_K_ATTN_DECODE, st);
+  return cfg->head_dim == 128 ? launch_kv4<128>(a, static_cast<int>(slots), st) : launch_kv4<64>(a, static_cast<int>(slots), st);
+}

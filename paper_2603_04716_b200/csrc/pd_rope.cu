@@ -1,0 +1,172 @@
+// Rotary positions scaled for long contexts (pd_rope_table_scaled) and the transform of q and k heads in front of attention
+// (pd_qk_norm_rope).
+#include <cmath>
+
+#include "pd_kv4.cuh"
+
+namespace pd {
+namespace {
+
+// ------------------------------------------------------------------------------------------------------------------ table
+// A thread computes `run` neighbouring positions of one pair: cos and sin of the first from the angle in half turns (product
+// and reduction in double), the others by turning on, 4 fused operations instead of a reduction and two polynomials each.
+// Angles are theirs to 2^-50 relative; 16 steps add 2^-48 at most, far below the final rounding to fp32.
+struct TableArgs {
+  double half_turns[64], c[64], s[64];  // f_i / pi, cos f_i, sin f_i
+  double magnitude;
+  float2* out;  // [n_pos, pairs]
+  int first, n_pos, pairs, run;
+};
+constexpr int TB_THREADS = 256;
+
+__global__ void __launch_bounds__(TB_THREADS) rope_table_kernel(const __grid_constant__ TableArgs a) {
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+  const long long item = 1ll * blockIdx.x * TB_THREADS + threadIdx.x;
+  const int i = static_cast<int>(item % a.pairs);
+  const long long p0 = item / a.pairs * a.run;
+  if (p0 >= a.n_pos) return;
+  const int n = static_cast<int>(min(1ll * a.run, a.n_pos - p0));
+  double s, c;
+  sincospi(static_cast<double>(a.first + p0) * a.half_turns[i], &s, &c);
+  c *= a.magnitude;
+  s *= a.magnitude;
+  const double dc = a.c[i], ds = a.s[i];
+  float2* out = a.out + p0 * a.pairs + i;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) {
+    out[static_cast<size_t>(k) * a.pairs] = make_float2(static_cast<float>(c), static_cast<float>(s));
+    const double c1 = c * dc - s * ds;
+    s = s * dc + c * ds;
+    c = c1;
+  }
+}
+
+// Frequencies of the pairs, in radians per position.
+void rope_frequencies(const pd_rope_cfg& r, double* f) {
+  const int pairs = r.rot_dim / 2;
+  const double pi = 3.14159265358979323846;
+  double theta = r.theta;
+  if (r.scaling == PD_ROPE_SCALE_BASE) theta *= std::pow(r.factor, r.rot_dim / (r.rot_dim - 2.0));
+  double a = 0, b = 0;
+  if (r.scaling == PD_ROPE_SCALE_INDEX) {
+    auto pair_of = [&](double turns) { return r.rot_dim * std::log(r.trained_len / (2 * pi * turns)) / (2 * std::log(theta)); };
+    a = std::fmax(std::floor(pair_of(r.high)), 0.0);
+    b = std::fmin(std::ceil(pair_of(r.low)), pairs - 1.0);
+  }
+  for (int i = 0; i < pairs; ++i) {
+    f[i] = std::pow(theta, -2.0 * i / r.rot_dim);
+    double keep = 1.0;
+    if (r.scaling == PD_ROPE_SCALE_LINEAR) keep = 0.0;
+    if (r.scaling == PD_ROPE_SCALE_TURNS) keep = (r.trained_len * f[i] / (2 * pi) - r.low) / (r.high - r.low);
+    if (r.scaling == PD_ROPE_SCALE_INDEX) keep = 1.0 - (i - a) / std::fmax(b - a, 1e-3);
+    keep = std::fmin(std::fmax(keep, 0.0), 1.0);
+    if (keep < 1.0) f[i] = keep * f[i] + (1.0 - keep) * f[i] / r.factor;
+  }
+}
+
+// -------------------------------------------------------------------------------------------------------------- q and k
+// HBM-bound at size, by launch and the latency of two loads (position, angles) below that.  hd / 16 lanes have a head of a row,
+// four heads of it one after the other with all loads in flight; blocks along y are groups of heads, so that a small batch
+// still covers the SMs.
+struct NormArgs {
+  const bf16* qkv;
+  bf16* q_out;
+  bf16* k_out;
+  const int32_t* positions;
+  int* err_word;
+  QkTransform t;
+  int ldqkv, ldq, ldk, rows, n_q_heads, n_kv_heads, q_blocks;
+};
+constexpr int NR_THREADS = 256;
+constexpr int NR_HEADS = 4;
+
+template <int HD, bool PAIRS>
+__global__ void __launch_bounds__(NR_THREADS) qk_norm_rope_kernel(const NormArgs a) {
+  constexpr int J = HD / 16;
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+  const int row = blockIdx.x * (NR_THREADS / J) + threadIdx.x / J, j = threadIdx.x % J;
+  const int pos = row < a.rows ? a.positions[row] : -1;
+  const bool far = a.t.rot > 0 && pos >= a.t.n_pos;
+  if (far && j == 0) report_place(a.err_word);
+  const bool live = pos >= 0 && !far;
+  const HeadShare<PAIRS> at(j, a.t.rot);
+  const float2* angles = a.t.table + static_cast<size_t>(live ? pos : 0) * (a.t.rot / 2);
+  const bool is_q = static_cast<int>(blockIdx.y) < a.q_blocks;
+  const int h0 = (is_q ? blockIdx.y : blockIdx.y - a.q_blocks) * NR_HEADS;
+  const size_t r = live ? row : 0;
+  const bf16* src = a.qkv + r * a.ldqkv + (is_q ? h0 : a.n_q_heads + h0) * HD;
+  bf16* dst = is_q ? a.q_out + r * a.ldq + h0 * HD : a.k_out + r * a.ldk + h0 * HD;
+  transform_heads<HD, PAIRS, NR_HEADS>(src, dst, (is_q ? a.n_q_heads : a.n_kv_heads) - h0, live, at, is_q ? a.t.q_gain : a.t.k_gain,
+                                       a.t.eps, angles, j);
+}
+
+}  // namespace
+}  // namespace pd
+
+extern "C" pd_status pd_rope_table_scaled(const pd_rope_cfg* rope, int32_t first_pos, int32_t n_pos, float* table, void* stream) {
+  using namespace pd;
+  if (!rope || rope->struct_size != sizeof(pd_rope_cfg)) return PD_ERR_INVALID_ARG;
+  if (rope->rot_dim <= 0 || rope->scaling < PD_ROPE_SCALE_NONE || rope->scaling > PD_ROPE_SCALE_INDEX) return PD_ERR_INVALID_ARG;
+  if (rope->rot_dim % 16 != 0 || rope->rot_dim > 128) return PD_ERR_UNSUPPORTED_SHAPE;
+  if (!(rope->theta > 1.0) || !std::isfinite(rope->theta) || !(rope->magnitude > 0.0) || !std::isfinite(rope->magnitude)) return PD_ERR_INVALID_ARG;
+  if (rope->scaling != PD_ROPE_SCALE_NONE && (!(rope->factor >= 1.0) || !std::isfinite(rope->factor))) return PD_ERR_INVALID_ARG;
+  if (rope->scaling >= PD_ROPE_SCALE_TURNS &&
+      (!(rope->low > 0.0) || !(rope->high > rope->low) || !std::isfinite(rope->high) || rope->trained_len < 1))
+    return PD_ERR_INVALID_ARG;
+  if (first_pos < 0 || n_pos < 0 || n_pos > 0x7fffffff - first_pos) return PD_ERR_INVALID_ARG;
+  if (n_pos == 0) return PD_OK;
+  if (!table || (reinterpret_cast<uintptr_t>(table) & 7u)) return PD_ERR_INVALID_ARG;
+  TableArgs a{};
+  double f[64];
+  rope_frequencies(*rope, f);
+  a.pairs = rope->rot_dim / 2;
+  for (int i = 0; i < a.pairs; ++i) {
+    a.half_turns[i] = f[i] / 3.14159265358979323846;
+    a.c[i] = std::cos(f[i]);
+    a.s[i] = std::sin(f[i]);
+  }
+  a.magnitude = rope->magnitude; a.out = reinterpret_cast<float2*>(table);
+  a.first = first_pos; a.n_pos = n_pos;
+  // long runs where there are threads enough for every SM all the same
+  a.run = 1ll * n_pos * a.pairs >= (1ll << 22) ? 16 : 4;
+  const long long items = (n_pos + (a.run - 1ll)) / a.run * a.pairs, blocks = (items + TB_THREADS - 1) / TB_THREADS;
+  if (blocks > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
+  PD_CUDA_TRY(launch_pdl(rope_table_kernel, dim3(static_cast<unsigned>(blocks)), dim3(TB_THREADS), 0, static_cast<cudaStream_t>(stream), a));
+  count_launch();
+  return PD_OK;
+}
+
+extern "C" pd_status pd_qk_norm_rope(const pd_layer_cfg* cfg, const pd_qk_transform* transform, const void* qkv, int32_t ldqkv,
+                                     void* q_out, int32_t ldq_out, void* k_out, int32_t ldk_out, const int32_t* positions, int32_t T,
+                                     int32_t* err_word, void* stream) {
+  using namespace pd;
+  PD_TRY(check_kv4_heads(cfg));
+  NormArgs a{};
+  PD_TRY(qk_transform_view(transform, cfg, &a.t));
+  if (T < 0) return PD_ERR_INVALID_ARG;
+  if (T == 0 || (!q_out && !k_out)) return PD_OK;
+  const int hd = cfg->head_dim;
+  if (1ll * (cfg->n_q_heads + cfg->n_kv_heads) * hd > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
+  if (!qkv || !positions || ldqkv < (cfg->n_q_heads + cfg->n_kv_heads) * hd || ldqkv % 8 != 0) return PD_ERR_INVALID_ARG;
+  if (q_out && (ldq_out < cfg->n_q_heads * hd || ldq_out % 8 != 0)) return PD_ERR_INVALID_ARG;
+  if (k_out && (ldk_out < cfg->n_kv_heads * hd || ldk_out % 8 != 0)) return PD_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(qkv) | reinterpret_cast<uintptr_t>(q_out) | reinterpret_cast<uintptr_t>(k_out)) & 15u)
+    return PD_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(positions) & 3u) return PD_ERR_INVALID_ARG;
+  a.qkv = static_cast<const bf16*>(qkv); a.q_out = static_cast<bf16*>(q_out); a.k_out = static_cast<bf16*>(k_out);
+  a.positions = positions; a.err_word = err_word;
+  a.ldqkv = ldqkv; a.ldq = ldq_out; a.ldk = ldk_out; a.rows = T; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
+  a.q_blocks = q_out ? (cfg->n_q_heads + NR_HEADS - 1) / NR_HEADS : 0;
+  const int y = a.q_blocks + (k_out ? (cfg->n_kv_heads + NR_HEADS - 1) / NR_HEADS : 0);
+  const int rows_per_block = NR_THREADS / (hd / 16);
+  const dim3 grid((T + (rows_per_block - 1ll)) / rows_per_block, y), block(NR_THREADS);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, st, a); };
+  const bool pairs = transform->layout == PD_ROPE_PAIRS;
+  PD_CUDA_TRY(hd == 128 ? (pairs ? go(qk_norm_rope_kernel<128, true>) : go(qk_norm_rope_kernel<128, false>))
+                        : (pairs ? go(qk_norm_rope_kernel<64, true>) : go(qk_norm_rope_kernel<64, false>)));
+  count_launch();
+  return PD_OK;
+}
