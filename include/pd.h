@@ -543,7 +543,7 @@ typedef struct {
  *   q_out      device bf16 [T, ldq_out], Hq * hd columns written; NULL: q is left alone.  May be qkv with ldq_out = ldqkv
  *   k_out      device bf16 [T, ldk_out], Hkv * hd columns written; NULL: k is left alone.  May be qkv + Hq * hd with
  *              ldk_out = ldqkv
- *   positions  device int32 [T]; a negative one leaves its row out (it is neither read nor written)
+ *   positions  device int32 [T]; a negative one leaves its row out (nothing is written)
  *   err_word   optional device int32, set to 2 where a position lies beyond the table (the row is left out)
  * Outputs that overlap qkv in any other way, or each other, are undefined.  Tensors start on 16-byte boundaries, pitches are
  * multiples of 8.  fp32 arithmetic, rounded once; the squares of a head must sum to less than 3e38.  Only head_dim and the head counts of cfg
@@ -585,7 +585,7 @@ typedef struct {
  *   q_out        transformed q, device bf16 [T, Hq*hd] contiguous, not overlapping qkv; NULL: only the cache is written
  *   cu_seqlens   as for pd_prefill_layer (device and host copy); both NULL: one row per request (a decode step)
  *   kv_len_dev   device int32[n_req]: tokens that sequence r holds already; its rows take positions kv_len[r],
- *                kv_len[r] + 1, ...  A negative value leaves the request out: none of its rows is read, written or cached.
+ *                kv_len[r] + 1, ...  A negative value leaves the request out: nothing is written or cached for its rows.
  *                kv_len itself is not modified
  *   err_word     optional device int32, set to 2 where a row has no place: a position beyond the page table or a page number
  *                outside the pool (q is still written, k and v are left out); a position beyond the rotation table (the row is left out)

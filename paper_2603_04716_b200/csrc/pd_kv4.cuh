@@ -139,64 +139,72 @@ __device__ __forceinline__ void turn(T (&f)[16], const float (&cs)[16]) {
     x = u; y = w;
   }
 }
-template <int LANES, class T>
-__device__ __forceinline__ T lanes_sum(T v) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-// RMSNorm (where there is a gain) and rotation of a lane's share of a head, in the precision of T.  All lanes of a warp call it.
+// RMSNorm (where there is a gain) and rotation of a lane's share of a head, in the precision of T, times `unit`.  The factor that
+// the norm has in common comes last: x * gain is exact in fp32, and in double so are its products with cos and sin.  All
+// lanes of a warp call it.
 template <int HD, bool PAIRS, class T>
 __device__ __forceinline__ void transform_share(const uint4 (&w)[2], bool norm, const uint4 (&gain)[2], double eps, bool turns,
-                                                const float (&cs)[16], T (&f)[16]) {
+                                                const float (&cs)[16], T unit, T (&f)[16]) {
   float x[16];
   unpack8(w[0], x);
   unpack8(w[1], x + 8);
 #pragma unroll
   for (int e = 0; e < 16; ++e) f[e] = static_cast<T>(x[e]);
   if (norm) {  // (the same for all lanes)
-    T sum = 0;
+    T sum[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sum = fma(f[e], f[e], sum);
-    sum = lanes_sum<HD / 16>(sum);
-    const T r = rsqrt(sum * static_cast<T>(1.0 / HD) + static_cast<T>(eps));
-    unpack8(gain[0], x);
-    unpack8(gain[1], x + 8);
+    for (int e = 0; e < 16; ++e) sum[e & 3] = fma(f[e], f[e], sum[e & 3]);
+    T all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) f[e] = f[e] * r * static_cast<T>(x[e]);
+    for (int o = HD / 32; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    unit *= rsqrt(all * static_cast<T>(1.0 / HD) + static_cast<T>(eps));
+    float g[16];
+    unpack8(gain[0], g);
+    unpack8(gain[1], g + 8);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] *= static_cast<T>(g[e]);
   }
   if (turns) turn<PAIRS>(f, cs);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) f[e] *= unit;
 }
-// NH heads (n_h of them there are) of one row in fp32, rounded to bf16 once; all loads go out before the first use.
+// NH heads (n_h of them there are) of one row in fp32, rounded to bf16 once.  The row is read before anything else is known
+// (`there`: it exists); `live`, the angles' row and the rest of the work wait for the position.
 template <int HD, bool PAIRS, int NH>
-__device__ __forceinline__ void transform_heads(const bf16* src, bf16* dst, int n_h, bool live, const HeadShare<PAIRS>& at, const bf16* gain,
-                                                double eps, const float2* angles, int j) {
-  uint4 w[NH][2], g[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+struct HeadsOfRow {
+  uint4 w[NH][2];
+  __device__ __forceinline__ HeadsOfRow(const bf16* src, int n_h, bool there, const HeadShare<PAIRS>& at) {
 #pragma unroll
-  for (int h = 0; h < NH; ++h) {
-    w[h][0] = w[h][1] = make_uint4(0, 0, 0, 0);
-    if (live && h < n_h) load_share(src + h * HD, at.a, at.b, w[h]);
-  }
-  float cs[16] = {};
-  if (live && at.turns) load_angles(angles, j, cs);
-  if (gain) load_share(gain, at.a, at.b, g);
-#pragma unroll
-  for (int h = 0; h < NH; ++h) {
-    float f[16];
-    transform_share<HD, PAIRS>(w[h], gain != nullptr, g, eps, at.turns, cs, f);
-    if (live && h < n_h) {
-      *reinterpret_cast<uint4*>(dst + h * HD + at.a) = pack8(f);
-      *reinterpret_cast<uint4*>(dst + h * HD + at.b) = pack8(f + 8);
+    for (int h = 0; h < NH; ++h) {
+      w[h][0] = w[h][1] = make_uint4(0, 0, 0, 0);
+      if (there && h < n_h) load_share(src + h * HD, at.a, at.b, w[h]);
     }
   }
-}
+  __device__ __forceinline__ void transform(bf16* dst, int n_h, bool live, const HeadShare<PAIRS>& at, const bf16* gain, double eps,
+                                            const float2* angles, int j) {
+    uint4 g[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    float cs[16] = {};
+    if (live && at.turns) load_angles(angles, j, cs);
+    if (gain) load_share(gain, at.a, at.b, g);
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      float f[16];
+      transform_share<HD, PAIRS>(w[h], gain != nullptr, g, eps, at.turns, cs, 1.f, f);
+      if (live && h < n_h) {
+        *reinterpret_cast<uint4*>(dst + h * HD + at.a) = pack8(f);
+        *reinterpret_cast<uint4*>(dst + h * HD + at.b) = pack8(f + 8);
+      }
+    }
+  }
+};
 
 // ------------------------------------------------------------------------------------------------------------ quantiser
 // A double as the float that compares the same with every number of at most 23 significant bits: rounded toward zero, the last
 // bit set if anything was lost.  Borders of the two formats times a scale have a handful of bits, so decisions are exact.
+// (Below 2^-126 nothing is decided.)
 __device__ __forceinline__ float sticky_float(double d) {
-  const float f = __double2float_rz(d);
-  return static_cast<double>(f) == d ? f : __uint_as_float(__float_as_uint(f) | 1u);
+  const uint32_t lost = static_cast<uint32_t>(__double2loint(d)) & 0x1fffffffu;
+  return __uint_as_float(__float_as_uint(__double2float_rz(d)) | (lost ? 1u : 0u));
 }
 // Largest magnitude of 8 values; NaN if one is infinite or NaN.
 __device__ __forceinline__ float chunk_max(const float* t) {
@@ -205,10 +213,16 @@ __device__ __forceinline__ float chunk_max(const float* t) {
   for (int e = 0; e < 8; ++e) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(fabsf(t[e])));
   return m <= 3.402823466e38f ? m : __int_as_float(0x7fc00000);
 }
-// The E4M3 scale of 16 values from their largest magnitude.  The quotient is rounded to the nearest float, which cannot move it
-// onto a border of E4M3 that it does not lie on (the border times 6 is a float, and amax differs from that by one step at least).
+// t / d by an approximate reciprocal, corrected by the exact remainder: the float nearest to within 2^-20 of a step.  That cannot
+// move it onto a border b of the formats that it does not lie on, or off one that it does: b * d is a float, t differs from it by
+// one step at least, and d has at most four significant bits, so the quotients differ by more than half a step of b.
+__device__ __forceinline__ float quotient(float t, float d, float inv) {
+  const float p = __fmul_rn(t, inv);
+  return __fmaf_rn(__fmaf_rn(-p, d, t), inv, p);
+}
+// The E4M3 scale of 16 values from their largest magnitude.
 __device__ __forceinline__ uint32_t kv4_scale(float amax) {
-  return amax == amax ? ptx::cvt_e4m3x2(__fdiv_rn(amax, 6.f), 0.f) : 0x7fu;
+  return amax == amax ? ptx::cvt_e4m3x2(quotient(amax, 6.f, 1.f / 6.f), 0.f) : 0x7fu;
 }
 __device__ __forceinline__ float e4m3_value(uint32_t code) {
   uint32_t h;
@@ -217,19 +231,17 @@ __device__ __forceinline__ float e4m3_value(uint32_t code) {
   asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.f32.f16 %0, lo; }" : "=f"(f) : "r"(h));
   return f;
 }
-// Eight values over a scale -> eight E2M1 codes, value i in bits 4 i .. 4 i + 3.  The quotient is the correctly rounded one: the
-// product with the nearest reciprocal, corrected by its exact remainder.
+// Eight values over a scale -> eight E2M1 codes, value i in bits 4 i .. 4 i + 3.
 __device__ __forceinline__ uint32_t kv4_codes(const float* t, float scale) {
-  const float inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
+  float inv;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+  if (!(scale > 0.f)) inv = 0.f;
   uint32_t r = 0;
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     float q[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float p = __fmul_rn(t[e + i], inv);
-      q[i] = __fmaf_rn(__fmaf_rn(-p, scale, t[e + i]), inv, p);
-    }
+    for (int i = 0; i < 2; ++i) q[i] = quotient(t[e + i], scale, inv);
     uint32_t c;
     asm("{ .reg .b8 c; .reg .b16 h; cvt.rn.satfinite.e2m1x2.f32 c, %1, %2; cvt.u16.u8 h, c; cvt.u32.u16 %0, h; }"
         : "=r"(c) : "f"(q[1]), "f"(q[0]));

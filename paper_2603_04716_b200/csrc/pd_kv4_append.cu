@@ -58,63 +58,68 @@ __device__ __forceinline__ long long pool_row(const Kv4Cache& c, int seq, int po
   return ((1ll * page * n_kv_heads + kvh) << c.log2_page) + (pos & ((1 << c.log2_page) - 1));
 }
 
-// Blocks along y are groups of query heads, then KV heads with their K and V.
+// Blocks along y are groups of query heads, then K heads, then V heads.
 template <int HD, bool PAIRS>
-__global__ void __launch_bounds__(KW_THREADS, 2) kv4_append_kernel(const Kv4AppendArgs a) {
+__global__ void __launch_bounds__(KW_THREADS, 3) kv4_append_kernel(const Kv4AppendArgs a) {
   constexpr int J = HD / 16;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
   const int row = blockIdx.x * (KW_THREADS / J) + threadIdx.x / J, j = threadIdx.x % J;
-  int req = row, first = row;
-  if (a.cu_seqlens) {
-    req = request_of<J>(a.cu_seqlens, a.n_req, row);
-    if (req < a.n_req) first = a.cu_seqlens[req];
-  }
-  const bool there = row < a.n_tokens && req < a.n_req;
-  const int len = there ? a.kv_len[req] : -1;
-  const long long p = 1ll * len + (row - first);
-  const bool far = len >= 0 && (a.t.rot > 0 ? p >= a.t.n_pos : p > 0x7fffffffll);
-  const bool live = len >= 0 && !far;
-  const int pos = live ? static_cast<int>(p) : 0;
   const HeadShare<PAIRS> at(j, a.t.rot);
-  const bf16* src = a.qkv + static_cast<size_t>(live ? row : 0) * a.ldqkv;
-  const float2* angles = a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2);
-
-  if (static_cast<int>(blockIdx.y) < a.q_blocks) {
-    const int h0 = blockIdx.y * KW_Q_HEADS;
-    bf16* dst = a.q_out + static_cast<size_t>(live ? row : 0) * (a.n_q_heads * HD) + h0 * HD;
-    transform_heads<HD, PAIRS, KW_Q_HEADS>(src + h0 * HD, dst, a.n_q_heads - h0, live, at, a.t.q_gain, a.t.eps, angles, j);
+  const bf16* const src = a.qkv + static_cast<size_t>(row < a.n_tokens ? row : 0) * a.ldqkv;
+  const int kv_block = static_cast<int>(blockIdx.y) - a.q_blocks;  // below 0: query heads
+  // the row goes out first, its place is looked up meanwhile
+  int req = row, first = row, len = -1;
+  auto find_request = [&] {
+    if (a.cu_seqlens) {
+      req = request_of<J>(a.cu_seqlens, a.n_req, row);
+      if (req < a.n_req) first = a.cu_seqlens[req];
+    }
+    if (row < a.n_tokens && req < a.n_req) len = a.kv_len[req];
+  };
+  auto position = [&](bool& live, bool& far) {
+    const long long p = 1ll * len + (row - first);
+    far = len >= 0 && (a.t.rot > 0 ? p >= a.t.n_pos : p > 0x7fffffffll);
+    live = len >= 0 && !far;
+    return live ? static_cast<int>(p) : 0;
+  };
+  bool live, far;
+  if (kv_block < 0) {
+    const int h0 = blockIdx.y * KW_Q_HEADS, n_h = a.n_q_heads - h0;
+    HeadsOfRow<HD, PAIRS, KW_Q_HEADS> heads(src + h0 * HD, n_h, row < a.n_tokens, at);
+    find_request();
+    const int pos = position(live, far);
+    bf16* const dst = a.q_out + static_cast<size_t>(live ? row : 0) * (a.n_q_heads * HD) + h0 * HD;
+    heads.transform(dst, n_h, live, at, a.t.q_gain, a.t.eps, a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j);
     return;
   }
-  const int kvh = blockIdx.y - a.q_blocks;
+  const bool is_v = kv_block >= a.n_kv_heads;
+  const int kvh = is_v ? kv_block - a.n_kv_heads : kv_block;
+  uint4 w[2] = {}, g[2] = {};
+  if (row < a.n_tokens) load_share(src + (a.n_q_heads + kv_block) * HD, at.a, at.b, w);
+  if (!is_v && a.t.k_gain) load_share(a.t.k_gain, at.a, at.b, g);
+  const int exp = kv4_exp(is_v ? a.c.v_exp : a.c.k_exp, kvh);
+  find_request();
+  const int pos = position(live, far);
+  float cs[16] = {};
+  if (!is_v && live && at.turns) load_angles(a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j, cs);
   const long long place = live ? pool_row(a.c, req, pos, a.n_kv_heads, kvh) : -1;
   if ((far || (live && place < 0)) && j == 0) report_place(a.err_word);
-  uint4 k[2] = {}, v[2] = {}, g[2] = {};
-  float cs[16] = {};
-  if (live) {
-    load_share(src + (a.n_q_heads + kvh) * HD, at.a, at.b, k);
-    load_share(src + (a.n_q_heads + a.n_kv_heads + kvh) * HD, at.a, at.b, v);
-    if (at.turns) load_angles(angles, j, cs);
-  }
-  if (a.t.k_gain) load_share(a.t.k_gain, at.a, at.b, g);
-  const int ke = kv4_exp(a.c.k_exp, kvh), ve = kv4_exp(a.c.v_exp, kvh);
-  const size_t at_row = static_cast<size_t>(place < 0 ? 0 : place);
+  const size_t to = static_cast<size_t>(place < 0 ? 0 : place);
   float t[16];
-  unpack8(v[0], t);
-  unpack8(v[1], t + 8);
-  const float v_unit = pow2f(-ve);
+  if (is_v) {
+    unpack8(w[0], t);
+    unpack8(w[1], t + 8);
+    const float unit = pow2f(-exp);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {  // (a finite value stays one, and an infinite one stays infinite)
-    const float x = __fmul_rz(t[e], v_unit);
-    t[e] = x;
+    for (int e = 0; e < 16; ++e) t[e] = __fmul_rz(t[e], unit);  // (a finite value stays one, and an infinite one stays infinite)
+  } else {
+    double f[16];
+    transform_share<HD, PAIRS>(w, a.t.k_gain != nullptr, g, a.t.eps, at.turns, cs, static_cast<double>(pow2f(-exp)), f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t[e] = sticky_float(f[e]);
   }
-  store_kv4<HD, PAIRS>(t, at, j, a.t.rot, place >= 0, a.c.v + at_row * (HD / 2), a.c.v_scale + at_row * (HD / 16));
-  double f[16];
-  transform_share<HD, PAIRS>(k, a.t.k_gain != nullptr, g, a.t.eps, at.turns, cs, f);
-  const double k_unit = static_cast<double>(pow2f(-ke));
-#pragma unroll
-  for (int e = 0; e < 16; ++e) t[e] = sticky_float(f[e] * k_unit);
-  store_kv4<HD, PAIRS>(t, at, j, a.t.rot, place >= 0, a.c.k + at_row * (HD / 2), a.c.k_scale + at_row * (HD / 16));
+  store_kv4<HD, PAIRS>(t, at, j, a.t.rot, place >= 0, (is_v ? a.c.v : a.c.k) + to * (HD / 2), (is_v ? a.c.v_scale : a.c.k_scale) + to * (HD / 16));
 }
 
 // ------------------------------------------------------------------------------- between pages and a contiguous bf16 cache
@@ -284,7 +289,7 @@ extern "C" pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_tr
   a.ldqkv = ldqkv; a.n_req = n_req; a.n_tokens = tokens; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
   a.q_blocks = q_out ? (cfg->n_q_heads + KW_Q_HEADS - 1) / KW_Q_HEADS : 0;
   const int rows = KW_THREADS / (hd / 16);
-  const dim3 grid((tokens + (rows - 1ll)) / rows, a.q_blocks + cfg->n_kv_heads), block(KW_THREADS);
+  const dim3 grid((tokens + (rows - 1ll)) / rows, a.q_blocks + 2 * cfg->n_kv_heads), block(KW_THREADS);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_KV_APPEND, st);
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, st, a); };

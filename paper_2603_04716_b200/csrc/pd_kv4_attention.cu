@@ -34,21 +34,35 @@ struct Kv4DecodeArgs {
   int n_splits, chunk;           // block x covers keys x * chunk .. (the last one whatever lies behind); chunk is a multiple of 64
 };
 
-constexpr int KA_WARPS = 8;
+#ifndef VW
+#define VW 4
+#endif
+#ifndef VS
+#define VS 3
+#endif
+#ifndef VB
+#define VB 4
+#endif
+#ifndef VBW
+#define VBW 2
+#endif
+constexpr int KA_WARPS = VW;
 constexpr int KA_THREADS = KA_WARPS * 32;
 constexpr int KA_KEYS = 32;                     // of a tile: two halves of 16, each within a page
-constexpr int KA_STAGES = 3;
-// p is kept as 2^7 p relative to a reference that may lag the running maximum by 2^8: at most 2^15, below f16's 65504.
-constexpr float P_SHIFT = 7.f, P_SLACK = 8.f, P_UNIT = 1.f / 128.f;
+constexpr int KA_STAGES = VS;
+// p is kept as 2^7 p relative to a reference that may lag the running maximum by 2^6: at most 2^13, with room below f16's 65504 for
+// what 7 - reference loses to rounding where scores are very large.
+constexpr float P_SHIFT = 7.f, P_SLACK = 6.f, P_UNIT = 1.f / 128.f;
 constexpr int KA_MIN_CHUNK = 256;               // keys of a part at least
-constexpr int KA_RESIDENT = 296;                // blocks that run together (half as many WIDE ones)
+constexpr int KA_RESIDENT = 148 * VB;                // blocks that run together (half as many WIDE ones)
 
 template <int HD>
 struct Kv4Smem {
   static constexpr int CODES = KA_KEYS * HD / 2, SCALES = KA_KEYS * HD / 16;  // bytes of a tile's K (or V)
   static constexpr int STAGE = 2 * (CODES + SCALES);                          // K codes, V codes, K scales, V scales
   static constexpr int RING = KA_WARPS * KA_STAGES * STAGE;
-  static constexpr int MERGE = KA_WARPS * 16 * (HD + 2) * 4;
+  static constexpr int MERGE_ROW = HD + 4;                                    // floats: a row of O, then l
+  static constexpr int MERGE = KA_WARPS * 16 * (MERGE_ROW + 1) * 4;           // and m of all rows behind
   static constexpr int BYTES = RING > MERGE ? RING : MERGE;
 };
 
@@ -72,6 +86,13 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same from an accumulator of zeros.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
@@ -120,14 +141,13 @@ __device__ __forceinline__ uint32_t lds8(uint32_t addr) {
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
   return v;
 }
-// 16 bytes to shared memory, of which the first `bytes` are read and the others become zeros.
-__device__ __forceinline__ void cp_async_part(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // WIDE: 9 to 16 columns (two column groups in both products).  MULTI: blocks of several tokens, or of sequences with several.
 template <int HD, bool WIDE, bool MULTI>
-__global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(const Kv4DecodeArgs a) {
+__global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel(const Kv4DecodeArgs a) {
   using SM = Kv4Smem<HD>;
   constexpr int KS = HD / 16;          // k-steps of K Q^T
   constexpr int MT = HD / 16;          // 16-feature tiles of O^T
@@ -211,44 +231,56 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
   // the next batch is fetched a batch ahead
   if (my_tiles > 32) { fetch_pages(32, id_nxt); check_pages(32, id_nxt); }
 
-  // The codes of 16 keys of a page are HD * 8 contiguous bytes, their scales HD.  All rows of a page can be read; keys that do
-  // not count (behind the end, pages that do not exist) get scales of zero instead of whatever is there.
+  // The codes of 16 keys of a page are HD * 8 contiguous bytes, their scales HD; a tile lies in one page unless pages have 16
+  // keys.  All rows of a page can be read, and page 0 stands in for one that does not exist: keys that do not count are masked
+  // later.  Rows of the pool are numbered in 32 bits, so an address is one multiplication.
   constexpr int NLD = HD / 64;
-  uint32_t dst_k[NLD], dst_v[NLD];
-#pragma unroll
-  for (int i = 0; i < NLD; ++i) {
-    const int ch = lane + 32 * i, r = ch / (HD / 32), c = ch % (HD / 32);
-    dst_k[i] = k_chunk<HD>(r, c);
-    dst_v[i] = SM::CODES + v_chunk<HD>(r, c);
-  }
-  // scales: a chunk of 16 bytes per lane, [half][K or V][chunk]
-  constexpr int SC = HD / 16;
-  const int sc_half = lane / (2 * SC), sc_kv = (lane / SC) & 1, sc_chunk = lane % SC;
-  const uint8_t* sc_src = (sc_kv ? a.c.v_scale : a.c.k_scale) + sc_chunk * 16;
-  const uint32_t dst_s = 2 * SM::CODES + sc_kv * SM::SCALES + sc_half * HD + sc_chunk * 16;
+  const uint32_t dst_k = k_chunk<HD>(lane / (HD / 32), lane % (HD / 32));
+  const uint32_t dst_v = SM::CODES + v_chunk<HD>(lane / (HD / 32), lane % (HD / 32));
+  const uint32_t page_rows = static_cast<uint32_t>(a.n_kv_heads) << l2p, head_row = static_cast<uint32_t>(kvh) << l2p;
+  const uint8_t* const k_base = a.c.k + lane * 16;
+  const uint8_t* const v_base = a.c.v + lane * 16;
+  // scales: a chunk of 16 bytes per lane, [K or V][chunk]
+  constexpr int SC = HD / 8;
+  const int sc_kv = (lane / SC) & 1, sc_chunk = lane % SC, sc_half = sc_chunk / (SC / 2);
+  const uint8_t* const s_base = (sc_kv ? a.c.v_scale : a.c.k_scale) + sc_chunk * 16 - (l2p > 4 ? 0 : sc_half * HD);
+  const uint32_t dst_s = 2 * SM::CODES + sc_kv * SM::SCALES + sc_chunk * 16;
   uint32_t valid = 0;  // of the tiles in flight, two bits each (the newest in bits 0-1): halves with keys
-  auto load_tile = [&](int i, int stage) {
+  auto load_tile = [&](int i, uint32_t to) {
     if (i > 0 && (i & 31) == 0) { id_cur[0] = id_nxt[0]; id_cur[1] = id_nxt[1]; }
     const int id0 = __shfl_sync(0xffffffffu, id_cur[0], i & 31), id1 = __shfl_sync(0xffffffffu, id_cur[1], i & 31);
-    const int key0 = key_begin(i);
-    const uint32_t to = ring + stage * SM::STAGE;
     valid = (valid << 2) | (id0 >= 0 ? 1u : 0u) | (id1 >= 0 ? 2u : 0u);
+    const uint32_t row = static_cast<uint32_t>(max(id0, 0)) * page_rows + head_row + (key_begin(i) & ((1 << l2p) - 1));
+    const uint32_t to_k = to + dst_k, to_v = to + dst_v;
+    const uint8_t* const k0 = k_base + static_cast<uint64_t>(row) * (HD / 2);
+    const uint8_t* const v0 = v_base + static_cast<uint64_t>(row) * (HD / 2);
+    if (l2p > 4) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int id = h ? id1 : id0, key = key0 + 16 * h;
-      const size_t row = ((static_cast<size_t>(max(id, 0)) * a.n_kv_heads + kvh) << l2p) + (key & ((1 << l2p) - 1));
-      const size_t at = row * (HD / 2) + lane * 16;
+      for (int n = 0; n < 2 * NLD; ++n) {
+        cp_async(to_k + 512 * n, k0 + 512 * n);
+        cp_async(to_v + 512 * n, v0 + 512 * n);
+      }
+      if (lane < 2 * SC) cp_async(to + dst_s, s_base + static_cast<uint64_t>(row) * (HD / 16));
+    } else {
+      const uint32_t row1 = static_cast<uint32_t>(max(id1, 0)) * page_rows + head_row;
+      const uint8_t* const k1 = k_base + static_cast<uint64_t>(row1) * (HD / 2);
+      const uint8_t* const v1 = v_base + static_cast<uint64_t>(row1) * (HD / 2);
 #pragma unroll
       for (int n = 0; n < NLD; ++n) {
-        ptx::cp_async_16(to + h * (HD * 8) + dst_k[n], a.c.k + at + 512 * n, true);
-        ptx::cp_async_16(to + h * (HD * 8) + dst_v[n], a.c.v + at + 512 * n, true);
+        cp_async(to_k + 512 * n, k0 + 512 * n);
+        cp_async(to_k + HD * 8 + 512 * n, k1 + 512 * n);
+        cp_async(to_v + 512 * n, v0 + 512 * n);
+        cp_async(to_v + HD * 8 + 512 * n, v1 + 512 * n);
       }
-      if (sc_half == h) cp_async_part(to + dst_s, sc_src + row * (HD / 16), id < 0 ? 0 : min(max((k_end - key) * (HD / 16) - sc_chunk * 16, 0), 16));
+      if (lane < 2 * SC) cp_async(to + dst_s, s_base + static_cast<uint64_t>(sc_half ? row1 : row) * (HD / 16));
     }
   };
+  uint32_t stage_in = ring, stage_out = ring;  // where the next tile goes, and the next one is taken from
+  auto next_stage = [&](uint32_t& at) { at = at == ring + (KA_STAGES - 1) * SM::STAGE ? ring : at + SM::STAGE; };
 #pragma unroll
   for (int s = 0; s < KA_STAGES - 1; ++s) {
-    if (s < my_tiles) load_tile(s, s); else valid <<= 2;
+    if (s < my_tiles) load_tile(s, stage_in); else valid <<= 2;
+    next_stage(stage_in);
     ptx::cp_async_commit();
   }
 
@@ -291,39 +323,41 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int i = 0; i < MT; ++i) o_acc[c][i][0] = o_acc[c][i][1] = o_acc[c][i][2] = o_acc[c][i][3] = 0.f;
-  // reference of the exponent (uniform over the lanes of a head; -inf: no key yet) and this lane's share of the sum
-  float m_ref[NC][2], l_sum[NC][2];
+  // Per column pair (packed): reference of the exponent (uniform over the lanes of a head; -inf: no key yet), what is added to a
+  // score for it, and this lane's share of the sum
+  float m_ref[NC][2];
+  uint64_t shift[NC], l_sum[NC], f_pair[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     m_ref[c][0] = m_ref[c][1] = -CUDART_INF_F;
-    l_sum[c][0] = l_sum[c][1] = 0.f;
+    shift[c] = ptx::pack_f32x2(P_SHIFT, P_SHIFT);  // (no key yet: every p is 0)
+    l_sum[c] = ptx::pack_f32x2(0.f, 0.f);
+    f_pair[c] = ptx::pack_f32x2(f_head[c][0], f_head[c][1]);
   }
   bool nan_seen = false;
 
   for (int i = 0; i < my_tiles; ++i) {
-    const int stage = i % KA_STAGES;
-    {
-      const int nxt = i + KA_STAGES - 1;
-      if (i > 0 && (i & 31) == 0 && i + 32 < my_tiles) { fetch_pages(i + 32, id_nxt); check_pages(i + 32, id_nxt); }
-      if (nxt < my_tiles) load_tile(nxt, nxt % KA_STAGES); else valid <<= 2;
-      ptx::cp_async_commit();
-    }
+    if (i > 0 && (i & 31) == 0 && i + 32 < my_tiles) { fetch_pages(i + 32, id_nxt); check_pages(i + 32, id_nxt); }
+    if (i + KA_STAGES - 1 < my_tiles) load_tile(i + KA_STAGES - 1, stage_in); else valid <<= 2;
+    next_stage(stage_in);
+    ptx::cp_async_commit();
     ptx::cp_async_wait<KA_STAGES - 1>();
     __syncwarp();
-    const uint32_t sk = ring + stage * SM::STAGE, sv = sk + SM::CODES, ssk = sv + SM::CODES, ssv = ssk + SM::SCALES;
+    const uint32_t sk = stage_out, sv = sk + SM::CODES, ssk = sv + SM::CODES, ssv = ssk + SM::SCALES;
     const int key0 = key_begin(i), halves = static_cast<int>((valid >> (2 * (KA_STAGES - 1))) & 3u);
-    if (MULTI && pos0 - key0 < KA_KEYS - 1) {
-      // Not every token of the block sees all keys, and 0 * NaN is NaN: scales of V that are NaN become 0 where not all see the
-      // key, and the rows that do see it are given their NaN at the end.  A key per lane.
-      if (key0 + lane > pos0) {
+    const bool masked = (MULTI ? min(k_end, pos0 + 1) : k_end) - key0 < KA_KEYS || halves != 3;
+    if (masked) {
+      // V of keys that do not count is multiplied with weights of 0, and 0 * NaN is NaN: their scales become 0.  Of keys that
+      // some tokens of the block see and others do not, scales that are NaN do, and the rows that see the key are given their NaN
+      // at the end.  A key per lane.
+      const bool counts = key0 + lane < k_end && (halves >> (lane >> 4)) & 1;
 #pragma unroll
-        for (int n = 0; n < HD / 64; ++n) {
-          const uint32_t at = ssv + lane * (HD / 16) + 4 * n, w = lds32(at);
-          bool seen = false;
-          const uint32_t d = drop_nans(w, seen);
-          if (seen) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(d) : "memory");
-          nan_seen |= seen;
-        }
+      for (int n = 0; n < HD / 64; ++n) {
+        const uint32_t at = ssv + lane * (HD / 16) + 4 * n, w = lds32(at);
+        bool seen = false;
+        const uint32_t d = !counts ? 0u : MULTI && key0 + lane > pos0 ? drop_nans(w, seen) : w;
+        if (d != w) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(d) : "memory");
+        nan_seen |= seen;
       }
       __syncwarp();
     }
@@ -333,10 +367,6 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float st[NC][2][4];
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st[c][0][e] = st[c][1][e] = 0.f;
       uint32_t w[2][W], sc[2][2];  // rows g, g + 8: codes and scales (as pairs of equal halves)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
@@ -365,18 +395,24 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
           a1[e] = mul_f16x2(a1[e], sc[1][j / 2]);
         }
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (int p = 0; p < 2; ++p) {
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
-            mma_f16(st[c][p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], qb[c][2 * j + p][0], qb[c][2 * j + p][1]);
+          for (int c = 0; c < NC; ++c) {
+            const uint32_t b0 = qb[c][2 * j + p][0], b1 = qb[c][2 * j + p][1];
+            if (j == 0) mma_f16_first(st[c][p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], b0, b1);
+            else mma_f16(st[c][p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], b0, b1);
+          }
+        }
       }
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[h][c][e] = (st[c][0][e] + st[c][1][e]) * f_head[c][e & 1];
+        for (int e = 0; e < 4; e += 2)
+          ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(st[c][0][e], st[c][0][e + 1]),
+                                                          ptx::pack_f32x2(st[c][1][e], st[c][1][e + 1])), f_pair[c]),
+                            x[h][c][e], x[h][c][e + 1]);
     }
     // ---- softmax
-    const bool masked = (MULTI ? min(k_end, pos0 + 1) : k_end) - key0 < KA_KEYS || halves != 3;
     if (masked) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
@@ -400,13 +436,14 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        mx[c][e] = fmaxf(fmaxf(x[0][c][e], x[0][c][2 + e]), fmaxf(x[1][c][e], x[1][c][2 + e]));
+        mx[c][e] = fmaxf(ptx::fmax3(x[0][c][e], x[0][c][2 + e], x[1][c][e]), x[1][c][2 + e]);
         grow |= mx[c][e] > m_ref[c][e] + P_SLACK;
       }
     }
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
+        float corr[2], add[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float m = mx[c][e];
@@ -414,12 +451,14 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
           const float m_new = fmaxf(m_ref[c][e], m);
-          const float corr = m_new == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][e] - m_new);
+          corr[e] = m_new == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][e] - m_new);
+          add[e] = P_SHIFT - (m_new == -CUDART_INF_F ? 0.f : m_new);
           m_ref[c][e] = m_new;
-          l_sum[c][e] *= corr;
 #pragma unroll
-          for (int n = 0; n < MT; ++n) { o_acc[c][n][e] *= corr; o_acc[c][n][2 + e] *= corr; }
+          for (int n = 0; n < MT; ++n) { o_acc[c][n][e] *= corr[e]; o_acc[c][n][2 + e] *= corr[e]; }
         }
+        shift[c] = ptx::pack_f32x2(add[0], add[1]);
+        l_sum[c] = ptx::mul_f32x2(l_sum[c], ptx::pack_f32x2(corr[0], corr[1]));
       }
     }
 #pragma unroll
@@ -427,17 +466,17 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
       uint32_t pb[NC][2];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        float (&y)[4] = x[h][c];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float ref = (m_ref[c][e] == -CUDART_INF_F ? 0.f : m_ref[c][e]) - P_SHIFT;  // (no key yet: every p is 0)
-          y[e] = ptx::ex2_approx(y[e] - ref);
-          y[2 + e] = ptx::ex2_approx(y[2 + e] - ref);
-          l_sum[c][e] += y[e] + y[2 + e];
+        for (int k = 0; k < 2; ++k) {
+          float y0, y1;
+          // (the rounded score, which is what the reference was taken from: very large ones would not cancel otherwise)
+          ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(x[h][c][2 * k], x[h][c][2 * k + 1]), shift[c]), y0, y1);
+          y0 = ptx::ex2_approx(y0);
+          y1 = ptx::ex2_approx(y1);
+          l_sum[c] = ptx::add_f32x2(l_sum[c], ptx::pack_f32x2(y0, y1));
+          // P^T as an operand: the transpose of the accumulator's 8 x 8 blocks
+          pb[c][k] = transpose8x8(pack_f16(y0, y1));
         }
-        // P^T as an operand: the transpose of the accumulator's 8 x 8 blocks
-        pb[c][0] = transpose8x8(pack_f16(y[0], y[1]));
-        pb[c][1] = transpose8x8(pack_f16(y[2], y[3]));
       }
       // ---- O^T += V^T P^T: this lane's keys are key_of(2 t4), key_of(2 t4 + 1) = t4, t4 + 4 of both 8-key groups, its features
       // g * hd / 8 ..; two keys share a word's nibbles, low and high
@@ -473,19 +512,37 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
           for (int c = 0; c < NC; ++c) mma_f16(o_acc[c][4 * j + n], even[0][n], odd[0][n], even[1][n], odd[1][n], pb[c][0], pb[c][1]);
       }
     }
+    next_stage(stage_out);
     __syncwarp();  // every lane has read this stage before it is refilled
   }
   ptx::cp_async_wait<0>();
+  float l_col[NC][2];
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int c = 0; c < NC; ++c) {
+    ptx::unpack_f32x2(l_sum[c], l_col[c][0], l_col[c][1]);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) l_sum[c][h] += __shfl_xor_sync(0xffffffffu, l_sum[c][h], o);
-  __syncthreads();  // every warp has left its ring: the memory is reused for the merge
-
-  float* mrg = reinterpret_cast<float*>(smem);
-  constexpr int RS = HD + 2;
+      for (int o = 4; o < 32; o <<= 1) l_col[c][h] += __shfl_xor_sync(0xffffffffu, l_col[c][h], o);
+  }
+  // Merge: the warps agree on the maximum of every column, scale what they have to it, and add up in shared memory.
+  constexpr int RS = SM::MERGE_ROW;
+  float* const mrg = reinterpret_cast<float*>(smem);
+  float* const m_all = mrg + KA_WARPS * 16 * RS;  // [column][warp]
+  __syncthreads();  // every warp has left its ring: the memory is reused
+  if (g == 0) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) m_all[(c * 8 + t4 * 2 + h) * KA_WARPS + warp] = m_ref[c][h];
+  }
+  __syncthreads();
+  auto column_max = [&](int col) {
+    float m = m_all[col * KA_WARPS];
+#pragma unroll
+    for (int w = 1; w < KA_WARPS; ++w) m = fmaxf(m, m_all[col * KA_WARPS + w]);
+    return m;
+  };
   const float o_unit = P_UNIT * pow2f(kv4_exp(a.c.v_exp, kvh));
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -493,30 +550,28 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
     for (int h = 0; h < 2; ++h) {
       const int col = c * 8 + t4 * 2 + h;
       if (col < n_cols) {
-        float* dst_row = mrg + (warp * 16 + col) * RS;
+        const float m = column_max(col);
+        const float f = m == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][h] - m), fo = f * o_unit;  // 0 for a warp that saw no key
+        float* const dst_row = mrg + (warp * 16 + col) * RS;
 #pragma unroll
-        for (int n = 0; n < MT; ++n) {
-          dst_row[g * (HD / 8) + 2 * n] = o_acc[c][n][h] * o_unit;
-          dst_row[g * (HD / 8) + 2 * n + 1] = o_acc[c][n][2 + h] * o_unit;
-        }
-        if (g == 0) { dst_row[HD] = m_ref[c][h]; dst_row[HD + 1] = l_sum[c][h] * P_UNIT; }
+        for (int n = 0; n < MT; ++n)
+          *reinterpret_cast<float2*>(dst_row + g * (HD / 8) + 2 * n) = make_float2(o_acc[c][n][h] * fo, o_acc[c][n][2 + h] * fo);
+        if (g == 0) dst_row[HD] = l_col[c][h] * (f * P_UNIT);
       }
     }
   }
   const bool nans = MULTI ? __syncthreads_or(nan_seen) : (__syncthreads(), false);
-  for (int idx = tid; idx < n_cols * HD; idx += KA_THREADS) {
+  const bool pairs = (reinterpret_cast<uintptr_t>(a.o) & 3u) == 0;
+  for (int idx = tid * 4; idx < n_cols * HD; idx += KA_THREADS * 4) {  // four neighbouring features of a column
     const int r = idx / HD, d = idx - r * HD;
-    float m = -CUDART_INF_F;
-#pragma unroll
-    for (int w = 0; w < KA_WARPS; ++w) m = fmaxf(m, mrg[(w * 16 + r) * RS + HD]);
-    const float m_use = m == -CUDART_INF_F ? 0.f : m;
-    float l = 0.f, o = 0.f;
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < KA_WARPS; ++w) {
       const float* src = mrg + (w * 16 + r) * RS;
-      const float f = exp2f(src[HD] - m_use);  // 0 for a warp that saw no key
-      l += src[HD + 1] * f;
-      o += src[d] * f;
+      const float4 v = *reinterpret_cast<const float4*>(src + d);
+      l += src[HD];
+      o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
     }
     const size_t row = out_row(r);
     if (MULTI && nans) {
@@ -524,14 +579,24 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? 1 : 2) kv4_decode_kernel(co
         const int id = table[key >> l2p];
         if (static_cast<unsigned>(id) >= static_cast<unsigned>(a.c.n_pages)) continue;
         const size_t at = ((static_cast<size_t>(id) * a.n_kv_heads + kvh) << l2p) + (key & ((1 << l2p) - 1));
-        if ((a.c.v_scale[at * (HD / 16) + d / 16] & 0x7f) == 0x7f) o = CUDART_NAN_F;
+        if ((a.c.v_scale[at * (HD / 16) + d / 16] & 0x7f) == 0x7f) o = make_float4(CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F);
       }
     }
     if (a.n_splits == 1) {
-      a.o[row * HD + d] = __float2bfloat16(l == 0.f ? 0.f : o / l);  // (no visible entry: zeros)
+      const float inv = l == 0.f ? 0.f : 1.f / l;  // (no visible entry: zeros)
+      const uint32_t lo = ptx::pack_bf16(o.x * inv, o.y * inv), hi = ptx::pack_bf16(o.z * inv, o.w * inv);
+      bf16* const dst = a.o + row * HD + d;
+      if (pairs) {
+        reinterpret_cast<uint32_t*>(dst)[0] = lo;
+        reinterpret_cast<uint32_t*>(dst)[1] = hi;
+      } else {  // results that start between two words
+        uint16_t* const dst16 = reinterpret_cast<uint16_t*>(dst);
+        dst16[0] = static_cast<uint16_t>(lo); dst16[1] = static_cast<uint16_t>(lo >> 16);
+        dst16[2] = static_cast<uint16_t>(hi); dst16[3] = static_cast<uint16_t>(hi >> 16);
+      }
     } else {
-      a.parts.o[(part_row0 + row) * HD + d] = o;
-      if (d == 0) a.parts.ml[part_row0 + row] = make_float2(m, l);
+      *reinterpret_cast<float4*>(a.parts.o + (part_row0 + row) * HD + d) = o;
+      if (d == 0) a.parts.ml[part_row0 + row] = make_float2(column_max(r), l);
     }
   }
 }
@@ -609,6 +674,7 @@ extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, cons
   if (!q || !out || !kv_len_dev || ldq < 1ll * cfg->n_q_heads * cfg->head_dim || ldq % 8 != 0) return PD_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(q) & 15u) || (reinterpret_cast<uintptr_t>(out) & 1u)) return PD_ERR_INVALID_ARG;
   if (max_kv_len < n_new || max_kv_len > (cache->table_ld << a.c.log2_page)) return PD_ERR_INVALID_ARG;
+  if ((1ll * cache->n_pages * cfg->n_kv_heads) << a.c.log2_page > 0xffffffffll) return PD_ERR_UNSUPPORTED_SHAPE;  // (rows of the pool)
   a.block_tokens = kv4_block_tokens(cfg->n_q_heads / cfg->n_kv_heads, n_new);
   a.seq_blocks = (n_new + a.block_tokens - 1) / a.block_tokens;
   const long long slots = 1ll * B * a.seq_blocks;

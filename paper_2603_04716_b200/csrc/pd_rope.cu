@@ -87,19 +87,18 @@ __global__ void __launch_bounds__(NR_THREADS) qk_norm_rope_kernel(const NormArgs
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
   const int row = blockIdx.x * (NR_THREADS / J) + threadIdx.x / J, j = threadIdx.x % J;
-  const int pos = row < a.rows ? a.positions[row] : -1;
+  const HeadShare<PAIRS> at(j, a.t.rot);
+  const bool is_q = static_cast<int>(blockIdx.y) < a.q_blocks, there = row < a.rows;
+  const int h0 = (is_q ? blockIdx.y : blockIdx.y - a.q_blocks) * NR_HEADS, n_h = (is_q ? a.n_q_heads : a.n_kv_heads) - h0;
+  const size_t r = there ? row : 0;
+  HeadsOfRow<HD, PAIRS, NR_HEADS> heads(a.qkv + r * a.ldqkv + (is_q ? h0 : a.n_q_heads + h0) * HD, n_h, there, at);
+  const int pos = there ? a.positions[row] : -1;
   const bool far = a.t.rot > 0 && pos >= a.t.n_pos;
   if (far && j == 0) report_place(a.err_word);
   const bool live = pos >= 0 && !far;
-  const HeadShare<PAIRS> at(j, a.t.rot);
   const float2* angles = a.t.table + static_cast<size_t>(live ? pos : 0) * (a.t.rot / 2);
-  const bool is_q = static_cast<int>(blockIdx.y) < a.q_blocks;
-  const int h0 = (is_q ? blockIdx.y : blockIdx.y - a.q_blocks) * NR_HEADS;
-  const size_t r = live ? row : 0;
-  const bf16* src = a.qkv + r * a.ldqkv + (is_q ? h0 : a.n_q_heads + h0) * HD;
   bf16* dst = is_q ? a.q_out + r * a.ldq + h0 * HD : a.k_out + r * a.ldk + h0 * HD;
-  transform_heads<HD, PAIRS, NR_HEADS>(src, dst, (is_q ? a.n_q_heads : a.n_kv_heads) - h0, live, at, is_q ? a.t.q_gain : a.t.k_gain,
-                                       a.t.eps, angles, j);
+  heads.transform(dst, n_h, live, at, is_q ? a.t.q_gain : a.t.k_gain, a.t.eps, angles, j);
 }
 
 }  // namespace
