@@ -1,6 +1,8 @@
 // What the kernels of the 4-bit paged KV cache share: the cache as kernels see it, host-side argument checks, the transform of q
 // and k heads (norm, rotation) and the quantiser.
 #pragma once
+#include <type_traits>
+
 #include "pd_common.cuh"
 #include "pd_ptx.cuh"
 
@@ -95,105 +97,195 @@ __device__ __forceinline__ void unpack8(const uint4& v, float* f) {
   f[4] = ptx::bf16_lo(v.z); f[5] = ptx::bf16_hi(v.z);
   f[6] = ptx::bf16_lo(v.w); f[7] = ptx::bf16_hi(v.w);
 }
-__device__ __forceinline__ uint4 pack8(const float* f) {
-  return make_uint4(ptx::pack_bf16(f[0], f[1]), ptx::pack_bf16(f[2], f[3]), ptx::pack_bf16(f[4], f[5]),
-                    ptx::pack_bf16(f[6], f[7]));
-}
 
-// A head of one row is the work of hd / 16 neighbouring lanes, 16 features each: two chunks of 8 that start at a and b.  With
-// halves paired, lane j < rot / 16 holds features 8 j .. and their partners rot / 2 + 8 j ..; every other lane 16 neighbours.
-// Either way the lane's 8 pairs are pairs 8 j .. of the table's row.
+template <int LANES, class T>
+__device__ __forceinline__ T lanes_sum(T v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ uint64_t dup_f32x2(float v) { return ptx::pack_f32x2(v, v); }
+
+// A head of one row is the work of hd / 8 neighbouring lanes, 8 features each: two chunks of 4 that start at a and b.  With halves
+// paired, lane j < rot / 8 holds features 4 j .. and their partners rot / 2 + 4 j ..; every other lane 8 neighbours.  Either way
+// the lane's 4 pairs are pairs 4 j .. of the table's row.
 template <bool PAIRS>
 struct HeadShare {
   int a, b;
   bool turns;
   __device__ __forceinline__ HeadShare(int j, int rot) {
-    turns = j < rot / 16;
+    turns = j < rot / 8;
     const bool split = !PAIRS && turns;
-    a = split ? 8 * j : 16 * j;
-    b = split ? rot / 2 + 8 * j : a + 8;
+    a = split ? 4 * j : 8 * j;
+    b = split ? rot / 2 + 4 * j : a + 4;
   }
-};
-
-__device__ __forceinline__ void load_share(const bf16* head, int a, int b, uint4 (&w)[2]) {
-  w[0] = *reinterpret_cast<const uint4*>(head + a);
-  w[1] = *reinterpret_cast<const uint4*>(head + b);
-}
-__device__ __forceinline__ void load_angles(const float2* row, int j, float (&cs)[16]) {
-  const float4* p = reinterpret_cast<const float4*>(row + j * 8);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 v = p[i];
-    cs[4 * i] = v.x; cs[4 * i + 1] = v.y; cs[4 * i + 2] = v.z; cs[4 * i + 3] = v.w;
+  __device__ __forceinline__ uint4 load(const bf16* head) const {
+    if (PAIRS) return *reinterpret_cast<const uint4*>(head + a);
+    const uint2 x = *reinterpret_cast<const uint2*>(head + a), y = *reinterpret_cast<const uint2*>(head + b);
+    return make_uint4(x.x, x.y, y.x, y.y);
   }
-}
-// (a, b) -> (a c - b s, b c + a s) of the lane's 8 pairs, in the precision of T.
-template <bool PAIRS, class T>
-__device__ __forceinline__ void turn(T (&f)[16], const float (&cs)[16]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const T c = static_cast<T>(cs[2 * e]), s = static_cast<T>(cs[2 * e + 1]);
-    T& x = f[PAIRS ? 2 * e : e];
-    T& y = f[PAIRS ? 2 * e + 1 : 8 + e];
-    const T u = x * c - y * s, w = y * c + x * s;
-    x = u; y = w;
-  }
-}
-// RMSNorm (where there is a gain) and rotation of a lane's share of a head, in the precision of T, times `unit`.  The factor that
-// the norm has in common comes last: x * gain is exact in fp32, and in double so are its products with cos and sin.  All
-// lanes of a warp call it.
-template <int HD, bool PAIRS, class T>
-__device__ __forceinline__ void transform_share(const uint4 (&w)[2], bool norm, const uint4 (&gain)[2], double eps, bool turns,
-                                                const float (&cs)[16], T unit, T (&f)[16]) {
-  float x[16];
-  unpack8(w[0], x);
-  unpack8(w[1], x + 8);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) f[e] = static_cast<T>(x[e]);
-  if (norm) {  // (the same for all lanes)
-    T sum[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sum[e & 3] = fma(f[e], f[e], sum[e & 3]);
-    T all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-    for (int o = HD / 32; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-    unit *= rsqrt(all * static_cast<T>(1.0 / HD) + static_cast<T>(eps));
-    float g[16];
-    unpack8(gain[0], g);
-    unpack8(gain[1], g + 8);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) f[e] *= static_cast<T>(g[e]);
-  }
-  if (turns) turn<PAIRS>(f, cs);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) f[e] *= unit;
-}
-// NH heads (n_h of them there are) of one row in fp32, rounded to bf16 once.  The row is read before anything else is known
-// (`there`: it exists); `live`, the angles' row and the rest of the work wait for the position.
-template <int HD, bool PAIRS, int NH>
-struct HeadsOfRow {
-  uint4 w[NH][2];
-  __device__ __forceinline__ HeadsOfRow(const bf16* src, int n_h, bool there, const HeadShare<PAIRS>& at) {
-#pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      w[h][0] = w[h][1] = make_uint4(0, 0, 0, 0);
-      if (there && h < n_h) load_share(src + h * HD, at.a, at.b, w[h]);
+  __device__ __forceinline__ void store(bf16* head, const uint4& w) const {
+    if (PAIRS) {
+      *reinterpret_cast<uint4*>(head + a) = w;
+    } else {
+      *reinterpret_cast<uint2*>(head + a) = make_uint2(w.x, w.y);
+      *reinterpret_cast<uint2*>(head + b) = make_uint2(w.z, w.w);
     }
   }
-  __device__ __forceinline__ void transform(bf16* dst, int n_h, bool live, const HeadShare<PAIRS>& at, const bf16* gain, double eps,
-                                            const float2* angles, int j) {
-    uint4 g[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    float cs[16] = {};
-    if (live && at.turns) load_angles(angles, j, cs);
-    if (gain) load_share(gain, at.a, at.b, g);
+  // The first and the second features of the lane's pairs 2 i and 2 i + 1, packed.
+  static __device__ __forceinline__ void unpack(const uint4& w, uint64_t (&u)[2], uint64_t (&v)[2]) {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      float f[16];
-      transform_share<HD, PAIRS>(w[h], gain != nullptr, g, eps, at.turns, cs, 1.f, f);
-      if (live && h < n_h) {
-        *reinterpret_cast<uint4*>(dst + h * HD + at.a) = pack8(f);
-        *reinterpret_cast<uint4*>(dst + h * HD + at.b) = pack8(f + 8);
+    for (int i = 0; i < 2; ++i) {
+      u[i] = PAIRS ? ptx::pack_f32x2(ptx::bf16_lo(x[2 * i]), ptx::bf16_lo(x[2 * i + 1])) : ptx::pack_f32x2(ptx::bf16_lo(x[i]), ptx::bf16_hi(x[i]));
+      v[i] = PAIRS ? ptx::pack_f32x2(ptx::bf16_hi(x[2 * i]), ptx::bf16_hi(x[2 * i + 1])) : ptx::pack_f32x2(ptx::bf16_lo(x[2 + i]), ptx::bf16_hi(x[2 + i]));
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const uint64_t (&u)[2], const uint64_t (&v)[2]) {
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float u0, u1, v0, v1;
+      ptx::unpack_f32x2(u[i], u0, u1);
+      ptx::unpack_f32x2(v[i], v0, v1);
+      x[PAIRS ? 2 * i : i] = PAIRS ? ptx::pack_bf16(u0, v0) : ptx::pack_bf16(u0, u1);
+      x[PAIRS ? 2 * i + 1 : 2 + i] = PAIRS ? ptx::pack_bf16(u1, v1) : ptx::pack_bf16(v0, v1);
+    }
+    return make_uint4(x[0], x[1], x[2], x[3]);
+  }
+};
+// A warp has a row, 256 / hd heads of it at a time, and the loads of STEPS such groups go out before anything else is known.
+template <int HD>
+constexpr int heads_per_step() { return 256 / HD; }
+template <int HD, bool PAIRS, int STEPS>
+__device__ __forceinline__ void load_heads(uint4 (&w)[STEPS], const bf16* first_head, int n_heads, const HeadShare<PAIRS>& at) {
+  const int mine = (threadIdx.x & 31) / (HD / 8);
+  const bf16* const head = first_head + mine * HD;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    w[i] = make_uint4(0, 0, 0, 0);
+    if (i * heads_per_step<HD>() + mine < n_heads) w[i] = at.load(head + i * 256);
+  }
+}
+// Of the two kernels that read rows: whether there is a norm and whether whole heads are rotated is decided once per warp, not per head.
+template <class F>
+__device__ __forceinline__ void with_flags(bool norm, bool whole, F f) {
+  if (norm) {
+    if (whole) f(std::true_type(), std::true_type()); else f(std::true_type(), std::false_type());
+  } else {
+    if (whole) f(std::false_type(), std::true_type()); else f(std::false_type(), std::false_type());
+  }
+}
+
+// ---- q, in fp32: n_heads heads of a row, rounded to bf16 once.  Gain and rotation are one product with a matrix of two by two
+// per pair, the same for all heads of the row; the factor that the norm has in common comes last.
+template <int HD, bool PAIRS, bool NORM, bool WHOLE, int STEPS>
+__device__ __forceinline__ void transform_heads(const uint4 (&w)[STEPS], bf16* first_head, int n_heads, const HeadShare<PAIRS>& at,
+                                                const bf16* gain, float eps, const float2* angles, int j) {
+  const bool turns = WHOLE || at.turns;
+  uint64_t mu[2], mv[2], nu[2], nv[2];  // first = mu first + nu second, second = mv second + nv first
+  at.unpack(NORM ? at.load(gain) : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), mu, mv);
+  if (turns) {
+    const float4* const cs = reinterpret_cast<const float4*>(angles + 4 * j);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 x = cs[i];
+      const uint64_t c = ptx::pack_f32x2(x.x, x.z);
+      nu[i] = ptx::mul_f32x2(mv[i], ptx::pack_f32x2(-x.y, -x.w));
+      nv[i] = ptx::mul_f32x2(mu[i], ptx::pack_f32x2(x.y, x.w));
+      mu[i] = ptx::mul_f32x2(mu[i], c);
+      mv[i] = ptx::mul_f32x2(mv[i], c);
+    }
+  }
+  const int mine = (threadIdx.x & 31) / (HD / 8);
+  bf16* const head = first_head + mine * HD;
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    uint64_t u[2], v[2], x[2], y[2];
+    at.unpack(w[s], u, v);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      x[i] = ptx::mul_f32x2(u[i], mu[i]);
+      y[i] = ptx::mul_f32x2(v[i], mv[i]);
+      if (turns) {
+        x[i] = ptx::fma_f32x2(v[i], nu[i], x[i]);
+        y[i] = ptx::fma_f32x2(u[i], nv[i], y[i]);
       }
+    }
+    if (NORM) {
+      float lo, hi, r;
+      ptx::unpack_f32x2(ptx::fma_f32x2(u[1], u[1], ptx::fma_f32x2(v[0], v[0], ptx::fma_f32x2(v[1], v[1], ptx::mul_f32x2(u[0], u[0])))), lo, hi);
+      asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(fmaf(lanes_sum<HD / 8>(lo + hi), 1.f / HD, eps)));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[i] = ptx::mul_f32x2(x[i], dup_f32x2(r));
+        y[i] = ptx::mul_f32x2(y[i], dup_f32x2(r));
+      }
+    }
+    if (s * heads_per_step<HD>() + mine < n_heads) at.store(head + s * 256, at.pack(x, y));
+  }
+}
+
+// The 8 features of a share in memory order of its chunks.
+__device__ __forceinline__ void unpack_share(const uint4& w, float (&f)[8]) {
+  f[0] = ptx::bf16_lo(w.x); f[1] = ptx::bf16_hi(w.x); f[2] = ptx::bf16_lo(w.y); f[3] = ptx::bf16_hi(w.y);
+  f[4] = ptx::bf16_lo(w.z); f[5] = ptx::bf16_hi(w.z); f[6] = ptx::bf16_lo(w.w); f[7] = ptx::bf16_hi(w.w);
+}
+
+// ---- k, in double.  A product of a gain and a cos or sin has 32 significant bits, its products with a feature 40: all of them are
+// exact, and the factor of the norm comes last.
+template <int HD, bool PAIRS, bool NORM, bool WHOLE>
+struct ExactTransform {
+  double m[8], n[8];  // feature = m feature + n partner
+  bool turns;
+  static __device__ __forceinline__ constexpr int first(int pair) { return PAIRS ? 2 * pair : pair; }
+  static __device__ __forceinline__ constexpr int second(int pair) { return PAIRS ? 2 * pair + 1 : 4 + pair; }
+  __device__ __forceinline__ ExactTransform(const HeadShare<PAIRS>& at, const bf16* gain, const float2* angles, int j) {
+    turns = WHOLE || at.turns;
+    float g[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    if (NORM) unpack_share(at.load(gain), g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = static_cast<double>(g[e]);
+    if (turns) {
+      const float4* const cs = reinterpret_cast<const float4*>(angles + 4 * j);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 x = cs[i];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const double c = p ? x.z : x.x, s = p ? x.w : x.y;
+          const int a = first(2 * i + p), b = second(2 * i + p);
+          n[a] = -m[b] * s;
+          n[b] = m[a] * s;
+          m[a] *= c;
+          m[b] *= c;
+        }
+      }
+    }
+  }
+  // All lanes of a warp call it.
+  __device__ __forceinline__ void operator()(const uint4& w, double eps, double (&f)[8]) const {
+    float x[8];
+    double v[8];
+    unpack_share(w, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = static_cast<double>(x[e]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = v[e] * m[e];
+    if (turns) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        f[first(p)] = fma(v[second(p)], n[first(p)], f[first(p)]);
+        f[second(p)] = fma(v[first(p)], n[second(p)], f[second(p)]);
+      }
+    }
+    if (NORM) {
+      double sum[2] = {0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e & 1] = fma(v[e], v[e], sum[e & 1]);
+      const double r = rsqrt(lanes_sum<HD / 8>(sum[0] + sum[1]) * (1.0 / HD) + eps);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= r;
     }
   }
 };
@@ -206,23 +298,23 @@ __device__ __forceinline__ float sticky_float(double d) {
   const uint32_t lost = static_cast<uint32_t>(__double2loint(d)) & 0x1fffffffu;
   return __uint_as_float(__float_as_uint(__double2float_rz(d)) | (lost ? 1u : 0u));
 }
-// Largest magnitude of 8 values; NaN if one is infinite or NaN.
+// Largest magnitude of 4 values; NaN if one of them is.
+__device__ __forceinline__ float max_nan3(float a, float b, float c) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  return m;
+}
 __device__ __forceinline__ float chunk_max(const float* t) {
-  float m = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(fabsf(t[e])));
-  return m <= 3.402823466e38f ? m : __int_as_float(0x7fc00000);
+  return max_nan3(max_nan3(fabsf(t[0]), fabsf(t[1]), fabsf(t[2])), fabsf(t[3]), 0.f);
 }
-// t / d by an approximate reciprocal, corrected by the exact remainder: the float nearest to within 2^-20 of a step.  That cannot
-// move it onto a border b of the formats that it does not lie on, or off one that it does: b * d is a float, t differs from it by
-// one step at least, and d has at most four significant bits, so the quotients differ by more than half a step of b.
-__device__ __forceinline__ float quotient(float t, float d, float inv) {
-  const float p = __fmul_rn(t, inv);
-  return __fmaf_rn(__fmaf_rn(-p, d, t), inv, p);
-}
-// The E4M3 scale of 16 values from their largest magnitude.
+// Quotients t / d are formed with an approximate reciprocal and corrected by the exact remainder, p + (t - p d) inv: the float
+// nearest to within 2^-20 of a step.  That cannot move one onto a border b of the formats that it does not lie on, or off one that
+// it does: b * d is a float, t differs from it by one step at least, and d has at most four significant bits, so the quotients
+// differ by more than half a step of b.
+// The E4M3 scale of 16 values from their largest magnitude; NaN if one of them is infinite or NaN.
 __device__ __forceinline__ uint32_t kv4_scale(float amax) {
-  return amax == amax ? ptx::cvt_e4m3x2(quotient(amax, 6.f, 1.f / 6.f), 0.f) : 0x7fu;
+  const float inv = 1.f / 6.f, p = __fmul_rn(amax, inv);
+  return amax <= 3.402823466e38f ? ptx::cvt_e4m3x2(__fmaf_rn(__fmaf_rn(p, -6.f, amax), inv, p), 0.f) : 0x7fu;
 }
 __device__ __forceinline__ float e4m3_value(uint32_t code) {
   uint32_t h;
@@ -231,55 +323,66 @@ __device__ __forceinline__ float e4m3_value(uint32_t code) {
   asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.f32.f16 %0, lo; }" : "=f"(f) : "r"(h));
   return f;
 }
-// Eight values over a scale -> eight E2M1 codes, value i in bits 4 i .. 4 i + 3.
-__device__ __forceinline__ uint32_t kv4_codes(const float* t, float scale) {
-  float inv;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(scale));
-  if (!(scale > 0.f)) inv = 0.f;
-  uint32_t r = 0;
+// Eight values over their scales (one of the first four, one of the others) -> eight E2M1 codes, value i in bits 4 i .. 4 i + 3.
+__device__ __forceinline__ uint32_t kv4_codes(const float (&t)[8], float scale0, float scale1) {
+  float q[8];
 #pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    float q[2];
+  for (int h = 0; h < 2; ++h) {
+    const float scale = h ? scale1 : scale0;
+    float inv;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+    if (!(scale > 0.f)) inv = 0.f;
+    const uint64_t inv2 = dup_f32x2(inv), neg2 = dup_f32x2(-scale);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) q[i] = quotient(t[e + i], scale, inv);
-    uint32_t c;
-    asm("{ .reg .b8 c; .reg .b16 h; cvt.rn.satfinite.e2m1x2.f32 c, %1, %2; cvt.u16.u8 h, c; cvt.u32.u16 %0, h; }"
-        : "=r"(c) : "f"(q[1]), "f"(q[0]));
-    r |= c << (4 * e);
-  }
-  return r;
-}
-// Stores a lane's share (16 values t in units of 2^exp) of one row: codes to row `codes`, scales to row `scales`.  The two
-// chunks of 8 whose common scale it is lie with one lane or, where halves are paired, with two.  All lanes of a warp call it.
-template <int HD, bool PAIRS>
-__device__ __forceinline__ void store_kv4(const float (&t)[16], const HeadShare<PAIRS>& at, int j, int rot, bool live, uint8_t* codes,
-                                          uint8_t* scales) {
-  const float m[2] = {chunk_max(t), chunk_max(t + 8)};
-  float group[2];
-  if (PAIRS) {
-    group[0] = group[1] = fmaxf(m[0], m[1]);
-    if (m[0] != m[0] || m[1] != m[1]) group[0] = group[1] = __int_as_float(0x7fc00000);
-  } else {
-    const int lane0 = (threadIdx.x & 31) - j;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int other = ((i ? at.b : at.a) >> 3) ^ 1;  // the neighbouring chunk, its lane and its place there
-      const bool split = other < rot / 8;
-      const int lane = split ? (other < rot / 16 ? other : other - rot / 16) : other >> 1;
-      const bool second = split ? other >= rot / 16 : other & 1;
-      const float m0 = __shfl_sync(0xffffffffu, m[0], lane0 + lane), m1 = __shfl_sync(0xffffffffu, m[1], lane0 + lane);
-      const float o = second ? m1 : m0;
-      group[i] = fmaxf(m[i], o);
-      if (m[i] != m[i] || o != o) group[i] = __int_as_float(0x7fc00000);
+    for (int e = 4 * h; e < 4 * h + 4; e += 2) {
+      const uint64_t v = ptx::pack_f32x2(t[e], t[e + 1]), p = ptx::mul_f32x2(v, inv2);
+      ptx::unpack_f32x2(ptx::fma_f32x2(ptx::fma_f32x2(p, neg2, v), inv2, p), q[e], q[e + 1]);
     }
   }
-  if (!live) return;
+  uint32_t r;
+  asm("{ .reg .b8 c0, c1, c2, c3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c0, %2, %1; cvt.rn.satfinite.e2m1x2.f32 c1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c2, %6, %5; cvt.rn.satfinite.e2m1x2.f32 c3, %8, %7;\n\t"
+      "mov.b32 %0, {c0, c1, c2, c3}; }"
+      : "=r"(r) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
+  return r;
+}
+// Stores a lane's share (8 values t) of one row: codes to row `codes`, scales, in units of 2^exp, to row `scales`.  With neighbours
+// in a lane the 16 that share a scale lie with two lanes.  Where halves are paired its four chunks of 4 may lie with four, in
+// either place: their maxima meet in `maxima`, 64 floats of the warp's own in shared memory.  All lanes of a warp call it; j is
+// the lane's place in its row.
+template <int HD, bool PAIRS>
+__device__ __forceinline__ void store_kv4(const float (&t)[8], int exp, const HeadShare<PAIRS>& at, int j, bool live, float* maxima,
+                                          uint8_t* codes, uint8_t* scales) {
+  float amax[2];
+  if (PAIRS) {
+    amax[0] = max_nan3(chunk_max(t), chunk_max(t + 4), 0.f);
+    amax[0] = max_nan3(amax[0], __shfl_xor_sync(0xffffffffu, amax[0], 1), 0.f);
+  } else {
+    float* const row = maxima + ((threadIdx.x & 31) - j) * 2;
+    row[at.a / 4] = chunk_max(t);
+    row[at.b / 4] = chunk_max(t + 4);
+    __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int f = i ? at.b : at.a;
-    const uint32_t s = kv4_scale(group[i]);
-    *reinterpret_cast<uint32_t*>(codes + f / 2) = kv4_codes(t + 8 * i, e4m3_value(s));
-    if ((f & 8) == 0) scales[f / 16] = static_cast<uint8_t>(s);
+    for (int i = 0; i < 2; ++i) {
+      const float4 m = *reinterpret_cast<const float4*>(row + (i ? at.b : at.a) / 16 * 4);
+      amax[i] = max_nan3(max_nan3(m.x, m.y, m.z), m.w, 0.f);
+    }
+    __syncwarp();  // (the next head's maxima go to the same place)
+  }
+  if (!live) return;
+  const float unit = pow2f(exp), inv_unit = pow2f(-exp);
+  // (toward zero: a finite value stays one, and an infinite one stays infinite)
+  const uint32_t s0 = kv4_scale(__fmul_rz(amax[0], inv_unit)), s1 = PAIRS ? s0 : kv4_scale(__fmul_rz(amax[1], inv_unit));
+  const uint32_t c = kv4_codes(t, e4m3_value(s0) * unit, e4m3_value(s1) * unit);
+  if (PAIRS) {
+    *reinterpret_cast<uint32_t*>(codes + at.a / 2) = c;
+    if ((j & 1) == 0) scales[j / 2] = static_cast<uint8_t>(s0);
+  } else {
+    *reinterpret_cast<uint16_t*>(codes + at.a / 2) = static_cast<uint16_t>(c);
+    *reinterpret_cast<uint16_t*>(codes + at.b / 2) = static_cast<uint16_t>(c >> 16);
+    if ((at.a & 12) == 0) scales[at.a / 16] = static_cast<uint8_t>(s0);
+    if ((at.b & 12) == 0) scales[at.b / 16] = static_cast<uint8_t>(s1);
   }
 }
 

@@ -11,9 +11,7 @@
 namespace pd {
 namespace {
 
-constexpr int KW_THREADS = 256;
-constexpr int KW_Q_HEADS = 4;  // query heads per block
-
+constexpr int KW_THREADS = 128;
 struct Kv4AppendArgs {
   const bf16* qkv;            // [T, ldqkv]: q heads, k heads, v heads
   bf16* q_out;                // [T, Hq*hd] or NULL
@@ -25,30 +23,6 @@ struct Kv4AppendArgs {
   int ldqkv, n_req, n_tokens, n_q_heads, n_kv_heads, q_blocks;
 };
 
-// The request of row `row`: how many requests end at or before it.  All lanes of a warp call it; its rows are the warp's
-// WARP_ROWS neighbouring ones.  Up to 32 requests take one load and a vote per row.
-template <int J>
-__device__ __forceinline__ int request_of(const int32_t* cu, int n_req, int row) {
-  const int lane = threadIdx.x & 31;
-  if (n_req <= 32) {
-    const int end = lane < n_req ? cu[lane + 1] : 0x7fffffff;
-    int req = 0;
-#pragma unroll
-    for (int i = 0; i < 32 / J; ++i) {
-      const int r = __shfl_sync(0xffffffffu, row, i * J);
-      const int n = __popc(__ballot_sync(0xffffffffu, end <= r));
-      if (lane / J == i) req = n;
-    }
-    return req;
-  }
-  int lo = 0, hi = n_req;  // the first r with cu[r + 1] > row
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid + 1] <= row) lo = mid + 1; else hi = mid;
-  }
-  return lo;
-}
-
 // The row of a position of a sequence in the pool, in rows; -1: no such page.
 __device__ __forceinline__ long long pool_row(const Kv4Cache& c, int seq, int pos, int n_kv_heads, int kvh) {
   const int pi = pos >> c.log2_page;
@@ -58,68 +32,100 @@ __device__ __forceinline__ long long pool_row(const Kv4Cache& c, int seq, int po
   return ((1ll * page * n_kv_heads + kvh) << c.log2_page) + (pos & ((1 << c.log2_page) - 1));
 }
 
-// Blocks along y are groups of query heads, then K heads, then V heads.
-template <int HD, bool PAIRS>
-__global__ void __launch_bounds__(KW_THREADS, 3) kv4_append_kernel(const Kv4AppendArgs a) {
-  constexpr int J = HD / 16;
+// The request of row `row`: how many requests end at or before it.  All lanes of a warp call it with the same row.
+__device__ __forceinline__ int request_of(const int32_t* cu, int n_req, int row) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = n_req;  // candidates lo .. lo + n - 1, and lo + n
+  while (n > 32) {        // 32 equal parts at a time: those whose last request ends at or before the row are passed over
+    const int part = (n + 31) / 32, last = min((lane + 1) * part, n) - 1;
+    const int passed = __popc(__ballot_sync(0xffffffffu, lane * part < n && cu[lo + last + 1] <= row));
+    lo += min(passed * part, n);
+    n = min(part, n - min(passed * part, n));
+  }
+  return lo + __popc(__ballot_sync(0xffffffffu, lane < n && cu[lo + lane + 1] <= row));
+}
+
+// A warp has a row; blocks along y are groups of query heads, then of K heads, then of V heads, 256 features STEPS times each.
+template <int HD, bool PAIRS, int STEPS>
+__global__ void __launch_bounds__(KW_THREADS, STEPS == 4 ? 8 : 5) kv4_append_kernel(const Kv4AppendArgs a) {
+  constexpr int J = HD / 8, STEP = heads_per_step<HD>(), HEADS = STEPS * STEP;
+  __shared__ __align__(16) float maxima[KW_THREADS * 2];
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const int row = blockIdx.x * (KW_THREADS / J) + threadIdx.x / J, j = threadIdx.x % J;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, j = lane % J, mine = lane / J;
+  const int row = blockIdx.x * (KW_THREADS / 32) + warp;
+  if (row >= a.n_tokens) return;
+  const int kv_blocks = (a.n_kv_heads + HEADS - 1) / HEADS, kv_block = static_cast<int>(blockIdx.y) - a.q_blocks;
+  const bool is_q = kv_block < 0, is_v = kv_block >= kv_blocks;
+  const int h0 = (is_q ? blockIdx.y : is_v ? kv_block - kv_blocks : kv_block) * HEADS;
+  const int n_heads = min((is_q ? a.n_q_heads : a.n_kv_heads) - h0, HEADS);
   const HeadShare<PAIRS> at(j, a.t.rot);
-  const bf16* const src = a.qkv + static_cast<size_t>(row < a.n_tokens ? row : 0) * a.ldqkv;
-  const int kv_block = static_cast<int>(blockIdx.y) - a.q_blocks;  // below 0: query heads
+  const HeadShare<true> plain(j, 0);  // of V: neighbours
   // the row goes out first, its place is looked up meanwhile
-  int req = row, first = row, len = -1;
-  auto find_request = [&] {
-    if (a.cu_seqlens) {
-      req = request_of<J>(a.cu_seqlens, a.n_req, row);
-      if (req < a.n_req) first = a.cu_seqlens[req];
-    }
-    if (row < a.n_tokens && req < a.n_req) len = a.kv_len[req];
-  };
-  auto position = [&](bool& live, bool& far) {
-    const long long p = 1ll * len + (row - first);
-    far = len >= 0 && (a.t.rot > 0 ? p >= a.t.n_pos : p > 0x7fffffffll);
-    live = len >= 0 && !far;
-    return live ? static_cast<int>(p) : 0;
-  };
-  bool live, far;
-  if (kv_block < 0) {
-    const int h0 = blockIdx.y * KW_Q_HEADS, n_h = a.n_q_heads - h0;
-    HeadsOfRow<HD, PAIRS, KW_Q_HEADS> heads(src + h0 * HD, n_h, row < a.n_tokens, at);
-    find_request();
-    const int pos = position(live, far);
-    bf16* const dst = a.q_out + static_cast<size_t>(live ? row : 0) * (a.n_q_heads * HD) + h0 * HD;
-    heads.transform(dst, n_h, live, at, a.t.q_gain, a.t.eps, a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j);
+  uint4 w[STEPS];
+  const bf16* const src = a.qkv + static_cast<size_t>(row) * a.ldqkv + ((is_q ? 0 : a.n_q_heads + (is_v ? a.n_kv_heads : 0)) + h0) * HD;
+  if (is_v) load_heads<HD, true>(w, src, n_heads, plain); else load_heads<HD, PAIRS>(w, src, n_heads, at);
+  int req = row, first = row;
+  if (a.cu_seqlens) {
+    req = request_of(a.cu_seqlens, a.n_req, row);
+    if (req >= a.n_req) return;
+    first = a.cu_seqlens[req];
+  }
+  const int len = a.kv_len[req];
+  if (len < 0) return;  // a request that is left out
+  const long long p = 1ll * len + (row - first);
+  if (a.t.rot > 0 ? p >= a.t.n_pos : p > 0x7fffffffll) {
+    report_place(a.err_word);
     return;
   }
-  const bool is_v = kv_block >= a.n_kv_heads;
-  const int kvh = is_v ? kv_block - a.n_kv_heads : kv_block;
-  uint4 w[2] = {}, g[2] = {};
-  if (row < a.n_tokens) load_share(src + (a.n_q_heads + kv_block) * HD, at.a, at.b, w);
-  if (!is_v && a.t.k_gain) load_share(a.t.k_gain, at.a, at.b, g);
-  const int exp = kv4_exp(is_v ? a.c.v_exp : a.c.k_exp, kvh);
-  find_request();
-  const int pos = position(live, far);
-  float cs[16] = {};
-  if (!is_v && live && at.turns) load_angles(a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j, cs);
-  const long long place = live ? pool_row(a.c, req, pos, a.n_kv_heads, kvh) : -1;
-  if ((far || (live && place < 0)) && j == 0) report_place(a.err_word);
-  const size_t to = static_cast<size_t>(place < 0 ? 0 : place);
-  float t[16];
-  if (is_v) {
-    unpack8(w[0], t);
-    unpack8(w[1], t + 8);
-    const float unit = pow2f(-exp);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) t[e] = __fmul_rz(t[e], unit);  // (a finite value stays one, and an infinite one stays infinite)
-  } else {
-    double f[16];
-    transform_share<HD, PAIRS>(w, a.t.k_gain != nullptr, g, a.t.eps, at.turns, cs, static_cast<double>(pow2f(-exp)), f);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) t[e] = sticky_float(f[e]);
+  const int pos = static_cast<int>(p);
+  const float2* const angles = a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2);
+  if (is_q) {
+    with_flags(a.t.q_gain != nullptr, a.t.rot == HD, [&](auto norm, auto whole) {
+      transform_heads<HD, PAIRS, decltype(norm)::value, decltype(whole)::value>(
+          w, a.q_out + (static_cast<size_t>(row) * a.n_q_heads + h0) * HD, n_heads, at, a.t.q_gain, static_cast<float>(a.t.eps), angles, j);
+    });
+    return;
   }
-  store_kv4<HD, PAIRS>(t, at, j, a.t.rot, place >= 0, (is_v ? a.c.v : a.c.k) + to * (HD / 2), (is_v ? a.c.v_scale : a.c.k_scale) + to * (HD / 16));
+  const long long place = pool_row(a.c, req, pos, a.n_kv_heads, h0);
+  if (place < 0) {
+    report_place(a.err_word);
+    return;
+  }
+  const size_t to = static_cast<size_t>(place) + (static_cast<size_t>(mine) << a.c.log2_page);
+  uint8_t* const codes = (is_v ? a.c.v : a.c.k) + to * (HD / 2);
+  uint8_t* const scales = (is_v ? a.c.v_scale : a.c.k_scale) + to * (HD / 16);
+  const int32_t* const exps = is_v ? a.c.v_exp : a.c.k_exp;
+  // group s of the heads
+  auto store = [&](int s, const float (&t)[8], const auto& share) {
+    const bool live = s * STEP + mine < n_heads;
+    const size_t rows = static_cast<size_t>(s * STEP) << a.c.log2_page;
+    store_kv4<HD>(t, live ? kv4_exp(exps, h0 + s * STEP + mine) : 0, share, j, live, maxima + warp * 64, codes + rows * (HD / 2),
+                  scales + rows * (HD / 16));
+  };
+  if (is_v) {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      if (s * STEP >= n_heads) break;
+      float t[8];
+      unpack_share(w[s], t);
+      store(s, t, plain);
+    }
+    return;
+  }
+  with_flags(a.t.k_gain != nullptr, a.t.rot == HD, [&](auto norm, auto whole) {
+    const ExactTransform<HD, PAIRS, decltype(norm)::value, decltype(whole)::value> transform(at, a.t.k_gain, angles, j);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      if (s * STEP >= n_heads) break;
+      double f[8];
+      float t[8];
+      transform(w[s], a.t.eps, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = sticky_float(f[e]);
+      store(s, t, at);
+    }
+  });
 }
 
 // ------------------------------------------------------------------------------- between pages and a contiguous bf16 cache
@@ -158,10 +164,10 @@ __device__ __forceinline__ long long copy_pool_row(const Kv4CopyArgs& a, const C
   return pos < 0 || pos > 0x7fffffffll ? -1 : pool_row(a.c, seq, static_cast<int>(pos), a.n_kv_heads, kvh);
 }
 
-// hd / 16 lanes have a row of K and of V.
+// hd / 8 lanes have a row of K and of V.
 template <int HD>
 __global__ void __launch_bounds__(KW_THREADS) kv4_write_kernel(const Kv4CopyArgs a) {
-  constexpr int J = HD / 16;
+  constexpr int J = HD / 8;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
   const int seq = blockIdx.z, kvh = blockIdx.y, j = threadIdx.x % J;
@@ -172,18 +178,18 @@ __global__ void __launch_bounds__(KW_THREADS) kv4_write_kernel(const Kv4CopyArgs
   const bool live = to >= 0 && from >= 0;
   if (mine && !live && j == 0) report_place(a.err_word);
   const HeadShare<true> at(j, 0);
+  uint4 w[2] = {};
+  if (live) {
+    w[0] = at.load(a.k + static_cast<size_t>(from) * HD);
+    w[1] = at.load(a.v + static_cast<size_t>(from) * HD);
+  }
+  const size_t row = static_cast<size_t>(live ? to : 0);
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
-    uint4 w[2] = {};
-    if (live) load_share((kv ? a.v : a.k) + static_cast<size_t>(from) * HD, at.a, at.b, w);
-    float t[16];
-    unpack8(w[0], t);
-    unpack8(w[1], t + 8);
-    const float unit = pow2f(-kv4_exp(kv ? a.c.v_exp : a.c.k_exp, kvh));
-#pragma unroll
-    for (int e = 0; e < 16; ++e) t[e] = __fmul_rz(t[e], unit);
-    const size_t row = static_cast<size_t>(live ? to : 0);
-    store_kv4<HD, true>(t, at, j, 0, live, (kv ? a.c.v : a.c.k) + row * (HD / 2), (kv ? a.c.v_scale : a.c.k_scale) + row * (HD / 16));
+    float t[8];
+    unpack_share(w[kv], t);
+    store_kv4<HD>(t, kv4_exp(kv ? a.c.v_exp : a.c.k_exp, kvh), at, j, live, nullptr, (kv ? a.c.v : a.c.k) + row * (HD / 2),
+                  (kv ? a.c.v_scale : a.c.k_scale) + row * (HD / 16));
   }
 }
 
@@ -284,18 +290,28 @@ extern "C" pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_tr
   const long long width = (cfg->n_q_heads + 2ll * cfg->n_kv_heads) * hd;
   if (!qkv || !kv_len_dev || ldqkv < width || ldqkv % 8 != 0) return PD_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(qkv) | reinterpret_cast<uintptr_t>(q_out)) & 15u) return PD_ERR_INVALID_ARG;
+  if ((1ll * cache->n_pages * cfg->n_kv_heads) << a.c.log2_page > 0xffffffffll) return PD_ERR_UNSUPPORTED_SHAPE;  // (rows of the pool)
   a.qkv = static_cast<const bf16*>(qkv); a.q_out = static_cast<bf16*>(q_out);
   a.cu_seqlens = cu_dev; a.kv_len = kv_len_dev; a.err_word = err_word;
   a.ldqkv = ldqkv; a.n_req = n_req; a.n_tokens = tokens; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
-  a.q_blocks = q_out ? (cfg->n_q_heads + KW_Q_HEADS - 1) / KW_Q_HEADS : 0;
-  const int rows = KW_THREADS / (hd / 16);
-  const dim3 grid((tokens + (rows - 1ll)) / rows, a.q_blocks + 2 * cfg->n_kv_heads), block(KW_THREADS);
+  // few rows: short chains count, so a warp has few heads; many: what concerns a row is done once for many heads
+#ifndef VST
+#define VST (tokens <= 1024 ? 2 : 4)
+#endif
+  const int steps = VST;
+  const int heads = steps * (256 / hd), rows = KW_THREADS / 32;
+  a.q_blocks = q_out ? (cfg->n_q_heads + heads - 1) / heads : 0;
+  const dim3 grid((tokens + (rows - 1ll)) / rows, a.q_blocks + 2 * ((cfg->n_kv_heads + heads - 1) / heads));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_KV_APPEND, st);
-  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, st, a); };
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(KW_THREADS), 0, st, a); };
   const bool pairs = transform->layout == PD_ROPE_PAIRS;
-  PD_CUDA_TRY(hd == 128 ? (pairs ? go(kv4_append_kernel<128, true>) : go(kv4_append_kernel<128, false>))
-                        : (pairs ? go(kv4_append_kernel<64, true>) : go(kv4_append_kernel<64, false>)));
+  auto of_steps = [&](auto n) {
+    constexpr int S = decltype(n)::value;
+    return hd == 128 ? (pairs ? go(kv4_append_kernel<128, true, S>) : go(kv4_append_kernel<128, false, S>))
+                     : (pairs ? go(kv4_append_kernel<64, true, S>) : go(kv4_append_kernel<64, false, S>));
+  };
+  PD_CUDA_TRY(steps == 4 ? of_steps(std::integral_constant<int, 4>()) : of_steps(std::integral_constant<int, 2>()));
   count_launch();
   return PD_OK;
 }
@@ -307,7 +323,7 @@ extern "C" pd_status pd_paged_kv4_write(const pd_layer_cfg* cfg, const pd_paged_
   Kv4CopyArgs a{};
   PD_TRY(copy_args(cfg, cache, begin, end, n_seqs, max_len, in, slots, origin, err_word, &a));
   if (a.n_seqs == 0) return PD_OK;
-  const int rows = KW_THREADS / (cfg->head_dim / 16);
+  const int rows = KW_THREADS / (cfg->head_dim / 8);
   const dim3 grid((max_len + (rows - 1ll)) / rows, cfg->n_kv_heads, n_seqs), block(KW_THREADS);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_KV_APPEND, st);

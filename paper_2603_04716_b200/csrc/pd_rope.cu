@@ -66,9 +66,9 @@ void rope_frequencies(const pd_rope_cfg& r, double* f) {
 }
 
 // -------------------------------------------------------------------------------------------------------------- q and k
-// HBM-bound at size, by launch and the latency of two loads (position, angles) below that.  hd / 16 lanes have a head of a row,
-// four heads of it one after the other with all loads in flight; blocks along y are groups of heads, so that a small batch
-// still covers the SMs.
+// HBM-bound at size, by launch and the latency of two loads (position, angles) below that.  A warp has a row and NR_STEPS * 256
+// features of its heads, all loads in flight; what concerns the row (its position, the angles, their products with the gains) is
+// done once for them.  Blocks along y are groups of heads, so that a small batch still covers the SMs.
 struct NormArgs {
   const bf16* qkv;
   bf16* q_out;
@@ -78,27 +78,43 @@ struct NormArgs {
   QkTransform t;
   int ldqkv, ldq, ldk, rows, n_q_heads, n_kv_heads, q_blocks;
 };
-constexpr int NR_THREADS = 256;
-constexpr int NR_HEADS = 4;
+#ifndef VT
+#define VT 4
+#endif
+#ifndef VS
+#define VS 4
+#endif
+#ifndef VM
+#define VM 8
+#endif
+constexpr int NR_WARPS = VT;
+constexpr int NR_STEPS = VS;
 
 template <int HD, bool PAIRS>
-__global__ void __launch_bounds__(NR_THREADS) qk_norm_rope_kernel(const NormArgs a) {
-  constexpr int J = HD / 16;
+__global__ void __launch_bounds__(NR_WARPS * 32, VM) qk_norm_rope_kernel(const NormArgs a) {
+  constexpr int J = HD / 8, HEADS = NR_STEPS * heads_per_step<HD>();
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const int row = blockIdx.x * (NR_THREADS / J) + threadIdx.x / J, j = threadIdx.x % J;
+  const int row = blockIdx.x * NR_WARPS + __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), j = (threadIdx.x & 31) % J;
+  if (row >= a.rows) return;
   const HeadShare<PAIRS> at(j, a.t.rot);
-  const bool is_q = static_cast<int>(blockIdx.y) < a.q_blocks, there = row < a.rows;
-  const int h0 = (is_q ? blockIdx.y : blockIdx.y - a.q_blocks) * NR_HEADS, n_h = (is_q ? a.n_q_heads : a.n_kv_heads) - h0;
-  const size_t r = there ? row : 0;
-  HeadsOfRow<HD, PAIRS, NR_HEADS> heads(a.qkv + r * a.ldqkv + (is_q ? h0 : a.n_q_heads + h0) * HD, n_h, there, at);
-  const int pos = there ? a.positions[row] : -1;
-  const bool far = a.t.rot > 0 && pos >= a.t.n_pos;
-  if (far && j == 0) report_place(a.err_word);
-  const bool live = pos >= 0 && !far;
-  const float2* angles = a.t.table + static_cast<size_t>(live ? pos : 0) * (a.t.rot / 2);
-  bf16* dst = is_q ? a.q_out + r * a.ldq + h0 * HD : a.k_out + r * a.ldk + h0 * HD;
-  heads.transform(dst, n_h, live, at, is_q ? a.t.q_gain : a.t.k_gain, a.t.eps, angles, j);
+  const bool is_q = static_cast<int>(blockIdx.y) < a.q_blocks;
+  const int h0 = (is_q ? blockIdx.y : blockIdx.y - a.q_blocks) * HEADS, n_heads = min((is_q ? a.n_q_heads : a.n_kv_heads) - h0, HEADS);
+  uint4 w[NR_STEPS];
+  load_heads<HD, PAIRS>(w, a.qkv + static_cast<size_t>(row) * a.ldqkv + (is_q ? h0 : a.n_q_heads + h0) * HD, n_heads, at);
+  const int pos = a.positions[row];
+  if (pos < 0) return;
+  if (a.t.rot > 0 && pos >= a.t.n_pos) {
+    report_place(a.err_word);
+    return;
+  }
+  bf16* dst = is_q ? a.q_out + static_cast<size_t>(row) * a.ldq + h0 * HD : a.k_out + static_cast<size_t>(row) * a.ldk + h0 * HD;
+  const bf16* const gain = is_q ? a.t.q_gain : a.t.k_gain;
+  with_flags(gain != nullptr, a.t.rot == HD, [&](auto norm, auto whole) {
+    constexpr bool NORM = decltype(norm)::value, WHOLE = decltype(whole)::value;
+    transform_heads<HD, PAIRS, NORM, WHOLE>(w, dst, n_heads, at, gain, static_cast<float>(a.t.eps),
+                                            a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j);
+  });
 }
 
 }  // namespace
@@ -157,10 +173,10 @@ extern "C" pd_status pd_qk_norm_rope(const pd_layer_cfg* cfg, const pd_qk_transf
   a.qkv = static_cast<const bf16*>(qkv); a.q_out = static_cast<bf16*>(q_out); a.k_out = static_cast<bf16*>(k_out);
   a.positions = positions; a.err_word = err_word;
   a.ldqkv = ldqkv; a.ldq = ldq_out; a.ldk = ldk_out; a.rows = T; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
-  a.q_blocks = q_out ? (cfg->n_q_heads + NR_HEADS - 1) / NR_HEADS : 0;
-  const int y = a.q_blocks + (k_out ? (cfg->n_kv_heads + NR_HEADS - 1) / NR_HEADS : 0);
-  const int rows_per_block = NR_THREADS / (hd / 16);
-  const dim3 grid((T + (rows_per_block - 1ll)) / rows_per_block, y), block(NR_THREADS);
+  const int heads = NR_STEPS * (256 / hd);
+  a.q_blocks = q_out ? (cfg->n_q_heads + heads - 1) / heads : 0;
+  const int y = a.q_blocks + (k_out ? (cfg->n_kv_heads + heads - 1) / heads : 0);
+  const dim3 grid((T + (NR_WARPS - 1ll)) / NR_WARPS, y), block(NR_WARPS * 32);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, st, a); };
   const bool pairs = transform->layout == PD_ROPE_PAIRS;
