@@ -295,10 +295,7 @@ extern "C" pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_tr
   a.cu_seqlens = cu_dev; a.kv_len = kv_len_dev; a.err_word = err_word;
   a.ldqkv = ldqkv; a.n_req = n_req; a.n_tokens = tokens; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
   // few rows: short chains count, so a warp has few heads; many: what concerns a row is done once for many heads
-#ifndef VST
-#define VST (tokens <= 1024 ? 2 : 4)
-#endif
-  const int steps = VST;
+  const int steps = tokens <= 1024 ? 2 : 4;
   const int heads = steps * (256 / hd), rows = KW_THREADS / 32;
   a.q_blocks = q_out ? (cfg->n_q_heads + heads - 1) / heads : 0;
   const dim3 grid((tokens + (rows - 1ll)) / rows, a.q_blocks + 2 * ((cfg->n_kv_heads + heads - 1) / heads));

@@ -30,39 +30,26 @@ struct Kv4DecodeArgs {
   int* err_word;
   Kv4Cache c;
   int ldq, rows, n_new, n_q_heads, n_kv_heads;
-  int block_tokens, seq_blocks;  // tokens of a block: block_tokens * group columns; blocks of a sequence
-  int n_splits, chunk;           // block x covers keys x * chunk .. (the last one whatever lies behind); chunk is a multiple of 64
+  int col_blocks;             // blocks of KA_COLS (token, head) pairs that a sequence and KV head has
+  int n_splits, chunk;        // part x covers keys x * chunk .. (the last one whatever lies behind); chunk is a multiple of 64
 };
 
-#ifndef VW
-#define VW 4
-#endif
-#ifndef VS
-#define VS 3
-#endif
-#ifndef VB
-#define VB 4
-#endif
-#ifndef VBW
-#define VBW 2
-#endif
-constexpr int KA_WARPS = VW;
-constexpr int KA_THREADS = KA_WARPS * 32;
 constexpr int KA_KEYS = 32;                     // of a tile: two halves of 16, each within a page
-constexpr int KA_STAGES = VS;
+constexpr int KA_STAGES = 3;
+constexpr int KA_COLS = 8;                      // (token, head) pairs of a block
 // p is kept as 2^7 p relative to a reference that may lag the running maximum by 2^6: at most 2^13, with room below f16's 65504 for
 // what 7 - reference loses to rounding where scores are very large.
 constexpr float P_SHIFT = 7.f, P_SLACK = 6.f, P_UNIT = 1.f / 128.f;
 constexpr int KA_MIN_CHUNK = 256;               // keys of a part at least
-constexpr int KA_RESIDENT = 148 * VB;                // blocks that run together (half as many WIDE ones)
+constexpr int KA_RESIDENT_WARPS = 148 * 16;     // warps that run together, in blocks of 4 or 8
 
-template <int HD>
+template <int HD, int WARPS>
 struct Kv4Smem {
   static constexpr int CODES = KA_KEYS * HD / 2, SCALES = KA_KEYS * HD / 16;  // bytes of a tile's K (or V)
   static constexpr int STAGE = 2 * (CODES + SCALES);                          // K codes, V codes, K scales, V scales
-  static constexpr int RING = KA_WARPS * KA_STAGES * STAGE;
+  static constexpr int RING = WARPS * KA_STAGES * STAGE;
   static constexpr int MERGE_ROW = HD + 4;                                    // floats: a row of O, then l
-  static constexpr int MERGE = KA_WARPS * 16 * (MERGE_ROW + 1) * 4;           // and m of all rows behind
+  static constexpr int MERGE = WARPS * KA_COLS * (MERGE_ROW + 1) * 4;         // and m of all rows behind
   static constexpr int BYTES = RING > MERGE ? RING : MERGE;
 };
 
@@ -145,16 +132,18 @@ __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// WIDE: 9 to 16 columns (two column groups in both products).  MULTI: blocks of several tokens, or of sequences with several.
-template <int HD, bool WIDE, bool MULTI>
-__global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel(const Kv4DecodeArgs a) {
-  using SM = Kv4Smem<HD>;
+// MULTI: sequences with several tokens.
+template <int HD, int KA_WARPS, bool MULTI>
+__global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kernel(const Kv4DecodeArgs a) {
+  using SM = Kv4Smem<HD, KA_WARPS>;
+  constexpr int KA_THREADS = KA_WARPS * 32;
   constexpr int KS = HD / 16;          // k-steps of K Q^T
   constexpr int MT = HD / 16;          // 16-feature tiles of O^T
-  constexpr int NC = WIDE ? 2 : 1;     // column groups of 8 (token, head) pairs
   constexpr int W = HD / 32;           // words of codes a lane has of a K row, and 2 W of V rows
   extern __shared__ __align__(128) uint8_t smem[];
-  const int split = blockIdx.x, kvh = blockIdx.y;
+  // The blocks that read the same keys are neighbours, so that all but one of them find them in L2.  Parts come last: what starts
+  // late is what few sequences are long enough for, and ends of sequences.
+  const int kvh = blockIdx.x / a.col_blocks, col0 = (blockIdx.x - kvh * a.col_blocks) * KA_COLS, b = blockIdx.y, split = blockIdx.z;
   const int group = a.n_q_heads / a.n_kv_heads;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, t4 = lane & 3;
@@ -162,11 +151,13 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
   ptx::grid_dependency_wait();
 
   const int l2p = a.c.log2_page, cap = a.c.table_ld << l2p;
-  const int b = MULTI ? blockIdx.z / a.seq_blocks : blockIdx.z;
-  const int tok0 = MULTI ? (blockIdx.z - b * a.seq_blocks) * a.block_tokens : 0;
-  const int n_tok = MULTI ? min(a.block_tokens, a.n_new - tok0) : 1;
-  const int row0 = (MULTI ? b * a.n_new : b) + tok0;
-  const int n_cols = n_tok * group;
+  // Column c of the block is pair col0 + c of the sequence: token (col0 + c) / group, head (col0 + c) % group
+  const int n_cols = min(KA_COLS, a.n_new * group - col0);
+  const int tok0 = MULTI ? col0 / group : 0, skew = col0 - tok0 * group;  // the first column is head `skew` of token tok0
+  const uint32_t inv_group = 65536u / group + 1u;
+  auto token_of = [&](int col) { return MULTI ? static_cast<int>(((col + skew) * inv_group) >> 16) : 0; };  // relative to tok0
+  auto head_of = [&](int col) { return col + skew - token_of(col) * group; };
+  const int n_tok = token_of(n_cols - 1) + 1, row0 = b * a.n_new + tok0;
   // Page numbers of the halves of 32 tiles of this warp at a time, a tile per lane.  The first 32 are read before the sequence's
   // length is known: entries behind its last page are read, too, but not used.
   const int32_t* table = a.c.table + static_cast<size_t>(b) * a.c.table_ld;
@@ -181,18 +172,12 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
   };
   int id_cur[2], id_nxt[2] = {-1, -1};
   fetch_pages(0, id_cur);
-  // Column c * 8 + j is token (c * 8 + j) / group, head (c * 8 + j) % group.  q of column c * 8 + g: this lane's share of all
-  // k-steps, features t4 * hd / 4 ..
-  const uint32_t inv_group = 65536u / group + 1u;
-  auto token_of = [&](int col) { return MULTI ? static_cast<int>((col * inv_group) >> 16) : 0; };
-  uint4 qw[NC][KS / 2];
+  // q of column g: this lane's share of all k-steps, features t4 * hd / 4 ..
+  uint4 qw[KS / 2];
+  {
+    const bf16* src = a.q + static_cast<size_t>(row0 + token_of(g)) * a.ldq + (kvh * group + head_of(g)) * HD + t4 * (HD / 4);
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int tok = token_of(c * 8 + g), head = c * 8 + g - tok * group;
-    const bf16* src = a.q + static_cast<size_t>(row0 + tok) * a.ldq + (kvh * group + head) * HD + t4 * (HD / 4);
-#pragma unroll
-    for (int s = 0; s < KS / 2; ++s)
-      qw[c][s] = c * 8 + g < n_cols ? *reinterpret_cast<const uint4*>(src + s * 8) : make_uint4(0u, 0u, 0u, 0u);
+    for (int s = 0; s < KS / 2; ++s) qw[s] = g < n_cols ? *reinterpret_cast<const uint4*>(src + s * 8) : make_uint4(0u, 0u, 0u, 0u);
   }
   const int len = a.kv_len[b];
   // position of the block's first token; a negative length: a padding sequence, none of its rows sees a key
@@ -203,8 +188,7 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
   const int k_end = split == a.n_splits - 1 ? total : static_cast<int>(min(1ll * total, 1ll * k_begin + a.chunk));
   // the row of column `col` among the partial results, and among the outputs (split 0)
   auto out_row = [&](int col) {
-    const int tok = token_of(col);
-    return static_cast<size_t>(row0 + tok) * a.n_q_heads + kvh * group + col - tok * group;
+    return static_cast<size_t>(row0 + token_of(col)) * a.n_q_heads + kvh * group + head_of(col);
   };
   const size_t part_row0 = static_cast<size_t>(split) * a.rows * a.n_q_heads;
   if (split > 0 && k_begin == k_end) {
@@ -285,15 +269,13 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
   }
 
   // Q^T as f16 operand fragments, every head scaled by a power of two so that its largest entry lies in [1, 2)
-  uint32_t qb[NC][KS][2];
-  float q_scale[NC];  // of the scores of head c * 8 + g, in log2 units
-  const float k_unit = pow2f(kv4_exp(a.c.k_exp, kvh));
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
+  uint32_t qb[KS][2];
+  uint64_t f_pair;  // of the scores of this lane's columns of S^T and O^T, 2 t4 and 2 t4 + 1, in log2 units
+  {
     float x[KS / 2][8], amax = 0.f;
 #pragma unroll
     for (int s = 0; s < KS / 2; ++s) {
-      unpack8(qw[c][s], x[s]);
+      unpack8(qw[s], x[s]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[s][e]));
     }
@@ -302,38 +284,23 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
     // 2^e <= amax < 2^(e+1), e kept where 2^e and 2^-e are normal (an infinite q stays infinite)
     const int e = min(max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -126), 126);
     const float inv = pow2f(-e);
-    q_scale[c] = rsqrtf(static_cast<float>(HD)) * LOG2E * pow2f(e) * k_unit;
+    const float scale = rsqrtf(static_cast<float>(HD)) * LOG2E * pow2f(e) * pow2f(kv4_exp(a.c.k_exp, kvh));
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int p = 0; p < 2; ++p)
-        qb[c][s][p] = pack_f16(x[s / 2][(s & 1) * 4 + 2 * p] * inv, x[s / 2][(s & 1) * 4 + 2 * p + 1] * inv);
-    }
-  }
-  // This lane's columns of S^T and O^T are c * 8 + 2 t4 + h, h = 0, 1.
-  float f_head[NC][2];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    f_head[c][0] = __shfl_sync(0xffffffffu, q_scale[c], t4 * 8);
-    f_head[c][1] = __shfl_sync(0xffffffffu, q_scale[c], t4 * 8 + 4);
+        qb[s][p] = pack_f16(x[s / 2][(s & 1) * 4 + 2 * p] * inv, x[s / 2][(s & 1) * 4 + 2 * p + 1] * inv);
+    f_pair = ptx::pack_f32x2(__shfl_sync(0xffffffffu, scale, t4 * 8), __shfl_sync(0xffffffffu, scale, t4 * 8 + 4));
   }
 
-  float o_acc[NC][MT][4];
+  float o_acc[MT][4];
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int i = 0; i < MT; ++i) o_acc[c][i][0] = o_acc[c][i][1] = o_acc[c][i][2] = o_acc[c][i][3] = 0.f;
-  // Per column pair (packed): reference of the exponent (uniform over the lanes of a head; -inf: no key yet), what is added to a
-  // score for it, and this lane's share of the sum
-  float m_ref[NC][2];
-  uint64_t shift[NC], l_sum[NC], f_pair[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    m_ref[c][0] = m_ref[c][1] = -CUDART_INF_F;
-    shift[c] = ptx::pack_f32x2(P_SHIFT, P_SHIFT);  // (no key yet: every p is 0)
-    l_sum[c] = ptx::pack_f32x2(0.f, 0.f);
-    f_pair[c] = ptx::pack_f32x2(f_head[c][0], f_head[c][1]);
-  }
+  for (int i = 0; i < MT; ++i) o_acc[i][0] = o_acc[i][1] = o_acc[i][2] = o_acc[i][3] = 0.f;
+  // Per column pair: reference of the exponent (uniform over the lanes of a head; -inf: no key yet), what is added to a score for
+  // it, and this lane's share of the sum
+  float m_ref[2] = {-CUDART_INF_F, -CUDART_INF_F};
+  uint64_t shift = ptx::pack_f32x2(P_SHIFT, P_SHIFT);  // (no key yet: every p is 0)
+  uint64_t l_sum = ptx::pack_f32x2(0.f, 0.f);
   bool nan_seen = false;
 
   for (int i = 0; i < my_tiles; ++i) {
@@ -363,10 +330,10 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
     }
 
     // ---- S^T = K Q^T: rows are keys key_of(g) and 8 + key_of(g) of each half, columns (token, head) pairs
-    float x[2][NC][4];  // [half][column group][key half][column] = (e >> 1, e & 1)
+    float x[2][4];  // [half][key half][column] = (e >> 1, e & 1)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float st[NC][2][4];
+      float st[2][4];
       uint32_t w[2][W], sc[2][2];  // rows g, g + 8: codes and scales (as pairs of equal halves)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
@@ -396,92 +363,72 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
         }
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-#pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            const uint32_t b0 = qb[c][2 * j + p][0], b1 = qb[c][2 * j + p][1];
-            if (j == 0) mma_f16_first(st[c][p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], b0, b1);
-            else mma_f16(st[c][p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], b0, b1);
-          }
+          if (j == 0) mma_f16_first(st[p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], qb[2 * j + p][0], qb[2 * j + p][1]);
+          else mma_f16(st[p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], qb[2 * j + p][0], qb[2 * j + p][1]);
         }
       }
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; e += 2)
-          ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(st[c][0][e], st[c][0][e + 1]),
-                                                          ptx::pack_f32x2(st[c][1][e], st[c][1][e + 1])), f_pair[c]),
-                            x[h][c][e], x[h][c][e + 1]);
+      for (int e = 0; e < 4; e += 2)
+        ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(st[0][e], st[0][e + 1]), ptx::pack_f32x2(st[1][e], st[1][e + 1])), f_pair),
+                          x[h][e], x[h][e + 1]);
     }
     // ---- softmax
     if (masked) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
+      for (int e = 0; e < 2; ++e) {
+        // the last key of the tile that the column's token sees
+        const int last = (MULTI ? min(pos0 + token_of(2 * t4 + e), k_end - 1) : k_end - 1) - key0;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          // the last key of the tile that the column's token sees
-          const int last = (MULTI ? min(pos0 + token_of(c * 8 + 2 * t4 + e), k_end - 1) : k_end - 1) - key0;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int lim = (halves >> h) & 1 ? last - 16 * h : -1;
-            if (key_of(g) > lim) x[h][c][e] = -CUDART_INF_F;
-            if (8 + key_of(g) > lim) x[h][c][2 + e] = -CUDART_INF_F;
-          }
+        for (int h = 0; h < 2; ++h) {
+          const int lim = (halves >> h) & 1 ? last - 16 * h : -1;
+          if (key_of(g) > lim) x[h][e] = -CUDART_INF_F;
+          if (8 + key_of(g) > lim) x[h][2 + e] = -CUDART_INF_F;
         }
       }
     }
     // the reference follows the maximum only when that has grown by more than P_SLACK (always at the first key)
-    float mx[NC][2];
+    float mx[2];
     bool grow = false;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        mx[c][e] = fmaxf(ptx::fmax3(x[0][c][e], x[0][c][2 + e], x[1][c][e]), x[1][c][2 + e]);
-        grow |= mx[c][e] > m_ref[c][e] + P_SLACK;
-      }
+    for (int e = 0; e < 2; ++e) {
+      mx[e] = fmaxf(ptx::fmax3(x[0][e], x[0][2 + e], x[1][e]), x[1][2 + e]);
+      grow |= mx[e] > m_ref[e] + P_SLACK;
     }
     if (__any_sync(0xffffffffu, grow)) {
+      float corr[2], add[2];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float corr[2], add[2];
+      for (int e = 0; e < 2; ++e) {
+        float m = mx[e];
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+        const float m_new = fmaxf(m_ref[e], m);
+        corr[e] = m_new == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[e] - m_new);
+        add[e] = P_SHIFT - (m_new == -CUDART_INF_F ? 0.f : m_new);
+        m_ref[e] = m_new;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float m = mx[c][e];
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-          const float m_new = fmaxf(m_ref[c][e], m);
-          corr[e] = m_new == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][e] - m_new);
-          add[e] = P_SHIFT - (m_new == -CUDART_INF_F ? 0.f : m_new);
-          m_ref[c][e] = m_new;
-#pragma unroll
-          for (int n = 0; n < MT; ++n) { o_acc[c][n][e] *= corr[e]; o_acc[c][n][2 + e] *= corr[e]; }
-        }
-        shift[c] = ptx::pack_f32x2(add[0], add[1]);
-        l_sum[c] = ptx::mul_f32x2(l_sum[c], ptx::pack_f32x2(corr[0], corr[1]));
+        for (int n = 0; n < MT; ++n) { o_acc[n][e] *= corr[e]; o_acc[n][2 + e] *= corr[e]; }
       }
+      shift = ptx::pack_f32x2(add[0], add[1]);
+      l_sum = ptx::mul_f32x2(l_sum, ptx::pack_f32x2(corr[0], corr[1]));
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32_t pb[NC][2];
+      uint32_t pb[2];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float y0, y1;
-          // (the rounded score, which is what the reference was taken from: very large ones would not cancel otherwise)
-          ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(x[h][c][2 * k], x[h][c][2 * k + 1]), shift[c]), y0, y1);
-          y0 = ptx::ex2_approx(y0);
-          y1 = ptx::ex2_approx(y1);
-          l_sum[c] = ptx::add_f32x2(l_sum[c], ptx::pack_f32x2(y0, y1));
-          // P^T as an operand: the transpose of the accumulator's 8 x 8 blocks
-          pb[c][k] = transpose8x8(pack_f16(y0, y1));
-        }
+      for (int k = 0; k < 2; ++k) {
+        float y0, y1;
+        // (the rounded score, which is what the reference was taken from: very large ones would not cancel otherwise)
+        ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(x[h][2 * k], x[h][2 * k + 1]), shift), y0, y1);
+        y0 = ptx::ex2_approx(y0);
+        y1 = ptx::ex2_approx(y1);
+        l_sum = ptx::add_f32x2(l_sum, ptx::pack_f32x2(y0, y1));
+        // P^T as an operand: the transpose of the accumulator's 8 x 8 blocks
+        pb[k] = transpose8x8(pack_f16(y0, y1));
       }
       // ---- O^T += V^T P^T: this lane's keys are key_of(2 t4), key_of(2 t4 + 1) = t4, t4 + 4 of both 8-key groups, its features
       // g * hd / 8 ..; two keys share a word's nibbles, low and high
-      uint32_t vw[4][W / 2], sv2[2];
-      uint32_t sb[4];
+      uint32_t vw[4][W / 2], sv2[2], sb[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * h + (r >> 1) * 8 + t4 + (r & 1) * 4;
@@ -507,34 +454,27 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
           for (int n = 0; n < 4; ++n) { even[k][n] = mul_f16x2(even[k][n], sv2[k]); odd[k][n] = mul_f16x2(odd[k][n], sv2[k]); }
         }
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int c = 0; c < NC; ++c) mma_f16(o_acc[c][4 * j + n], even[0][n], odd[0][n], even[1][n], odd[1][n], pb[c][0], pb[c][1]);
+        for (int n = 0; n < 4; ++n) mma_f16(o_acc[4 * j + n], even[0][n], odd[0][n], even[1][n], odd[1][n], pb[0], pb[1]);
       }
     }
     next_stage(stage_out);
     __syncwarp();  // every lane has read this stage before it is refilled
   }
   ptx::cp_async_wait<0>();
-  float l_col[NC][2];
+  float l_col[2];
+  ptx::unpack_f32x2(l_sum, l_col[0], l_col[1]);
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    ptx::unpack_f32x2(l_sum[c], l_col[c][0], l_col[c][1]);
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) l_col[c][h] += __shfl_xor_sync(0xffffffffu, l_col[c][h], o);
-  }
+    for (int o = 4; o < 32; o <<= 1) l_col[h] += __shfl_xor_sync(0xffffffffu, l_col[h], o);
   // Merge: the warps agree on the maximum of every column, scale what they have to it, and add up in shared memory.
   constexpr int RS = SM::MERGE_ROW;
   float* const mrg = reinterpret_cast<float*>(smem);
-  float* const m_all = mrg + KA_WARPS * 16 * RS;  // [column][warp]
+  float* const m_all = mrg + KA_WARPS * KA_COLS * RS;  // [column][warp]
   __syncthreads();  // every warp has left its ring: the memory is reused
   if (g == 0) {
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) m_all[(c * 8 + t4 * 2 + h) * KA_WARPS + warp] = m_ref[c][h];
+    m_all[(t4 * 2) * KA_WARPS + warp] = m_ref[0];
+    m_all[(t4 * 2 + 1) * KA_WARPS + warp] = m_ref[1];
   }
   __syncthreads();
   auto column_max = [&](int col) {
@@ -545,19 +485,16 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
   };
   const float o_unit = P_UNIT * pow2f(kv4_exp(a.c.v_exp, kvh));
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
+  for (int h = 0; h < 2; ++h) {
+    const int col = t4 * 2 + h;
+    if (col < n_cols) {
+      const float m = column_max(col);
+      const float f = m == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[h] - m), fo = f * o_unit;  // 0 for a warp that saw no key
+      float* const dst_row = mrg + (warp * KA_COLS + col) * RS;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int col = c * 8 + t4 * 2 + h;
-      if (col < n_cols) {
-        const float m = column_max(col);
-        const float f = m == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][h] - m), fo = f * o_unit;  // 0 for a warp that saw no key
-        float* const dst_row = mrg + (warp * 16 + col) * RS;
-#pragma unroll
-        for (int n = 0; n < MT; ++n)
-          *reinterpret_cast<float2*>(dst_row + g * (HD / 8) + 2 * n) = make_float2(o_acc[c][n][h] * fo, o_acc[c][n][2 + h] * fo);
-        if (g == 0) dst_row[HD] = l_col[c][h] * (f * P_UNIT);
-      }
+      for (int n = 0; n < MT; ++n)
+        *reinterpret_cast<float2*>(dst_row + g * (HD / 8) + 2 * n) = make_float2(o_acc[n][h] * fo, o_acc[n][2 + h] * fo);
+      if (g == 0) dst_row[HD] = l_col[h] * (f * P_UNIT);
     }
   }
   const bool nans = MULTI ? __syncthreads_or(nan_seen) : (__syncthreads(), false);
@@ -568,7 +505,7 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < KA_WARPS; ++w) {
-      const float* src = mrg + (w * 16 + r) * RS;
+      const float* src = mrg + (w * KA_COLS + r) * RS;
       const float4 v = *reinterpret_cast<const float4*>(src + d);
       l += src[HD];
       o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
@@ -601,52 +538,55 @@ __global__ void __launch_bounds__(KA_THREADS, WIDE ? VBW : VB) kv4_decode_kernel
   }
 }
 
-template <int HD, bool WIDE, bool MULTI>
-pd_status launch_kv4(const Kv4DecodeArgs& a, int slots, cudaStream_t s) {
-  using SM = Kv4Smem<HD>;
+template <int HD, int WARPS, bool MULTI>
+pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, cudaStream_t s) {
+  using SM = Kv4Smem<HD, WARPS>;
   static PerDeviceInt smem_opt_in;
-  PD_TRY(opt_in_smem(smem_opt_in, kv4_decode_kernel<HD, WIDE, MULTI>, SM::BYTES));
-  PD_CUDA_TRY(launch_pdl(kv4_decode_kernel<HD, WIDE, MULTI>, dim3(a.n_splits, a.n_kv_heads, slots), dim3(KA_THREADS), SM::BYTES, s, a));
+  PD_TRY(opt_in_smem(smem_opt_in, kv4_decode_kernel<HD, WARPS, MULTI>, SM::BYTES));
+  PD_CUDA_TRY(launch_pdl(kv4_decode_kernel<HD, WARPS, MULTI>, dim3(a.col_blocks * a.n_kv_heads, batch, a.n_splits), dim3(WARPS * 32), SM::BYTES, s, a));
   count_launch();
   if (a.n_splits > 1) return launch_paged_join(a.parts, a.o, 1ll * a.rows * a.n_q_heads, a.n_splits, HD, s);
   return PD_OK;
 }
 template <int HD>
-pd_status launch_kv4(const Kv4DecodeArgs& a, int slots, cudaStream_t s) {
-  const bool wide = a.block_tokens * (a.n_q_heads / a.n_kv_heads) > 8;
-  if (a.n_new > 1) return wide ? launch_kv4<HD, true, true>(a, slots, s) : launch_kv4<HD, false, true>(a, slots, s);
-  return wide ? launch_kv4<HD, true, false>(a, slots, s) : launch_kv4<HD, false, false>(a, slots, s);
+pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int warps, cudaStream_t s) {
+  if (a.n_new > 1) return warps == 4 ? launch_kv4<HD, 4, true>(a, batch, s) : launch_kv4<HD, 8, true>(a, batch, s);
+  return warps == 4 ? launch_kv4<HD, 4, false>(a, batch, s) : launch_kv4<HD, 8, false>(a, batch, s);
 }
-
-// Tokens of a block: eight columns where the tokens of a sequence fit them (half the registers), else sixteen.
-int kv4_block_tokens(int group, int n_new) { return group * n_new <= 8 ? n_new : std::min(n_new, 16 / group); }
 
 // Key ranges are cut into equal parts while there are fewer blocks than run together, into parts of at least KA_MIN_CHUNK keys
 // and at most `longest` keys.  The sequences of a batch may differ in length, which the host does not know, so a part is at most
-// 4096 keys, and from about one block per SM on half as many parts again as run together even the lengths out.  No more
-// than 16 parts are made for the length alone, since max_kv_len may be a capacity far above the lengths.
-struct Split { int n, chunk; };
-int kv4_most_blocks(long long blocks) { return blocks <= 148 ? KA_RESIDENT : KA_RESIDENT * 3 / 2; }
-Split kv4_split(long long slots, int n_kv_heads, int max_kv_len) {
-  const long long blocks = slots * n_kv_heads;
-  const long long want = std::max(1ll, kv4_most_blocks(blocks) / blocks);
+// 4096 keys, and from a quarter of the blocks that run together on more parts than would run together even the lengths out: half
+// as many again, or, where they are long enough to be worth their join, twice as many (24 sequences of 100 to 4351 keys, 384
+// blocks: 42 us with half as many again, 37 with twice as many; 64 sequences of 2000 keys, 512 blocks: 36 and 41).  No more than 16
+// parts are made for the length alone, since max_kv_len may be a capacity far above the lengths.
+// Blocks have 4 warps, which costs a short stream of tiles less at both ends (256 sequences of 2304 keys: 122 us, 134 with 8), or 8 where
+// the keys of a block are cut into many parts, of which there are half as many to join (one sequence of 32768 keys: 19 and 17 us).
+struct Split { int n, chunk, warps; };
+constexpr int KA_FEW_BLOCKS = 74, KA_MORE_PARTS = 2;
+Split kv4_split(long long blocks, int batch, int max_kv_len) {
+  Split sp;
+  sp.warps = blocks <= KA_FEW_BLOCKS ? 8 : 4;
+  const long long resident = KA_RESIDENT_WARPS / sp.warps;
+  const long long most = blocks <= 148 ? resident : max_kv_len >= 4096 ? resident * KA_MORE_PARTS : resident * 3 / 2;
+  const long long want = std::max(1ll, most / blocks);
   long long chunk = (max_kv_len + want - 1) / want;
-  chunk = std::min(chunk, slots > 1 ? std::max(4096ll, max_kv_len / 16ll) : static_cast<long long>(max_kv_len));
+  chunk = std::min(chunk, batch > 1 ? std::max(4096ll, max_kv_len / 16ll) : static_cast<long long>(max_kv_len));
   chunk = std::min((std::max<long long>(chunk, KA_MIN_CHUNK) + 63) / 64 * 64, 0x7fffffc0ll);
-  return {static_cast<int>((max_kv_len + chunk - 1) / chunk), static_cast<int>(chunk)};
+  sp.n = static_cast<int>((max_kv_len + chunk - 1) / chunk);
+  sp.chunk = static_cast<int>(chunk);
+  return sp;
 }
 // (part, row) pairs, row = (token, query head), that any call of up to these sizes has at most, where it has parts at all: a
-// buffer of that size serves every smaller call, too.  Parts made to fill the GPU are at most as many as kv4_split asks for,
-// of at least KA_MIN_CHUNK keys and at most 16 rows; parts made for their length are as many as the bound allows.
-long long kv4_most_part_rows(int batch, int n_new, int n_q_heads, int n_kv_heads, int max_kv_len) {
+// buffer of that size serves every smaller call, too.  Parts made to fill the GPU are at most as many blocks of KA_COLS rows as
+// kv4_split asks for, of at least KA_MIN_CHUNK keys; parts made for their length are as many as the bound allows.
+long long kv4_most_part_rows(int batch, int n_new, int n_q_heads, int max_kv_len) {
   if (batch <= 0 || n_new <= 0 || max_kv_len <= KA_MIN_CHUNK) return 0;
-  const int group = n_q_heads / n_kv_heads;
-  const long long tokens = std::min(n_new, std::max(16 / group, 1));   // of a block at most
-  const long long by_length = (max_kv_len + (KA_MIN_CHUNK - 1ll)) / KA_MIN_CHUNK;
-  const long long fill = std::min(KA_RESIDENT * 3ll / 2 / n_kv_heads * tokens, by_length * batch * n_new);
+  const long long rows = 1ll * batch * n_new * n_q_heads;
+  const long long fill = std::min(1ll * KA_RESIDENT_WARPS / 4 * KA_MORE_PARTS * KA_COLS, (max_kv_len + (KA_MIN_CHUNK - 1ll)) / KA_MIN_CHUNK * rows);
   // (17: of max_kv_len / 16 keys, rounded down, and what is left)
   const long long length = std::min(17ll, (max_kv_len + 4095ll) / 4096);
-  return std::max(fill, length > 1 ? length * batch * n_new : 0) * n_q_heads;
+  return std::max(fill, length > 1 ? length * rows : 0);
 }
 
 }  // namespace
@@ -656,7 +596,7 @@ extern "C" pd_status pd_paged_kv4_decode_attention_workspace_bytes(const pd_laye
                                                                    size_t* out_bytes) {
   PD_TRY(pd::check_kv4_heads(cfg));
   if (!out_bytes || B < 0 || n_new < 1 || max_kv_len < 0) return PD_ERR_INVALID_ARG;
-  const long long rows = pd::kv4_most_part_rows(B, n_new, cfg->n_q_heads, cfg->n_kv_heads, max_kv_len);
+  const long long rows = pd::kv4_most_part_rows(B, n_new, cfg->n_q_heads, max_kv_len);
   *out_bytes = rows ? pd::paged_parts_bytes(static_cast<size_t>(rows), cfg->head_dim) : 0;
   return PD_OK;
 }
@@ -675,12 +615,11 @@ extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, cons
   if ((reinterpret_cast<uintptr_t>(q) & 15u) || (reinterpret_cast<uintptr_t>(out) & 1u)) return PD_ERR_INVALID_ARG;
   if (max_kv_len < n_new || max_kv_len > (cache->table_ld << a.c.log2_page)) return PD_ERR_INVALID_ARG;
   if ((1ll * cache->n_pages * cfg->n_kv_heads) << a.c.log2_page > 0xffffffffll) return PD_ERR_UNSUPPORTED_SHAPE;  // (rows of the pool)
-  a.block_tokens = kv4_block_tokens(cfg->n_q_heads / cfg->n_kv_heads, n_new);
-  a.seq_blocks = (n_new + a.block_tokens - 1) / a.block_tokens;
-  const long long slots = 1ll * B * a.seq_blocks;
-  if (slots > 65535) return PD_ERR_UNSUPPORTED_SHAPE;
+  const long long pairs = 1ll * n_new * (cfg->n_q_heads / cfg->n_kv_heads);
+  if (B > 65535 || n_new > 65535 || 1ll * B * n_new * cfg->n_q_heads > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
+  a.col_blocks = static_cast<int>((pairs + KA_COLS - 1) / KA_COLS);
   a.rows = B * n_new;
-  const Split sp = kv4_split(slots, cfg->n_kv_heads, max_kv_len);
+  const Split sp = kv4_split(1ll * B * a.col_blocks * cfg->n_kv_heads, B, max_kv_len);
   a.n_splits = sp.n; a.chunk = sp.chunk;
   if (a.n_splits > 1) {
     const size_t part_rows = static_cast<size_t>(a.n_splits) * a.rows * cfg->n_q_heads;
@@ -693,5 +632,5 @@ extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, cons
   a.ldq = ldq; a.n_new = n_new; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_ATTN_DECODE, st);
-  return cfg->head_dim == 128 ? launch_kv4<128>(a, static_cast<int>(slots), st) : launch_kv4<64>(a, static_cast<int>(slots), st);
+  return cfg->head_dim == 128 ? launch_kv4<128>(a, B, sp.warps, st) : launch_kv4<64>(a, B, sp.warps, st);
 }

@@ -1,5 +1,6 @@
 // Rotary positions scaled for long contexts (pd_rope_table_scaled) and the transform of q and k heads in front of attention
 // (pd_qk_norm_rope).
+#include <algorithm>
 #include <cmath>
 
 #include "pd_kv4.cuh"
@@ -10,35 +11,37 @@ namespace {
 // ------------------------------------------------------------------------------------------------------------------ table
 // A thread computes `run` neighbouring positions of one pair: cos and sin of the first from the angle in half turns (product
 // and reduction in double), the others by turning on, 4 fused operations instead of a reduction and two polynomials each.
-// Angles are theirs to 2^-50 relative; 16 steps add 2^-48 at most, far below the final rounding to fp32.
+// Angles are theirs to 2^-50 relative; 16 steps add 2^-48 at most, far below the final rounding to fp32.  A thread keeps its
+// pair for all runs that it does: its three constants differ from lane to lane, and constant memory serves one address at a time
+// (fetched for each run of 16, they took half of the time).
 struct TableArgs {
   double half_turns[64], c[64], s[64];  // f_i / pi, cos f_i, sin f_i
   double magnitude;
   float2* out;  // [n_pos, pairs]
   int first, n_pos, pairs, run;
 };
-constexpr int TB_THREADS = 256;
+constexpr int TB_THREADS = 256;  // at most: as many as are a multiple of the pairs
 
 __global__ void __launch_bounds__(TB_THREADS) rope_table_kernel(const __grid_constant__ TableArgs a) {
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const long long item = 1ll * blockIdx.x * TB_THREADS + threadIdx.x;
-  const int i = static_cast<int>(item % a.pairs);
-  const long long p0 = item / a.pairs * a.run;
-  if (p0 >= a.n_pos) return;
-  const int n = static_cast<int>(min(1ll * a.run, a.n_pos - p0));
-  double s, c;
-  sincospi(static_cast<double>(a.first + p0) * a.half_turns[i], &s, &c);
-  c *= a.magnitude;
-  s *= a.magnitude;
-  const double dc = a.c[i], ds = a.s[i];
-  float2* out = a.out + p0 * a.pairs + i;
+  const int i = threadIdx.x % a.pairs, runs = blockDim.x / a.pairs;
+  const double half_turns = a.half_turns[i], dc = a.c[i], ds = a.s[i];
+  const long long step = 1ll * gridDim.x * runs * a.run;
+  for (long long p0 = (1ll * blockIdx.x * runs + threadIdx.x / a.pairs) * a.run; p0 < a.n_pos; p0 += step) {
+    const int n = static_cast<int>(min(1ll * a.run, a.n_pos - p0));
+    double s, c;
+    sincospi(static_cast<double>(a.first + p0) * half_turns, &s, &c);
+    c *= a.magnitude;
+    s *= a.magnitude;
+    float2* out = a.out + p0 * a.pairs + i;
 #pragma unroll 4
-  for (int k = 0; k < n; ++k) {
-    out[static_cast<size_t>(k) * a.pairs] = make_float2(static_cast<float>(c), static_cast<float>(s));
-    const double c1 = c * dc - s * ds;
-    s = s * dc + c * ds;
-    c = c1;
+    for (int k = 0; k < n; ++k) {
+      out[static_cast<size_t>(k) * a.pairs] = make_float2(static_cast<float>(c), static_cast<float>(s));
+      const double c1 = c * dc - s * ds;
+      s = s * dc + c * ds;
+      c = c1;
+    }
   }
 }
 
@@ -78,20 +81,11 @@ struct NormArgs {
   QkTransform t;
   int ldqkv, ldq, ldk, rows, n_q_heads, n_kv_heads, q_blocks;
 };
-#ifndef VT
-#define VT 4
-#endif
-#ifndef VS
-#define VS 4
-#endif
-#ifndef VM
-#define VM 8
-#endif
-constexpr int NR_WARPS = VT;
-constexpr int NR_STEPS = VS;
+constexpr int NR_WARPS = 4;
+constexpr int NR_STEPS = 4;
 
 template <int HD, bool PAIRS>
-__global__ void __launch_bounds__(NR_WARPS * 32, VM) qk_norm_rope_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(NR_WARPS * 32, 8) qk_norm_rope_kernel(const NormArgs a) {
   constexpr int J = HD / 8, HEADS = NR_STEPS * heads_per_step<HD>();
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
@@ -146,9 +140,9 @@ extern "C" pd_status pd_rope_table_scaled(const pd_rope_cfg* rope, int32_t first
   a.first = first_pos; a.n_pos = n_pos;
   // long runs where there are threads enough for every SM all the same
   a.run = 1ll * n_pos * a.pairs >= (1ll << 22) ? 16 : 4;
-  const long long items = (n_pos + (a.run - 1ll)) / a.run * a.pairs, blocks = (items + TB_THREADS - 1) / TB_THREADS;
-  if (blocks > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
-  PD_CUDA_TRY(launch_pdl(rope_table_kernel, dim3(static_cast<unsigned>(blocks)), dim3(TB_THREADS), 0, static_cast<cudaStream_t>(stream), a));
+  const int runs = TB_THREADS / a.pairs;
+  const long long blocks = std::min((n_pos + (1ll * a.run * runs - 1)) / (1ll * a.run * runs), 148ll * 8);
+  PD_CUDA_TRY(launch_pdl(rope_table_kernel, dim3(static_cast<unsigned>(blocks)), dim3(runs * a.pairs), 0, static_cast<cudaStream_t>(stream), a));
   count_launch();
   return PD_OK;
 }

@@ -160,7 +160,8 @@ def test_decode_workspace_refusals(pdlib):
     refused(pdlib, pdlib.PD_ERR_WORKSPACE_TOO_SMALL, f, workspace_bytes=need // 2)
     wide = cache(pdlib, n_seqs=70000)
     refused(pdlib, pdlib.PD_ERR_UNSUPPORTED_SHAPE, calls(pdlib)["decode"], c=c, k=wide, t=None, batch=65536)
-    refused(pdlib, pdlib.PD_ERR_UNSUPPORTED_SHAPE, calls(pdlib)["decode"], c=c, k=wide, t=None, batch=40000, n_new=7)
+    refused(pdlib, pdlib.PD_ERR_UNSUPPORTED_SHAPE, calls(pdlib)["decode"], c=c, k=cache(pdlib, table_ld=1 << 12), t=None, batch=1, n_new=65536, max_kv_len=65536)
+    refused(pdlib, pdlib.PD_ERR_UNSUPPORTED_SHAPE, calls(pdlib)["decode"], c=c, k=cache(pdlib, n_seqs=70000, table_ld=1 << 12), t=None, batch=60000, n_new=10000, max_kv_len=65536)
     for bad in [(c, -1, 1, 5), (c, 1, 0, 5), (c, 1, 1, -5)]:
         with pytest.raises(pdlib.PdError):
             pdlib.pd_paged_kv4_decode_attention_workspace_bytes(*bad)
