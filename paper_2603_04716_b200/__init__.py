@@ -672,13 +672,21 @@ class RopeConfig:
     magnitude: float = 1.0
 
     def c_struct(self) -> pd_rope_cfg:
+        """A C struct of this configuration, the caller's own."""
         return pd_rope_cfg(C.sizeof(pd_rope_cfg), self.rot_dim, self.scaling, self.trained_len, self.theta, self.factor,
                            self.low, self.high, self.magnitude)
+
+    def _c_ref(self):
+        made = self.__dict__.get("_made")
+        if made is None:
+            made = self.c_struct()
+            object.__setattr__(self, "_made", made)
+        return C.byref(made)
 
 
 def pd_rope_table_scaled(rope: RopeConfig, first_pos: int, n_pos: int, table, stream=None):
     """table: device fp32 [n_pos, rot_dim / 2, 2] -> cos and sin of positions first_pos .. first_pos + n_pos - 1."""
-    _check(_lib.pd_rope_table_scaled(C.byref(rope.c_struct()), first_pos, n_pos, _ptr(table), _stream_ptr(stream)),
+    _check(_lib.pd_rope_table_scaled(rope._c_ref(), first_pos, n_pos, _ptr(table), _stream_ptr(stream)),
            "pd_rope_table_scaled")
 
 
