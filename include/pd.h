@@ -620,8 +620,8 @@ pd_status pd_paged_kv4_read(const pd_layer_cfg* cfg, const pd_paged_kv4_cache* c
  *   q, out        device bf16 [B * n_new, ldq] / [B * n_new, Hq*hd], q 16-byte aligned, out only as its elements are, ldq a
  *                 multiple of 8
  *   kv_len_dev    device int32[B]; a sequence with kv_len[b] < 0 gets all-zero rows; entries beyond the table are left out
- *   B, n_new      at most 65535, n_new at least 1, B * n_new * Hq below 2^31.  The keys are fetched once for every 8 (token, query
- *                 head) pairs of a KV head, all but the first time from L2
+ *   B, n_new      at most 65535, n_new at least 1, B * n_new * Hq below 2^31.  The keys are fetched once for every 16 (token,
+ *                 query head) pairs of a KV head, all but the first time from L2
  *   max_kv_len    host upper bound of kv_len[b] + n_new, at most table_ld * page_len (it sizes the split of the key range; a
  *                 longer sequence is still computed whole)
  *   workspace     at least pd_paged_kv4_decode_attention_workspace_bytes() bytes, 256-byte aligned (may be NULL where that is

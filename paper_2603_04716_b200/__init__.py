@@ -304,13 +304,17 @@ class LayerConfig:
         return pd_layer_cfg(C.sizeof(pd_layer_cfg), self.d_model, self.n_q_heads, self.n_kv_heads, self.head_dim,
                             self.d_ff, self.rms_eps, self.rope_theta, self.max_pos, int(self.fp8_projections))
 
-    def _c_ref(self):
-        """A reference to the struct that the calls of this module pass, made once (the library only reads it)."""
+    def _c(self):
+        """The struct that the calls of this module pass, made once (the library only reads it)."""
         made = self.__dict__.get("_made")
         if made is None:
             made = self.c_struct()
             object.__setattr__(self, "_made", made)
-        return C.byref(made)
+        return made
+
+    def _c_ref(self):
+        """A reference to it."""
+        return C.byref(self._c())
 
     @property
     def n_qkv(self) -> int:
@@ -655,6 +659,7 @@ def pd_paged_prefill_attention(cfg: LayerConfig, q, ldq: int, out, cu_seqlens_de
            "pd_paged_prefill_attention")
 
 
+# (structs go to these calls as they are: ctypes passes their address, in less time than a reference to them takes)
 ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_TURNS, ROPE_SCALE_INDEX = range(5)
 ROPE_HALVES, ROPE_PAIRS = range(2)
 
@@ -676,17 +681,17 @@ class RopeConfig:
         return pd_rope_cfg(C.sizeof(pd_rope_cfg), self.rot_dim, self.scaling, self.trained_len, self.theta, self.factor,
                            self.low, self.high, self.magnitude)
 
-    def _c_ref(self):
+    def _c(self):
         made = self.__dict__.get("_made")
         if made is None:
             made = self.c_struct()
             object.__setattr__(self, "_made", made)
-        return C.byref(made)
+        return made
 
 
 def pd_rope_table_scaled(rope: RopeConfig, first_pos: int, n_pos: int, table, stream=None):
     """table: device fp32 [n_pos, rot_dim / 2, 2] -> cos and sin of positions first_pos .. first_pos + n_pos - 1."""
-    _check(_lib.pd_rope_table_scaled(rope._c_ref(), first_pos, n_pos, _ptr(table), _stream_ptr(stream)),
+    _check(_lib.pd_rope_table_scaled(rope._c(), first_pos, n_pos, _ptr(table), _stream_ptr(stream)),
            "pd_rope_table_scaled")
 
 
@@ -699,7 +704,7 @@ def qk_transform_struct(table, n_pos: int, rot_dim: int, layout: int = ROPE_HALV
 def pd_qk_norm_rope(cfg: LayerConfig, transform: pd_qk_transform, qkv, ldqkv: int, q_out, ldq_out: int, k_out, ldk_out: int,
                     positions_dev, rows: int, err_word=None, stream=None):
     """q_out, k_out: device bf16 rows, None to leave q or k alone; qkv itself (k: behind its q heads) with ldqkv for in place."""
-    _check(_lib.pd_qk_norm_rope(cfg._c_ref(), C.byref(transform), _ptr(qkv), ldqkv, _ptr(q_out), ldq_out, _ptr(k_out), ldk_out,
+    _check(_lib.pd_qk_norm_rope(cfg._c(), transform, _ptr(qkv), ldqkv, _ptr(q_out), ldq_out, _ptr(k_out), ldk_out,
                                 _ptr(positions_dev), rows, _ptr(err_word), _stream_ptr(stream)), "pd_qk_norm_rope")
 
 
@@ -718,27 +723,27 @@ def pd_paged_kv4_append(cfg: LayerConfig, transform: pd_qk_transform, qkv, ldqkv
         if len(cu_seqlens_host) != n_req + 1:
             raise ValueError("cu_seqlens has one entry more than there are requests")
         cu = _i32_array(cu_seqlens_host)
-    _check(_lib.pd_paged_kv4_append(cfg._c_ref(), C.byref(transform), _ptr(qkv), ldqkv, _ptr(q_out), _ptr(cu_seqlens_dev), cu, n_req,
-                                    _ptr(kv_len_dev), C.byref(cache), _ptr(err_word), _stream_ptr(stream)), "pd_paged_kv4_append")
+    _check(_lib.pd_paged_kv4_append(cfg._c(), transform, _ptr(qkv), ldqkv, _ptr(q_out), _ptr(cu_seqlens_dev), cu, n_req,
+                                    _ptr(kv_len_dev), cache, _ptr(err_word), _stream_ptr(stream)), "pd_paged_kv4_append")
 
 
 def pd_paged_kv4_write(cfg: LayerConfig, cache: pd_paged_kv4_cache, begin_dev, end_dev, n_seqs: int, max_len: int,
                        kv_in: pd_kv_cache, slots_dev=None, origin_dev=None, err_word=None, stream=None):
     """Positions begin .. end - 1 of every sequence from a bf16 cache into the 4-bit pages."""
-    _check(_lib.pd_paged_kv4_write(cfg._c_ref(), C.byref(cache), _ptr(begin_dev), _ptr(end_dev), n_seqs, max_len, C.byref(kv_in),
+    _check(_lib.pd_paged_kv4_write(cfg._c(), cache, _ptr(begin_dev), _ptr(end_dev), n_seqs, max_len, kv_in,
                                    _ptr(slots_dev), _ptr(origin_dev), _ptr(err_word), _stream_ptr(stream)), "pd_paged_kv4_write")
 
 
 def pd_paged_kv4_read(cfg: LayerConfig, cache: pd_paged_kv4_cache, begin_dev, end_dev, n_seqs: int, max_len: int,
                       kv_out: pd_kv_cache, slots_dev=None, origin_dev=None, err_word=None, stream=None):
     """Positions begin .. end - 1 of every sequence from the 4-bit pages into a bf16 cache, exactly."""
-    _check(_lib.pd_paged_kv4_read(cfg._c_ref(), C.byref(cache), _ptr(begin_dev), _ptr(end_dev), n_seqs, max_len, C.byref(kv_out),
+    _check(_lib.pd_paged_kv4_read(cfg._c(), cache, _ptr(begin_dev), _ptr(end_dev), n_seqs, max_len, kv_out,
                                   _ptr(slots_dev), _ptr(origin_dev), _ptr(err_word), _stream_ptr(stream)), "pd_paged_kv4_read")
 
 
 def pd_paged_kv4_decode_attention_workspace_bytes(cfg: LayerConfig, batch: int, n_new: int, max_kv_len: int) -> int:
     out = C.c_size_t(0)
-    _check(_lib.pd_paged_kv4_decode_attention_workspace_bytes(cfg._c_ref(), batch, n_new, max_kv_len, C.byref(out)),
+    _check(_lib.pd_paged_kv4_decode_attention_workspace_bytes(cfg._c(), batch, n_new, max_kv_len, C.byref(out)),
            "pd_paged_kv4_decode_attention_workspace_bytes")
     return out.value
 
@@ -746,8 +751,8 @@ def pd_paged_kv4_decode_attention_workspace_bytes(cfg: LayerConfig, batch: int, 
 def pd_paged_kv4_decode_attention(cfg: LayerConfig, q, ldq: int, out, kv_len_dev, batch: int, n_new: int, max_kv_len: int,
                                   cache: pd_paged_kv4_cache, workspace, workspace_bytes: int, err_word=None, stream=None):
     """Row b * n_new + j of q and out: token j of sequence b, at position kv_len[b] + j."""
-    _check(_lib.pd_paged_kv4_decode_attention(cfg._c_ref(), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch, n_new, max_kv_len,
-                                              C.byref(cache), _ptr(workspace), workspace_bytes, _ptr(err_word),
+    _check(_lib.pd_paged_kv4_decode_attention(cfg._c(), _ptr(q), ldq, _ptr(out), _ptr(kv_len_dev), batch, n_new, max_kv_len,
+                                              cache, _ptr(workspace), workspace_bytes, _ptr(err_word),
                                               _stream_ptr(stream)), "pd_paged_kv4_decode_attention")
 
 

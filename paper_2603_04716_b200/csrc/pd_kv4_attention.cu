@@ -36,20 +36,22 @@ struct Kv4DecodeArgs {
 
 constexpr int KA_KEYS = 32;                     // of a tile: two halves of 16, each within a page
 constexpr int KA_STAGES = 3;
-constexpr int KA_COLS = 8;                      // (token, head) pairs of a block
 // p is kept as 2^7 p relative to a reference that may lag the running maximum by 2^6: at most 2^13, with room below f16's 65504 for
 // what 7 - reference loses to rounding where scores are very large.
 constexpr float P_SHIFT = 7.f, P_SLACK = 6.f, P_UNIT = 1.f / 128.f;
 constexpr int KA_MIN_CHUNK = 256;               // keys of a part at least
-constexpr int KA_RESIDENT_WARPS = 148 * 16;     // warps that run together, in blocks of 4 or 8
+// (token, head) pairs, the columns of both products: one or two groups of 8 a block.  A second group shares the conversion of K and V,
+// half of a tile's instructions, and costs registers: 12 warps of an SM run together instead of 16.
+constexpr int ka_cols(int col_groups) { return 8 * col_groups; }
+constexpr int ka_resident_warps(int col_groups) { return 148 * (col_groups == 1 ? 16 : 12); }
 
-template <int HD, int WARPS>
+template <int HD, int WARPS, int NC>
 struct Kv4Smem {
   static constexpr int CODES = KA_KEYS * HD / 2, SCALES = KA_KEYS * HD / 16;  // bytes of a tile's K (or V)
   static constexpr int STAGE = 2 * (CODES + SCALES);                          // K codes, V codes, K scales, V scales
   static constexpr int RING = WARPS * KA_STAGES * STAGE;
   static constexpr int MERGE_ROW = HD + 4;                                    // floats: a row of O, then l
-  static constexpr int MERGE = WARPS * KA_COLS * (MERGE_ROW + 1) * 4;         // and m of all rows behind
+  static constexpr int MERGE = WARPS * ka_cols(NC) * (MERGE_ROW + 1) * 4;     // and m of all rows behind
   static constexpr int BYTES = RING > MERGE ? RING : MERGE;
 };
 
@@ -132,10 +134,11 @@ __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// MULTI: sequences with several tokens.
-template <int HD, int KA_WARPS, bool MULTI>
-__global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kernel(const Kv4DecodeArgs a) {
-  using SM = Kv4Smem<HD, KA_WARPS>;
+// NC: groups of 8 columns.  MULTI: sequences with several tokens.
+template <int HD, int KA_WARPS, int NC, bool MULTI>
+__global__ void __launch_bounds__(KA_WARPS * 32, ka_resident_warps(NC) / 148 / KA_WARPS) kv4_decode_kernel(const Kv4DecodeArgs a) {
+  using SM = Kv4Smem<HD, KA_WARPS, NC>;
+  constexpr int KA_COLS = ka_cols(NC);
   constexpr int KA_THREADS = KA_WARPS * 32;
   constexpr int KS = HD / 16;          // k-steps of K Q^T
   constexpr int MT = HD / 16;          // 16-feature tiles of O^T
@@ -172,12 +175,14 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
   };
   int id_cur[2], id_nxt[2] = {-1, -1};
   fetch_pages(0, id_cur);
-  // q of column g: this lane's share of all k-steps, features t4 * hd / 4 ..
-  uint4 qw[KS / 2];
-  {
-    const bf16* src = a.q + static_cast<size_t>(row0 + token_of(g)) * a.ldq + (kvh * group + head_of(g)) * HD + t4 * (HD / 4);
+  // q of column 8 c + g: this lane's share of all k-steps, features t4 * hd / 4 ..
+  uint4 qw[NC][KS / 2];
 #pragma unroll
-    for (int s = 0; s < KS / 2; ++s) qw[s] = g < n_cols ? *reinterpret_cast<const uint4*>(src + s * 8) : make_uint4(0u, 0u, 0u, 0u);
+  for (int c = 0; c < NC; ++c) {
+    const int col = 8 * c + g;
+    const bf16* src = a.q + static_cast<size_t>(row0 + token_of(col)) * a.ldq + (kvh * group + head_of(col)) * HD + t4 * (HD / 4);
+#pragma unroll
+    for (int s = 0; s < KS / 2; ++s) qw[c][s] = col < n_cols ? *reinterpret_cast<const uint4*>(src + s * 8) : make_uint4(0u, 0u, 0u, 0u);
   }
   const int len = a.kv_len[b];
   // position of the block's first token; a negative length: a padding sequence, none of its rows sees a key
@@ -268,14 +273,17 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
     ptx::cp_async_commit();
   }
 
-  // Q^T as f16 operand fragments, every head scaled by a power of two so that its largest entry lies in [1, 2)
-  uint32_t qb[KS][2];
-  uint64_t f_pair;  // of the scores of this lane's columns of S^T and O^T, 2 t4 and 2 t4 + 1, in log2 units
-  {
+  // Q^T as f16 operand fragments, every head scaled by a power of two so that its largest entry lies in [1, 2).  With two groups of
+  // columns they stay in shared memory, the same for all warps.
+  __shared__ __align__(16) uint4 q_frag[NC == 1 ? 1 : NC][KS / 2][NC == 1 ? 1 : 32];  // of a pair of k-steps
+  uint4 qb[KS / 2];
+  uint64_t f_pair[NC];  // of the scores of this lane's columns of S^T and O^T, 8 c + 2 t4 and the next, in log2 units
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
     float x[KS / 2][8], amax = 0.f;
 #pragma unroll
     for (int s = 0; s < KS / 2; ++s) {
-      unpack8(qw[s], x[s]);
+      unpack8(qw[c][s], x[s]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[s][e]));
     }
@@ -286,21 +294,31 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
     const float inv = pow2f(-e);
     const float scale = rsqrtf(static_cast<float>(HD)) * LOG2E * pow2f(e) * pow2f(kv4_exp(a.c.k_exp, kvh));
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-        qb[s][p] = pack_f16(x[s / 2][(s & 1) * 4 + 2 * p] * inv, x[s / 2][(s & 1) * 4 + 2 * p + 1] * inv);
-    f_pair = ptx::pack_f32x2(__shfl_sync(0xffffffffu, scale, t4 * 8), __shfl_sync(0xffffffffu, scale, t4 * 8 + 4));
+    for (int s = 0; s < KS / 2; ++s) {
+      qb[s] = make_uint4(pack_f16(x[s][0] * inv, x[s][1] * inv), pack_f16(x[s][2] * inv, x[s][3] * inv),
+                         pack_f16(x[s][4] * inv, x[s][5] * inv), pack_f16(x[s][6] * inv, x[s][7] * inv));
+      if (NC > 1 && warp == 0) q_frag[c][s][lane] = qb[s];
+    }
+    f_pair[c] = ptx::pack_f32x2(__shfl_sync(0xffffffffu, scale, t4 * 8), __shfl_sync(0xffffffffu, scale, t4 * 8 + 4));
   }
+  const uint32_t q_at = NC > 1 ? ptx::smem_u32(&q_frag[0][0][NC == 1 ? 0 : lane]) : 0;
+  if (NC > 1) __syncthreads();
 
-  float o_acc[MT][4];
+  float o_acc[NC][MT][4];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) o_acc[i][0] = o_acc[i][1] = o_acc[i][2] = o_acc[i][3] = 0.f;
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) o_acc[c][i][0] = o_acc[c][i][1] = o_acc[c][i][2] = o_acc[c][i][3] = 0.f;
   // Per column pair: reference of the exponent (uniform over the lanes of a head; -inf: no key yet), what is added to a score for
   // it, and this lane's share of the sum
-  float m_ref[2] = {-CUDART_INF_F, -CUDART_INF_F};
-  uint64_t shift = ptx::pack_f32x2(P_SHIFT, P_SHIFT);  // (no key yet: every p is 0)
-  uint64_t l_sum = ptx::pack_f32x2(0.f, 0.f);
+  float m_ref[NC][2];
+  uint64_t shift[NC], l_sum[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m_ref[c][0] = m_ref[c][1] = -CUDART_INF_F;
+    shift[c] = ptx::pack_f32x2(P_SHIFT, P_SHIFT);  // (no key yet: every p is 0)
+    l_sum[c] = ptx::pack_f32x2(0.f, 0.f);
+  }
   bool nan_seen = false;
 
   for (int i = 0; i < my_tiles; ++i) {
@@ -330,10 +348,10 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
     }
 
     // ---- S^T = K Q^T: rows are keys key_of(g) and 8 + key_of(g) of each half, columns (token, head) pairs
-    float x[2][4];  // [half][key half][column] = (e >> 1, e & 1)
+    float x[2][NC][4];  // [half][column group][key half][column] = (e >> 1, e & 1)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float st[2][4];
+      float st[NC][2][4];
       uint32_t w[2][W], sc[2][2];  // rows g, g + 8: codes and scales (as pairs of equal halves)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
@@ -362,69 +380,90 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
           a1[e] = mul_f16x2(a1[e], sc[1][j / 2]);
         }
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          if (j == 0) mma_f16_first(st[p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], qb[2 * j + p][0], qb[2 * j + p][1]);
-          else mma_f16(st[p], a0[2 * p], a1[2 * p], a0[2 * p + 1], a1[2 * p + 1], qb[2 * j + p][0], qb[2 * j + p][1]);
+        for (int c = 0; c < NC; ++c) {
+          const uint4 b = NC > 1 ? lds128(q_at + (c * (KS / 2) + j) * 512) : qb[j];
+          if (j == 0) {
+            mma_f16_first(st[c][0], a0[0], a1[0], a0[1], a1[1], b.x, b.y);
+            mma_f16_first(st[c][1], a0[2], a1[2], a0[3], a1[3], b.z, b.w);
+          } else {
+            mma_f16(st[c][0], a0[0], a1[0], a0[1], a1[1], b.x, b.y);
+            mma_f16(st[c][1], a0[2], a1[2], a0[3], a1[3], b.z, b.w);
+          }
         }
       }
 #pragma unroll
-      for (int e = 0; e < 4; e += 2)
-        ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(st[0][e], st[0][e + 1]), ptx::pack_f32x2(st[1][e], st[1][e + 1])), f_pair),
-                          x[h][e], x[h][e + 1]);
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2)
+          ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(st[c][0][e], st[c][0][e + 1]),
+                                                          ptx::pack_f32x2(st[c][1][e], st[c][1][e + 1])), f_pair[c]),
+                            x[h][c][e], x[h][c][e + 1]);
     }
     // ---- softmax
     if (masked) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        // the last key of the tile that the column's token sees
-        const int last = (MULTI ? min(pos0 + token_of(2 * t4 + e), k_end - 1) : k_end - 1) - key0;
+      for (int c = 0; c < NC; ++c) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int lim = (halves >> h) & 1 ? last - 16 * h : -1;
-          if (key_of(g) > lim) x[h][e] = -CUDART_INF_F;
-          if (8 + key_of(g) > lim) x[h][2 + e] = -CUDART_INF_F;
+        for (int e = 0; e < 2; ++e) {
+          // the last key of the tile that the column's token sees
+          const int last = (MULTI ? min(pos0 + token_of(8 * c + 2 * t4 + e), k_end - 1) : k_end - 1) - key0;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int lim = (halves >> h) & 1 ? last - 16 * h : -1;
+            if (key_of(g) > lim) x[h][c][e] = -CUDART_INF_F;
+            if (8 + key_of(g) > lim) x[h][c][2 + e] = -CUDART_INF_F;
+          }
         }
       }
     }
     // the reference follows the maximum only when that has grown by more than P_SLACK (always at the first key)
-    float mx[2];
+    float mx[NC][2];
     bool grow = false;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      mx[e] = fmaxf(ptx::fmax3(x[0][e], x[0][2 + e], x[1][e]), x[1][2 + e]);
-      grow |= mx[e] > m_ref[e] + P_SLACK;
-    }
-    if (__any_sync(0xffffffffu, grow)) {
-      float corr[2], add[2];
+    for (int c = 0; c < NC; ++c) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float m = mx[e];
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-        const float m_new = fmaxf(m_ref[e], m);
-        corr[e] = m_new == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[e] - m_new);
-        add[e] = P_SHIFT - (m_new == -CUDART_INF_F ? 0.f : m_new);
-        m_ref[e] = m_new;
-#pragma unroll
-        for (int n = 0; n < MT; ++n) { o_acc[n][e] *= corr[e]; o_acc[n][2 + e] *= corr[e]; }
+        mx[c][e] = fmaxf(ptx::fmax3(x[0][c][e], x[0][c][2 + e], x[1][c][e]), x[1][c][2 + e]);
+        grow |= mx[c][e] > m_ref[c][e] + P_SLACK;
       }
-      shift = ptx::pack_f32x2(add[0], add[1]);
-      l_sum = ptx::mul_f32x2(l_sum, ptx::pack_f32x2(corr[0], corr[1]));
+    }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float corr[2], add[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float m = mx[c][e];
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+          const float m_new = fmaxf(m_ref[c][e], m);
+          corr[e] = m_new == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][e] - m_new);
+          add[e] = P_SHIFT - (m_new == -CUDART_INF_F ? 0.f : m_new);
+          m_ref[c][e] = m_new;
+#pragma unroll
+          for (int n = 0; n < MT; ++n) { o_acc[c][n][e] *= corr[e]; o_acc[c][n][2 + e] *= corr[e]; }
+        }
+        shift[c] = ptx::pack_f32x2(add[0], add[1]);
+        l_sum[c] = ptx::mul_f32x2(l_sum[c], ptx::pack_f32x2(corr[0], corr[1]));
+      }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32_t pb[2];
+      uint32_t pb[NC][2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float y0, y1;
-        // (the rounded score, which is what the reference was taken from: very large ones would not cancel otherwise)
-        ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(x[h][2 * k], x[h][2 * k + 1]), shift), y0, y1);
-        y0 = ptx::ex2_approx(y0);
-        y1 = ptx::ex2_approx(y1);
-        l_sum = ptx::add_f32x2(l_sum, ptx::pack_f32x2(y0, y1));
-        // P^T as an operand: the transpose of the accumulator's 8 x 8 blocks
-        pb[k] = transpose8x8(pack_f16(y0, y1));
+      for (int c = 0; c < NC; ++c) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float y0, y1;
+          // (the rounded score, which is what the reference was taken from: very large ones would not cancel otherwise)
+          ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(x[h][c][2 * k], x[h][c][2 * k + 1]), shift[c]), y0, y1);
+          y0 = ptx::ex2_approx(y0);
+          y1 = ptx::ex2_approx(y1);
+          l_sum[c] = ptx::add_f32x2(l_sum[c], ptx::pack_f32x2(y0, y1));
+          // P^T as an operand: the transpose of the accumulator's 8 x 8 blocks
+          pb[c][k] = transpose8x8(pack_f16(y0, y1));
+        }
       }
       // ---- O^T += V^T P^T: this lane's keys are key_of(2 t4), key_of(2 t4 + 1) = t4, t4 + 4 of both 8-key groups, its features
       // g * hd / 8 ..; two keys share a word's nibbles, low and high
@@ -454,27 +493,35 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
           for (int n = 0; n < 4; ++n) { even[k][n] = mul_f16x2(even[k][n], sv2[k]); odd[k][n] = mul_f16x2(odd[k][n], sv2[k]); }
         }
 #pragma unroll
-        for (int n = 0; n < 4; ++n) mma_f16(o_acc[4 * j + n], even[0][n], odd[0][n], even[1][n], odd[1][n], pb[0], pb[1]);
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) mma_f16(o_acc[c][4 * j + n], even[0][n], odd[0][n], even[1][n], odd[1][n], pb[c][0], pb[c][1]);
       }
     }
     next_stage(stage_out);
     __syncwarp();  // every lane has read this stage before it is refilled
   }
   ptx::cp_async_wait<0>();
-  float l_col[2];
-  ptx::unpack_f32x2(l_sum, l_col[0], l_col[1]);
+  float l_col[NC][2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int c = 0; c < NC; ++c) {
+    ptx::unpack_f32x2(l_sum[c], l_col[c][0], l_col[c][1]);
 #pragma unroll
-    for (int o = 4; o < 32; o <<= 1) l_col[h] += __shfl_xor_sync(0xffffffffu, l_col[h], o);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) l_col[c][h] += __shfl_xor_sync(0xffffffffu, l_col[c][h], o);
+  }
   // Merge: the warps agree on the maximum of every column, scale what they have to it, and add up in shared memory.
   constexpr int RS = SM::MERGE_ROW;
   float* const mrg = reinterpret_cast<float*>(smem);
   float* const m_all = mrg + KA_WARPS * KA_COLS * RS;  // [column][warp]
   __syncthreads();  // every warp has left its ring: the memory is reused
   if (g == 0) {
-    m_all[(t4 * 2) * KA_WARPS + warp] = m_ref[0];
-    m_all[(t4 * 2 + 1) * KA_WARPS + warp] = m_ref[1];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      m_all[(8 * c + t4 * 2) * KA_WARPS + warp] = m_ref[c][0];
+      m_all[(8 * c + t4 * 2 + 1) * KA_WARPS + warp] = m_ref[c][1];
+    }
   }
   __syncthreads();
   auto column_max = [&](int col) {
@@ -485,16 +532,19 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
   };
   const float o_unit = P_UNIT * pow2f(kv4_exp(a.c.v_exp, kvh));
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int col = t4 * 2 + h;
-    if (col < n_cols) {
-      const float m = column_max(col);
-      const float f = m == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[h] - m), fo = f * o_unit;  // 0 for a warp that saw no key
-      float* const dst_row = mrg + (warp * KA_COLS + col) * RS;
+  for (int c = 0; c < NC; ++c) {
 #pragma unroll
-      for (int n = 0; n < MT; ++n)
-        *reinterpret_cast<float2*>(dst_row + g * (HD / 8) + 2 * n) = make_float2(o_acc[n][h] * fo, o_acc[n][2 + h] * fo);
-      if (g == 0) dst_row[HD] = l_col[h] * (f * P_UNIT);
+    for (int h = 0; h < 2; ++h) {
+      const int col = 8 * c + t4 * 2 + h;
+      if (col < n_cols) {
+        const float m = column_max(col);
+        const float f = m == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m_ref[c][h] - m), fo = f * o_unit;  // 0 for a warp that saw no key
+        float* const dst_row = mrg + (warp * KA_COLS + col) * RS;
+#pragma unroll
+        for (int n = 0; n < MT; ++n)
+          *reinterpret_cast<float2*>(dst_row + g * (HD / 8) + 2 * n) = make_float2(o_acc[c][n][h] * fo, o_acc[c][n][2 + h] * fo);
+        if (g == 0) dst_row[HD] = l_col[c][h] * (f * P_UNIT);
+      }
     }
   }
   const bool nans = MULTI ? __syncthreads_or(nan_seen) : (__syncthreads(), false);
@@ -538,20 +588,21 @@ __global__ void __launch_bounds__(KA_WARPS * 32, 16 / KA_WARPS) kv4_decode_kerne
   }
 }
 
-template <int HD, int WARPS, bool MULTI>
+template <int HD, int WARPS, int NC, bool MULTI>
 pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, cudaStream_t s) {
-  using SM = Kv4Smem<HD, WARPS>;
+  using SM = Kv4Smem<HD, WARPS, NC>;
   static PerDeviceInt smem_opt_in;
-  PD_TRY(opt_in_smem(smem_opt_in, kv4_decode_kernel<HD, WARPS, MULTI>, SM::BYTES));
-  PD_CUDA_TRY(launch_pdl(kv4_decode_kernel<HD, WARPS, MULTI>, dim3(a.col_blocks * a.n_kv_heads, batch, a.n_splits), dim3(WARPS * 32), SM::BYTES, s, a));
+  PD_TRY(opt_in_smem(smem_opt_in, kv4_decode_kernel<HD, WARPS, NC, MULTI>, SM::BYTES));
+  PD_CUDA_TRY(launch_pdl(kv4_decode_kernel<HD, WARPS, NC, MULTI>, dim3(a.col_blocks * a.n_kv_heads, batch, a.n_splits), dim3(WARPS * 32), SM::BYTES, s, a));
   count_launch();
   if (a.n_splits > 1) return launch_paged_join(a.parts, a.o, 1ll * a.rows * a.n_q_heads, a.n_splits, HD, s);
   return PD_OK;
 }
 template <int HD>
-pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int warps, cudaStream_t s) {
-  if (a.n_new > 1) return warps == 4 ? launch_kv4<HD, 4, true>(a, batch, s) : launch_kv4<HD, 8, true>(a, batch, s);
-  return warps == 4 ? launch_kv4<HD, 4, false>(a, batch, s) : launch_kv4<HD, 8, false>(a, batch, s);
+pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int col_groups, int warps, cudaStream_t s) {
+  if (col_groups == 2) return a.n_new > 1 ? launch_kv4<HD, 4, 2, true>(a, batch, s) : launch_kv4<HD, 4, 2, false>(a, batch, s);
+  if (a.n_new > 1) return warps == 4 ? launch_kv4<HD, 4, 1, true>(a, batch, s) : launch_kv4<HD, 8, 1, true>(a, batch, s);
+  return warps == 4 ? launch_kv4<HD, 4, 1, false>(a, batch, s) : launch_kv4<HD, 8, 1, false>(a, batch, s);
 }
 
 // Key ranges are cut into equal parts while there are fewer blocks than run together, into parts of at least KA_MIN_CHUNK keys
@@ -564,10 +615,10 @@ pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int warps, cudaStream_t 
 // the keys of a block are cut into many parts, of which there are half as many to join (one sequence of 32768 keys: 19 and 17 us).
 struct Split { int n, chunk, warps; };
 constexpr int KA_FEW_BLOCKS = 74, KA_MORE_PARTS = 2;
-Split kv4_split(long long blocks, int batch, int max_kv_len) {
+Split kv4_split(long long blocks, int col_groups, int batch, int max_kv_len) {
   Split sp;
-  sp.warps = blocks <= KA_FEW_BLOCKS ? 8 : 4;
-  const long long resident = KA_RESIDENT_WARPS / sp.warps;
+  sp.warps = col_groups == 1 && blocks <= KA_FEW_BLOCKS ? 8 : 4;
+  const long long resident = ka_resident_warps(col_groups) / sp.warps;
   const long long most = blocks <= 148 ? resident : max_kv_len >= 4096 ? resident * KA_MORE_PARTS : resident * 3 / 2;
   const long long want = std::max(1ll, most / blocks);
   long long chunk = (max_kv_len + want - 1) / want;
@@ -578,12 +629,12 @@ Split kv4_split(long long blocks, int batch, int max_kv_len) {
   return sp;
 }
 // (part, row) pairs, row = (token, query head), that any call of up to these sizes has at most, where it has parts at all: a
-// buffer of that size serves every smaller call, too.  Parts made to fill the GPU are at most as many blocks of KA_COLS rows as
-// kv4_split asks for, of at least KA_MIN_CHUNK keys; parts made for their length are as many as the bound allows.
+// buffer of that size serves every smaller call, too.  Parts made to fill the GPU are at most as many blocks of 16 rows as
+// kv4_split asks for (two groups of columns; of one, fewer rows), of at least KA_MIN_CHUNK keys; parts made for their length are as many as the bound allows.
 long long kv4_most_part_rows(int batch, int n_new, int n_q_heads, int max_kv_len) {
   if (batch <= 0 || n_new <= 0 || max_kv_len <= KA_MIN_CHUNK) return 0;
   const long long rows = 1ll * batch * n_new * n_q_heads;
-  const long long fill = std::min(1ll * KA_RESIDENT_WARPS / 4 * KA_MORE_PARTS * KA_COLS, (max_kv_len + (KA_MIN_CHUNK - 1ll)) / KA_MIN_CHUNK * rows);
+  const long long fill = std::min(1ll * ka_resident_warps(2) / 4 * KA_MORE_PARTS * ka_cols(2), (max_kv_len + (KA_MIN_CHUNK - 1ll)) / KA_MIN_CHUNK * rows);
   // (17: of max_kv_len / 16 keys, rounded down, and what is left)
   const long long length = std::min(17ll, (max_kv_len + 4095ll) / 4096);
   return std::max(fill, length > 1 ? length * rows : 0);
@@ -617,9 +668,10 @@ extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, cons
   if ((1ll * cache->n_pages * cfg->n_kv_heads) << a.c.log2_page > 0xffffffffll) return PD_ERR_UNSUPPORTED_SHAPE;  // (rows of the pool)
   const long long pairs = 1ll * n_new * (cfg->n_q_heads / cfg->n_kv_heads);
   if (B > 65535 || n_new > 65535 || 1ll * B * n_new * cfg->n_q_heads > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
-  a.col_blocks = static_cast<int>((pairs + KA_COLS - 1) / KA_COLS);
+  const int col_groups = pairs > 8 ? 2 : 1;
+  a.col_blocks = static_cast<int>((pairs + ka_cols(col_groups) - 1) / ka_cols(col_groups));
   a.rows = B * n_new;
-  const Split sp = kv4_split(1ll * B * a.col_blocks * cfg->n_kv_heads, B, max_kv_len);
+  const Split sp = kv4_split(1ll * B * a.col_blocks * cfg->n_kv_heads, col_groups, B, max_kv_len);
   a.n_splits = sp.n; a.chunk = sp.chunk;
   if (a.n_splits > 1) {
     const size_t part_rows = static_cast<size_t>(a.n_splits) * a.rows * cfg->n_q_heads;
@@ -632,5 +684,5 @@ extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, cons
   a.ldq = ldq; a.n_new = n_new; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_ATTN_DECODE, st);
-  return cfg->head_dim == 128 ? launch_kv4<128>(a, B, sp.warps, st) : launch_kv4<64>(a, B, sp.warps, st);
+  return cfg->head_dim == 128 ? launch_kv4<128>(a, B, col_groups, sp.warps, st) : launch_kv4<64>(a, B, col_groups, sp.warps, st);
 }
