@@ -559,7 +559,7 @@ pd_status pd_qk_norm_rope(const pd_layer_cfg* cfg, const pd_qk_transform* transf
  *   k_exp, v_exp        device int32 [Hkv], a power of two per head, from a calibration; NULL: 0.  Held to -30 .. 30
  *   page_table          device int32 [n_seqs, table_ld]: position p of sequence s lies in page page_table[s][p / page_len], row
  *                       p % page_len.  Entries of pages that hold no token are not used (they may be read).
- *   page_len            16, 32, 64 or 128;  table_ld * page_len below 2^31
+ *   page_len            16, 32, 64 or 128;  table_ld * page_len below 2^31, n_pages * Hkv * page_len at most 2^32 - 1
  * value = code * scale * 2^exp[head].  Of 16 neighbouring features x, in units of 2^exp: scale = E4M3(max|x| / 6), saturating at
  * 448, code = E2M1(x / scale), saturating at 6, both rounded to nearest even from the exact quotient; a scale of 0 has codes of
  * 0.  So magnitudes from 2^-10 to 2688 times 2^exp are represented, and 16 features none of which exceeds 6 * 2^-10 times 2^exp are
@@ -605,7 +605,7 @@ pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_transform* tr
  *   origin       device int32[n_seqs]: position p is row p - origin[s] of the bf16 cache; NULL: 0
  *   err_word     optional device int32, set to 2 where a position is negative, lies beyond the page table or has a page number
  *                outside the pool, or where a slot or a row lies outside the bf16 cache; such rows are left out
- * Rows outside the range are left as they were.  k and v of the bf16 cache start on 16-byte boundaries.  n_seqs at most 65535 and
+ * Rows outside the range are left as they were.  Two sequences of one call must not write the same row.  k and v of the bf16 cache start on 16-byte boundaries.  n_seqs at most 65535 and
  * the n_seqs of the page table.  Only enqueues work; one kernel; no workspace. */
 pd_status pd_paged_kv4_write(const pd_layer_cfg* cfg, const pd_paged_kv4_cache* cache, const int32_t* begin, const int32_t* end,
                              int32_t n_seqs, int32_t max_len, const pd_kv_cache* in, const int32_t* slots, const int32_t* origin,

@@ -23,8 +23,8 @@ struct Kv4Cache {
   int n_pages, log2_page, table_ld;
 };
 
-// Checks the description (not the device contents) and fills the device view.
-inline pd_status kv4_cache_view(const pd_paged_kv4_cache* c, Kv4Cache* out) {
+// Checks the description (not the device contents) and fills the device view; kv_heads: of the configuration, checked before.
+inline pd_status kv4_cache_view(const pd_paged_kv4_cache* c, int kv_heads, Kv4Cache* out) {
   if (!c || c->struct_size != sizeof(pd_paged_kv4_cache)) return PD_ERR_INVALID_ARG;
   if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales || !c->page_table) return PD_ERR_INVALID_ARG;
   if (c->n_pages <= 0 || c->n_seqs <= 0 || c->table_ld <= 0) return PD_ERR_INVALID_ARG;
@@ -43,6 +43,7 @@ inline pd_status kv4_cache_view(const pd_paged_kv4_cache* c, Kv4Cache* out) {
   }
   // positions are 32-bit: table_ld pages must not reach past them
   if (c->table_ld > (0x7fffffff >> l2)) return PD_ERR_UNSUPPORTED_SHAPE;
+  if ((1ll * c->n_pages * kv_heads) << l2 > 0xffffffffll) return PD_ERR_UNSUPPORTED_SHAPE;  // (so are rows of the pool)
   out->k = static_cast<uint8_t*>(c->k_codes); out->v = static_cast<uint8_t*>(c->v_codes);
   out->k_scale = static_cast<uint8_t*>(c->k_scales); out->v_scale = static_cast<uint8_t*>(c->v_scales);
   out->k_exp = c->k_exp; out->v_exp = c->v_exp; out->table = c->page_table;

@@ -74,6 +74,7 @@ __global__ void __launch_bounds__(KW_THREADS, STEPS == 4 ? 8 : 5) kv4_append_ker
   const int len = a.kv_len[req];
   if (len < 0) return;  // a request that is left out
   const long long p = 1ll * len + (row - first);
+  if (p < 0) return;  // (never with consistent inputs)
   if (a.t.rot > 0 ? p >= a.t.n_pos : p > 0x7fffffffll) {
     report_place(a.err_word);
     return;
@@ -253,7 +254,7 @@ pd_status copy_args(const pd_layer_cfg* cfg, const pd_paged_kv4_cache* cache, co
                     int32_t max_len, const pd_kv_cache* flat, const int32_t* slots, const int32_t* origin, int32_t* err_word,
                     Kv4CopyArgs* a) {
   PD_TRY(check_kv4_heads(cfg));
-  PD_TRY(kv4_cache_view(cache, &a->c));
+  PD_TRY(kv4_cache_view(cache, cfg->n_kv_heads, &a->c));
   if (!flat || flat->struct_size != sizeof(pd_kv_cache) || n_seqs < 0 || n_seqs > cache->n_seqs || max_len < 0) return PD_ERR_INVALID_ARG;
   if (n_seqs > 65535) return PD_ERR_UNSUPPORTED_SHAPE;
   if (n_seqs == 0 || max_len == 0) return PD_OK;
@@ -275,7 +276,7 @@ extern "C" pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_tr
   using namespace pd;
   PD_TRY(check_kv4_heads(cfg));
   Kv4AppendArgs a{};
-  PD_TRY(kv4_cache_view(cache, &a.c));
+  PD_TRY(kv4_cache_view(cache, cfg->n_kv_heads, &a.c));
   PD_TRY(qk_transform_view(transform, cfg, &a.t));
   if (n_req < 0 || n_req > cache->n_seqs || (cu_dev == nullptr) != (cu_host == nullptr)) return PD_ERR_INVALID_ARG;
   int tokens = n_req;
@@ -290,7 +291,6 @@ extern "C" pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_tr
   const long long width = (cfg->n_q_heads + 2ll * cfg->n_kv_heads) * hd;
   if (!qkv || !kv_len_dev || ldqkv < width || ldqkv % 8 != 0) return PD_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(qkv) | reinterpret_cast<uintptr_t>(q_out)) & 15u) return PD_ERR_INVALID_ARG;
-  if ((1ll * cache->n_pages * cfg->n_kv_heads) << a.c.log2_page > 0xffffffffll) return PD_ERR_UNSUPPORTED_SHAPE;  // (rows of the pool)
   a.qkv = static_cast<const bf16*>(qkv); a.q_out = static_cast<bf16*>(q_out);
   a.cu_seqlens = cu_dev; a.kv_len = kv_len_dev; a.err_word = err_word;
   a.ldqkv = ldqkv; a.n_req = n_req; a.n_tokens = tokens; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;

@@ -659,13 +659,12 @@ extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, cons
   using namespace pd;
   PD_TRY(check_kv4_heads(cfg));
   Kv4DecodeArgs a{};
-  PD_TRY(kv4_cache_view(cache, &a.c));
+  PD_TRY(kv4_cache_view(cache, cfg->n_kv_heads, &a.c));
   if (B < 0 || B > cache->n_seqs || n_new < 1) return PD_ERR_INVALID_ARG;
   if (B == 0) return PD_OK;
   if (!q || !out || !kv_len_dev || ldq < 1ll * cfg->n_q_heads * cfg->head_dim || ldq % 8 != 0) return PD_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(q) & 15u) || (reinterpret_cast<uintptr_t>(out) & 1u)) return PD_ERR_INVALID_ARG;
   if (max_kv_len < n_new || max_kv_len > (cache->table_ld << a.c.log2_page)) return PD_ERR_INVALID_ARG;
-  if ((1ll * cache->n_pages * cfg->n_kv_heads) << a.c.log2_page > 0xffffffffll) return PD_ERR_UNSUPPORTED_SHAPE;  // (rows of the pool)
   const long long pairs = 1ll * n_new * (cfg->n_q_heads / cfg->n_kv_heads);
   if (B > 65535 || n_new > 65535 || 1ll * B * n_new * cfg->n_q_heads > 0x7fffffffll) return PD_ERR_UNSUPPORTED_SHAPE;
   const int col_groups = pairs > 8 ? 2 : 1;

@@ -47,7 +47,7 @@ def test_struct_layouts(pdlib):
 BAD_CACHES = [dict(k_codes=None), dict(v_codes=None), dict(k_scales=None), dict(v_scales=None), dict(page_table=None), dict(n_pages=0),
               dict(n_seqs=0), dict(table_ld=0), dict(n_pages=-1), dict(k_codes=PTR + 8), dict(v_scales=PTR + 8), dict(k_exp=PTR + 2),
               dict(v_exp=PTR + 1), dict(page_table=PTR + 2)]
-BAD_PAGES = [dict(page_len=0), dict(page_len=24), dict(page_len=256), dict(page_len=8), dict(table_ld=1 << 25)]
+BAD_PAGES = [dict(n_pages=1 << 26), dict(page_len=0), dict(page_len=24), dict(page_len=256), dict(page_len=8), dict(table_ld=1 << 25)]
 BAD_TURNS = [dict(layout=2), dict(layout=-1), dict(rot_dim=0), dict(rot_dim=80), dict(n_pos=0), dict(n_pos=-4), dict(eps=-1.0),
              dict(eps=float("nan")), dict(eps=float("inf")), dict(table=PTR + 8), dict(q_gain=PTR + 2), dict(k_gain=PTR + 8)]
 
