@@ -180,13 +180,14 @@ __device__ __forceinline__ void with_flags(bool norm, bool whole, F f) {
 
 // ---- q, in fp32: n_heads heads of a row, rounded to bf16 once.  Gain and rotation are one product with a matrix of two by two
 // per pair, the same for all heads of the row; the factor that the norm has in common comes last.
-template <int HD, bool PAIRS, bool NORM, bool WHOLE, int STEPS>
-__device__ __forceinline__ void transform_heads(const uint4 (&w)[STEPS], bf16* first_head, int n_heads, const HeadShare<PAIRS>& at,
-                                                const bf16* gain, float eps, const float2* angles, int j) {
-  const bool turns = WHOLE || at.turns;
+template <int HD, bool PAIRS, bool NORM, bool WHOLE>
+struct FastTransform {
   uint64_t mu[2], mv[2], nu[2], nv[2];  // first = mu first + nu second, second = mv second + nv first
-  at.unpack(NORM ? at.load(gain) : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), mu, mv);
-  if (turns) {
+  bool turns;
+  __device__ __forceinline__ FastTransform(const HeadShare<PAIRS>& at, const bf16* gain, const float2* angles, int j) {
+    turns = WHOLE || at.turns;
+    at.unpack(NORM ? at.load(gain) : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), mu, mv);
+    if (!turns) return;
     const float4* const cs = reinterpret_cast<const float4*>(angles + 4 * j);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -198,34 +199,37 @@ __device__ __forceinline__ void transform_heads(const uint4 (&w)[STEPS], bf16* f
       mv[i] = ptx::mul_f32x2(mv[i], c);
     }
   }
-  const int mine = (threadIdx.x & 31) / (HD / 8);
-  bf16* const head = first_head + mine * HD;
+  template <int STEPS>
+  __device__ __forceinline__ void operator()(const uint4 (&w)[STEPS], bf16* first_head, int n_heads, const HeadShare<PAIRS>& at, float eps) const {
+    const int mine = (threadIdx.x & 31) / (HD / 8);
+    bf16* const head = first_head + mine * HD;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    uint64_t u[2], v[2], x[2], y[2];
-    at.unpack(w[s], u, v);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x[i] = ptx::mul_f32x2(u[i], mu[i]);
-      y[i] = ptx::mul_f32x2(v[i], mv[i]);
-      if (turns) {
-        x[i] = ptx::fma_f32x2(v[i], nu[i], x[i]);
-        y[i] = ptx::fma_f32x2(u[i], nv[i], y[i]);
-      }
-    }
-    if (NORM) {
-      float lo, hi, r;
-      ptx::unpack_f32x2(ptx::fma_f32x2(u[1], u[1], ptx::fma_f32x2(v[0], v[0], ptx::fma_f32x2(v[1], v[1], ptx::mul_f32x2(u[0], u[0])))), lo, hi);
-      asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(fmaf(lanes_sum<HD / 8>(lo + hi), 1.f / HD, eps)));
+    for (int s = 0; s < STEPS; ++s) {
+      uint64_t u[2], v[2], x[2], y[2];
+      at.unpack(w[s], u, v);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        x[i] = ptx::mul_f32x2(x[i], dup_f32x2(r));
-        y[i] = ptx::mul_f32x2(y[i], dup_f32x2(r));
+        x[i] = ptx::mul_f32x2(u[i], mu[i]);
+        y[i] = ptx::mul_f32x2(v[i], mv[i]);
+        if (turns) {
+          x[i] = ptx::fma_f32x2(v[i], nu[i], x[i]);
+          y[i] = ptx::fma_f32x2(u[i], nv[i], y[i]);
+        }
       }
+      if (NORM) {
+        float lo, hi, r;
+        ptx::unpack_f32x2(ptx::fma_f32x2(u[1], u[1], ptx::fma_f32x2(v[0], v[0], ptx::fma_f32x2(v[1], v[1], ptx::mul_f32x2(u[0], u[0])))), lo, hi);
+        asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(fmaf(lanes_sum<HD / 8>(lo + hi), 1.f / HD, eps)));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          x[i] = ptx::mul_f32x2(x[i], dup_f32x2(r));
+          y[i] = ptx::mul_f32x2(y[i], dup_f32x2(r));
+        }
+      }
+      if (s * heads_per_step<HD>() + mine < n_heads) at.store(head + s * 256, at.pack(x, y));
     }
-    if (s * heads_per_step<HD>() + mine < n_heads) at.store(head + s * 256, at.pack(x, y));
   }
-}
+};
 
 // The 8 features of a share in memory order of its chunks.
 __device__ __forceinline__ void unpack_share(const uint4& w, float (&f)[8]) {

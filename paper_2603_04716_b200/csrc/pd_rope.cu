@@ -106,8 +106,8 @@ __global__ void __launch_bounds__(NR_WARPS * 32, 8) qk_norm_rope_kernel(const No
   const bf16* const gain = is_q ? a.t.q_gain : a.t.k_gain;
   with_flags(gain != nullptr, a.t.rot == HD, [&](auto norm, auto whole) {
     constexpr bool NORM = decltype(norm)::value, WHOLE = decltype(whole)::value;
-    transform_heads<HD, PAIRS, NORM, WHOLE>(w, dst, n_heads, at, gain, static_cast<float>(a.t.eps),
-                                            a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j);
+    const FastTransform<HD, PAIRS, NORM, WHOLE> transform(at, gain, a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j);
+    transform(w, dst, n_heads, at, static_cast<float>(a.t.eps));
   });
 }
 

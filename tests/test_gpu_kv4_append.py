@@ -205,6 +205,24 @@ def test_read_back(pdlib, hkv, hd, page_len):
         np.testing.assert_array_equal(from_dev(v), want_v)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_read_into_a_cache_that_starts_on_sixteen_bytes(pdlib, hd):
+    import torch
+    hkv, n = 3, 50
+    c = Cache4(pdlib, hkv, hd, 16, [n], seed=hd).fill([n], np.random.default_rng(hd)).upload()
+    cfg = pdlib.LayerConfig(hkv * hd, hkv, hkv, hd, 64)
+    k, v = (torch.zeros(hkv * 60 * hd + 16, dtype=torch.int16, device="cuda") for _ in range(2))
+    assert k.data_ptr() % 32 == 0
+    back = pdlib.kv_cache_struct(k.data_ptr() + 16, v.data_ptr() + 16, 1, 60)
+    pdlib.pd_paged_kv4_read(cfg, c.struct, None, i32_dev([n]), 1, n, back)
+    for dev, want in zip((k, v), c.kv(0, n)):
+        got = from_dev(dev)
+        assert not got[:8].any() and not got[-8:].any()
+        got = got[8:-8].reshape(hkv, 60, hd)
+        np.testing.assert_array_equal(got[:, :n].transpose(1, 0, 2), want)
+        assert not got[:, n:].any()
+
+
 def test_read_reports_what_has_no_place(pdlib):
     import torch
     hkv, hd, p = 2, 64, 16
