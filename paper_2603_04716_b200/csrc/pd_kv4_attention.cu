@@ -10,6 +10,10 @@
 // four V rows per 16 keys: its scales are a byte or two per row.  Features of two V rows are paired by shifts and masks on whole
 // words before they are converted.  q is scaled by a power of two per head into f16 range.  The reference of the exponent
 // follows the maximum lazily, so a tile costs one vote instead of a reduction over its keys.  Softmax statistics and O are fp32.
+// A tile of 32 keys costs a warp 565 instructions (128 conversions, 128 products with scales, 32 MMAs), a warp 660 more at both ends:
+// instructions and their latency bind as much as HBM.  Measured, heads of 128: 256 sequences of 2,304 keys, 32 / 8 heads (640 MB)
+// 117 to 131 us, 4.9 to 5.5 TB/s; each 1,024 keys more cost 52 us (5.8 TB/s), and pages shared in L2 take the same time.  24 sequences of
+// 100 to 4,351 keys, two tokens, 64 / 8 heads 30 us; one of 32,768 keys 17.
 #include <math_constants.h>
 
 #include <algorithm>

@@ -13,7 +13,8 @@ namespace {
 // and reduction in double), the others by turning on, 4 fused operations instead of a reduction and two polynomials each.
 // Angles are theirs to 2^-50 relative; 16 steps add 2^-48 at most, far below the final rounding to fp32.  A thread keeps its
 // pair for all runs that it does: its three constants differ from lane to lane, and constant memory serves one address at a time
-// (fetched for each run of 16, they took half of the time).
+// (fetched for each run of 16, they cost 14.1 us instead of 13.0 for 131,072 positions of 64 pairs; 25 for runs of 8).  67 MB written at
+// 5.2 TB/s; 1000 positions of 32 pairs take 2.3 us, mostly the launch and the first angle.
 struct TableArgs {
   double half_turns[64], c[64], s[64];  // f_i / pi, cos f_i, sin f_i
   double magnitude;
@@ -72,6 +73,7 @@ void rope_frequencies(const pd_rope_cfg& r, double* f) {
 // HBM-bound at size, by launch and the latency of two loads (position, angles) below that.  A warp has a row and NR_STEPS * 256
 // features of its heads, all loads in flight; what concerns the row (its position, the angles, their products with the gains) is
 // done once for them.  Blocks along y are groups of heads, so that a small batch still covers the SMs.
+// Measured: 4,099 rows of 32 + 8 heads of 128 (84 MB) 15.5 us, 5.5 TB/s; 200 rows of 64 + 8 heads 3.0 us.
 struct NormArgs {
   const bf16* qkv;
   bf16* q_out;
