@@ -2,7 +2,8 @@
 //
 // o = softmax(q K^T / sqrt(hd)) V per query head over the sequence's pages; K and V are E2M1 codes times an E4M3 scale per 16
 // features.  HBM-bound: 0.5625 bytes per element, read once (by every block of tokens).  One block per (part of the key range,
-// KV head, sequence and block of tokens); every warp streams its own 32-key tiles through a private cp.async ring.
+// KV head, sequence and block of tokens); parts join in a cluster or in a kernel of their own; every
+// warp streams its own 32-key tiles through a private cp.async ring.
 //   S^T = K Q^T    m16n8k16 in f16: rows are 16 keys, columns 8 (token, head of the group) pairs.
 //   O^T = V^T P^T  m16n8k16: rows are features.
 // A code times its scale has six significant bits and lies in 2^-10 .. 2688: exact in f16.  The contraction order of a product
@@ -40,6 +41,7 @@ struct Kv4DecodeArgs {
 
 constexpr int KA_KEYS = 32;                     // of a tile: two halves of 16, each within a page
 constexpr int KA_STAGES = 3;
+constexpr int KA_CLUSTER = 8;                   // parts that can meet in a cluster at most
 // p is kept as 2^7 p relative to a reference that may lag the running maximum by 2^6: at most 2^13, with room below f16's 65504 for
 // what 7 - reference loses to rounding where scores are very large.
 constexpr float P_SHIFT = 7.f, P_SLACK = 6.f, P_UNIT = 1.f / 128.f;
@@ -55,7 +57,7 @@ struct Kv4Smem {
   static constexpr int STAGE = 2 * (CODES + SCALES);                          // K codes, V codes, K scales, V scales
   static constexpr int RING = WARPS * KA_STAGES * STAGE;
   static constexpr int MERGE_ROW = HD + 4;                                    // floats: a row of O, then l
-  static constexpr int MERGE = WARPS * ka_cols(NC) * (MERGE_ROW + 1) * 4;     // and m of all rows behind
+  static constexpr int MERGE = (WARPS * (MERGE_ROW + 1) + 2) * ka_cols(NC) * 4;  // m of all rows behind, and (m, l) of the columns
   static constexpr int BYTES = RING > MERGE ? RING : MERGE;
 };
 
@@ -138,8 +140,9 @@ __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// NC: groups of 8 columns.  MULTI: sequences with several tokens.
-template <int HD, int KA_WARPS, int NC, bool MULTI>
+// NC: groups of 8 columns.  MULTI: sequences with several tokens.  TOGETHER: the parts of a key range are a cluster, which joins them
+// itself.
+template <int HD, int KA_WARPS, int NC, bool MULTI, bool TOGETHER>
 __global__ void __launch_bounds__(KA_WARPS * 32, ka_resident_warps(NC) / 148 / KA_WARPS) kv4_decode_kernel(const Kv4DecodeArgs a) {
   using SM = Kv4Smem<HD, KA_WARPS, NC>;
   constexpr int KA_COLS = ka_cols(NC);
@@ -201,7 +204,7 @@ __global__ void __launch_bounds__(KA_WARPS * 32, ka_resident_warps(NC) / 148 / K
   };
   const size_t part_row0 = static_cast<size_t>(split) * a.rows * a.n_q_heads;
   if (split > 0 && k_begin == k_end) {
-    if (tid < n_cols) a.parts.ml[part_row0 + out_row(tid)] = make_float2(-CUDART_INF_F, 0.f);
+    if (!TOGETHER && tid < n_cols) a.parts.ml[part_row0 + out_row(tid)] = make_float2(-CUDART_INF_F, 0.f);
     return;
   }
   const int n_tiles_blk = static_cast<int>((static_cast<uint32_t>(k_end - k_begin) + KA_KEYS - 1) / KA_KEYS);
@@ -519,6 +522,7 @@ __global__ void __launch_bounds__(KA_WARPS * 32, ka_resident_warps(NC) / 148 / K
   constexpr int RS = SM::MERGE_ROW;
   float* const mrg = reinterpret_cast<float*>(smem);
   float* const m_all = mrg + KA_WARPS * KA_COLS * RS;  // [column][warp]
+  float2* const ml = reinterpret_cast<float2*>(m_all + KA_WARPS * KA_COLS);
   __syncthreads();  // every warp has left its ring: the memory is reused
   if (g == 0) {
 #pragma unroll
@@ -553,6 +557,19 @@ __global__ void __launch_bounds__(KA_WARPS * 32, ka_resident_warps(NC) / 148 / K
   }
   const bool nans = MULTI ? __syncthreads_or(nan_seen) : (__syncthreads(), false);
   const bool pairs = (reinterpret_cast<uintptr_t>(a.o) & 3u) == 0;
+  auto store_out = [&](size_t row, int d, const float4& o, float l) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // (no visible entry: zeros)
+    const uint32_t lo = ptx::pack_bf16(o.x * inv, o.y * inv), hi = ptx::pack_bf16(o.z * inv, o.w * inv);
+    bf16* const dst = a.o + row * HD + d;
+    if (pairs) {
+      reinterpret_cast<uint32_t*>(dst)[0] = lo;
+      reinterpret_cast<uint32_t*>(dst)[1] = hi;
+    } else {  // results that start between two words
+      uint16_t* const dst16 = reinterpret_cast<uint16_t*>(dst);
+      dst16[0] = static_cast<uint16_t>(lo); dst16[1] = static_cast<uint16_t>(lo >> 16);
+      dst16[2] = static_cast<uint16_t>(hi); dst16[3] = static_cast<uint16_t>(hi >> 16);
+    }
+  };
   for (int idx = tid * 4; idx < n_cols * HD; idx += KA_THREADS * 4) {  // four neighbouring features of a column
     const int r = idx / HD, d = idx - r * HD;
     float l = 0.f;
@@ -573,40 +590,80 @@ __global__ void __launch_bounds__(KA_WARPS * 32, ka_resident_warps(NC) / 148 / K
         if ((a.c.v_scale[at * (HD / 16) + d / 16] & 0x7f) == 0x7f) o = make_float4(CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F);
       }
     }
-    if (a.n_splits == 1) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;  // (no visible entry: zeros)
-      const uint32_t lo = ptx::pack_bf16(o.x * inv, o.y * inv), hi = ptx::pack_bf16(o.z * inv, o.w * inv);
-      bf16* const dst = a.o + row * HD + d;
-      if (pairs) {
-        reinterpret_cast<uint32_t*>(dst)[0] = lo;
-        reinterpret_cast<uint32_t*>(dst)[1] = hi;
-      } else {  // results that start between two words
-        uint16_t* const dst16 = reinterpret_cast<uint16_t*>(dst);
-        dst16[0] = static_cast<uint16_t>(lo); dst16[1] = static_cast<uint16_t>(lo >> 16);
-        dst16[2] = static_cast<uint16_t>(hi); dst16[3] = static_cast<uint16_t>(hi >> 16);
-      }
+    if (!TOGETHER && a.n_splits == 1) {
+      store_out(row, d, o, l);
+    } else if (TOGETHER) {
+      *reinterpret_cast<float4*>(mrg + r * RS + d) = o;  // (the first warp's row: read by this thread alone, but for l behind it)
+      if (d == 0) ml[r] = make_float2(column_max(r), l);
     } else {
       *reinterpret_cast<float4*>(a.parts.o + (part_row0 + row) * HD + d) = o;
       if (d == 0) a.parts.ml[part_row0 + row] = make_float2(column_max(r), l);
     }
   }
+  if (!TOGETHER) return;
+  // The parts that have keys meet (those without have left: a barrier does not wait for them), and each joins a share of the rows
+  // over all of them.
+  const int n_parts = min(a.n_splits, max(1, static_cast<int>((static_cast<uint32_t>(total) + a.chunk - 1) / a.chunk)));
+  __syncwarp();
+  ptx::cluster_sync_all();
+  for (int idx = (split * KA_THREADS + tid) * 4; idx < n_cols * HD; idx += n_parts * KA_THREADS * 4) {
+    const int r = idx / HD, d = idx - r * HD;
+    const uint32_t ml_at = ptx::smem_u32(ml + r), o_at = ptx::smem_u32(mrg + r * RS + d);
+    float m[KA_CLUSTER], ls[KA_CLUSTER], m_max = -CUDART_INF_F;
+    float4 v[KA_CLUSTER];
+#pragma unroll
+    for (int x = 0; x < KA_CLUSTER; ++x) {
+      m[x] = -CUDART_INF_F; ls[x] = 0.f; v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (x < n_parts) {
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m[x]), "=f"(ls[x]) : "r"(ptx::map_to_cta(ml_at, x)) : "memory");
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(v[x].x), "=f"(v[x].y), "=f"(v[x].z), "=f"(v[x].w) : "r"(ptx::map_to_cta(o_at, x)) : "memory");
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < KA_CLUSTER; ++x) m_max = fmaxf(m_max, m[x]);
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < KA_CLUSTER; ++x) {
+      if (x < n_parts) {
+        const float f = m_max == -CUDART_INF_F ? 1.f : ptx::ex2_approx(m[x] - m_max);
+        l = fmaf(ls[x], f, l);
+        o.x = fmaf(v[x].x, f, o.x); o.y = fmaf(v[x].y, f, o.y); o.z = fmaf(v[x].z, f, o.z); o.w = fmaf(v[x].w, f, o.w);
+      }
+    }
+    store_out(out_row(r), d, o, l);
+  }
+  __syncwarp();
+  ptx::cluster_sync_all();  // nobody leaves before its rows are read
 }
 
-template <int HD, int WARPS, int NC, bool MULTI>
+template <int HD, int WARPS, int NC, bool MULTI, bool TOGETHER>
 pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, cudaStream_t s) {
   using SM = Kv4Smem<HD, WARPS, NC>;
+  const auto kernel = kv4_decode_kernel<HD, WARPS, NC, MULTI, TOGETHER>;
   static PerDeviceInt smem_opt_in;
-  PD_TRY(opt_in_smem(smem_opt_in, kv4_decode_kernel<HD, WARPS, NC, MULTI>, SM::BYTES));
-  PD_CUDA_TRY(launch_pdl(kv4_decode_kernel<HD, WARPS, NC, MULTI>, dim3(a.col_blocks * a.n_kv_heads, batch, a.n_splits), dim3(WARPS * 32), SM::BYTES, s, a));
+  PD_TRY(opt_in_smem(smem_opt_in, kernel, SM::BYTES));
+  const dim3 grid(a.col_blocks * a.n_kv_heads, batch, a.n_splits), block(WARPS * 32);
+  if (TOGETHER) {
+    PD_CUDA_TRY(launch_pdl_cluster(kernel, grid, block, dim3(1, 1, a.n_splits), SM::BYTES, s, a));
+  } else {
+    PD_CUDA_TRY(launch_pdl(kernel, grid, block, SM::BYTES, s, a));
+  }
   count_launch();
-  if (a.n_splits > 1) return launch_paged_join(a.parts, a.o, 1ll * a.rows * a.n_q_heads, a.n_splits, HD, s);
+  if (!TOGETHER && a.n_splits > 1) return launch_paged_join(a.parts, a.o, 1ll * a.rows * a.n_q_heads, a.n_splits, HD, s);
   return PD_OK;
 }
+template <int HD, int WARPS, int NC>
+pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, bool together, cudaStream_t s) {
+  if (a.n_new > 1) return together ? launch_kv4<HD, WARPS, NC, true, true>(a, batch, s) : launch_kv4<HD, WARPS, NC, true, false>(a, batch, s);
+  return together ? launch_kv4<HD, WARPS, NC, false, true>(a, batch, s) : launch_kv4<HD, WARPS, NC, false, false>(a, batch, s);
+}
+struct Split { int n, chunk, warps; bool together; };
 template <int HD>
-pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int col_groups, int warps, cudaStream_t s) {
-  if (col_groups == 2) return a.n_new > 1 ? launch_kv4<HD, 4, 2, true>(a, batch, s) : launch_kv4<HD, 4, 2, false>(a, batch, s);
-  if (a.n_new > 1) return warps == 4 ? launch_kv4<HD, 4, 1, true>(a, batch, s) : launch_kv4<HD, 8, 1, true>(a, batch, s);
-  return warps == 4 ? launch_kv4<HD, 4, 1, false>(a, batch, s) : launch_kv4<HD, 8, 1, false>(a, batch, s);
+pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int col_groups, const Split& sp, cudaStream_t s) {
+  if (col_groups == 2) return launch_kv4<HD, 4, 2>(a, batch, sp.together, s);
+  return sp.warps == 4 ? launch_kv4<HD, 4, 1>(a, batch, sp.together, s) : launch_kv4<HD, 8, 1>(a, batch, sp.together, s);
 }
 
 // Key ranges are cut into equal parts while there are fewer blocks than run together, into parts of at least KA_MIN_CHUNK keys
@@ -617,7 +674,11 @@ pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int col_groups, int warp
 // parts are made for the length alone, since max_kv_len may be a capacity far above the lengths.
 // Blocks have 4 warps, which costs a short stream of tiles less at both ends (256 sequences of 2304 keys: 122 us, 134 with 8), or 8 where
 // the keys of a block are cut into many parts, of which there are half as many to join (one sequence of 32768 keys: 19 and 17 us).
-struct Split { int n, chunk, warps; };
+// Up to KA_CLUSTER parts that all run at once, with some room (a cluster's blocks need places in one part of the GPU), are a cluster
+// and join in shared memory instead of in a kernel of their own (8 sequences of 2,000 keys: 10.6 and 8.7 us; 16 of 1,000: 10.7 and 9.0; 18
+// of 3,000, 97 % of what runs at once: 21.2 and 24.0), and nine or ten parts are made eight for it (4 of 4,000: 10.8 and 9.1; two of 4,000,
+// sixteen made eight: 7.6 and 8.7).  Where more blocks than that wait for a place, blocks that end one by one are
+// better (24 ragged sequences: 30 and 42 us).
 constexpr int KA_FEW_BLOCKS = 74, KA_MORE_PARTS = 2;
 Split kv4_split(long long blocks, int col_groups, int batch, int max_kv_len) {
   Split sp;
@@ -627,9 +688,14 @@ Split kv4_split(long long blocks, int col_groups, int batch, int max_kv_len) {
   const long long want = std::max(1ll, most / blocks);
   long long chunk = (max_kv_len + want - 1) / want;
   chunk = std::min(chunk, batch > 1 ? std::max(4096ll, max_kv_len / 16ll) : static_cast<long long>(max_kv_len));
-  chunk = std::min((std::max<long long>(chunk, KA_MIN_CHUNK) + 63) / 64 * 64, 0x7fffffc0ll);
-  sp.n = static_cast<int>((max_kv_len + chunk - 1) / chunk);
+  auto in_steps = [](long long keys) { return std::min((std::max<long long>(keys, KA_MIN_CHUNK) + 63) / 64 * 64, 0x7fffffc0ll); };
+  auto parts = [&] { return (max_kv_len + chunk - 1) / chunk; };
+  chunk = in_steps(chunk);
+  auto fits = [&](long long n) { return blocks * n * 8 <= resident * 7; };
+  if (parts() > KA_CLUSTER && parts() <= KA_CLUSTER * 5 / 4 && fits(KA_CLUSTER)) chunk = in_steps((max_kv_len + KA_CLUSTER - 1) / KA_CLUSTER);
+  sp.n = static_cast<int>(parts());
   sp.chunk = static_cast<int>(chunk);
+  sp.together = sp.n > 1 && sp.n <= KA_CLUSTER && fits(sp.n);
   return sp;
 }
 // (part, row) pairs, row = (token, query head), that any call of up to these sizes has at most, where it has parts at all: a
@@ -687,5 +753,5 @@ extern "C" pd_status pd_paged_kv4_decode_attention(const pd_layer_cfg* cfg, cons
   a.ldq = ldq; a.n_new = n_new; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   TraceScope ts(PD_K_ATTN_DECODE, st);
-  return cfg->head_dim == 128 ? launch_kv4<128>(a, B, col_groups, sp.warps, st) : launch_kv4<64>(a, B, col_groups, sp.warps, st);
+  return cfg->head_dim == 128 ? launch_kv4<128>(a, B, col_groups, sp, st) : launch_kv4<64>(a, B, col_groups, sp, st);
 }

@@ -83,6 +83,36 @@ def test_long_sequence(pdlib, hq, hkv, hd, page_len, n, n_new):
     check(c, hq, q, kv_len, alone, n_new)
 
 
+@pytest.mark.parametrize("n_new", [1, 3])
+@pytest.mark.parametrize("hq,hkv,hd", [(8, 2, 128), (32, 8, 64)])
+def test_parts_that_join_in_either_way(pdlib, n_new, hq, hkv, hd):
+    """The same rows with keys cut into one part to more than ten (a bound of 256 keys each), few sequences and among many that pad:
+    parts without keys, with a NaN that the last token alone sees, and a sequence that reaches past the bound."""
+    lens = [2000, 60, 700, 257]
+    c = Cache4(pdlib, hkv, hd, 64, lens, seed=16).fill(lens, np.random.default_rng(16), 0.5)
+    c.table = np.pad(c.table, ((0, 60), (0, 64 - c.width)), constant_values=-1)
+    c.width = 64
+    k_nan, v_nan = (c.table[0, 1999 // 64], 0, 1999 % 64, 1), (c.table[2, 699 // 64], 1, 699 % 64, 2)
+    kv_len = [n - n_new for n in lens]
+    q = queries(76, 64, n_new, hq, hd)
+    for broken in (False, True):
+        if broken:
+            c.ks[k_nan] = c.vs[v_nan] = 0x7F
+        c.upload()
+        bad = np.zeros((4, n_new, hq, hd), bool)
+        group = hq // hkv
+        if broken:
+            bad[0, -1, :group] = True
+            bad[2, -1, group:2 * group, 32:48] = True
+        for pads in (0, 60):
+            for most in (256, 512, 1100, 2000, 2048, 2300, 2560, 2817, 4096):
+                got = decode(pdlib, c, hq, q[:4 + pads], kv_len + [-1] * pads, n_new, max_kv=most)
+                assert not got[4:].any()
+                np.testing.assert_array_equal(np.isnan(got[:4]), bad, err_msg=f"{pads} {most}")
+                if not broken:
+                    check(c, hq, q[:4], kv_len, got[:4], n_new)
+
+
 def test_sizes_far_apart_and_large_queries(pdlib):
     """Values of V over many octaves, queries from 1e-20 to 1e20 (the softmax is then one-hot or flat), zeros."""
     hq, hkv, hd = 8, 2, 64
