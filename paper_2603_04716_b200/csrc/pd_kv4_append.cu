@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(KW_THREADS, STEPS == 4 ? 8 : 5) kv4_append_ker
   const int len = a.kv_len[req];
   if (len < 0 || row < first) return;  // a request that is left out (and never with consistent inputs)
   const uint32_t pos = static_cast<uint32_t>(len) + static_cast<uint32_t>(row - first);
-  if (pos >= (a.t.rot > 0 ? static_cast<uint32_t>(a.t.n_pos) : 0x80000000u)) {
+  if (a.t.rot > 0 && pos >= static_cast<uint32_t>(a.t.n_pos)) {
     report_place(a.err_word);
     return;
   }

@@ -180,6 +180,18 @@ def test_rows_without_a_place(pdlib):
             assert (np.abs(q[3:] - y) <= transform_bound(y, mag)).all()
 
 
+def test_rows_behind_the_last_position(pdlib):
+    """Positions 2^31 - 1 and 2^31 have no place; without a rotation table their q is there all the same."""
+    import torch
+    c, t = Cache4(pdlib, 2, 64, 16, [32], seed=13).upload(), Transform(pdlib, 64, 0, 0)
+    x, err = rows_of(12, 2, 4, 2, 64), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = append(pdlib, c, t, x, [2 ** 31 - 1], cu=[0, 2], err=err)
+    assert int(err.item()) == 2
+    y, mag = t.q(x[:, :4], [0, 0])
+    assert (np.abs(q - y) <= transform_bound(y, mag)).all()
+    c.assert_equal()
+
+
 # ------------------------------------------------------------------------------------------------------ read and write
 @pytest.mark.parametrize("hkv,hd,page_len", [(2, 64, 16), (8, 128, 64), (1, 128, 32), (3, 64, 128)])
 def test_read_back(pdlib, hkv, hd, page_len):
