@@ -679,7 +679,8 @@ pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int col_groups, const Sp
 // of 3,000, 97 % of what runs at once: 21.2 and 24.0), and nine or ten parts are made eight for it (4 of 4,000: 10.8 and 9.1; two of 4,000,
 // sixteen made eight: 7.6 and 8.7).  Where more blocks than that wait for a place, blocks that end one by one are
 // better (24 ragged sequences: 30 and 42 us).
-constexpr int KA_FEW_BLOCKS = 74, KA_MORE_PARTS = 2;
+// The kernel that joins reads KA_JOIN_ROUND parts at a time, so a few more are made as many (one of 32,768: 37 parts 17.4 us, 32 parts 16.4).
+constexpr int KA_FEW_BLOCKS = 74, KA_MORE_PARTS = 2, KA_JOIN_ROUND = 32;
 Split kv4_split(long long blocks, int col_groups, int batch, int max_kv_len) {
   Split sp;
   sp.warps = col_groups == 1 && blocks <= KA_FEW_BLOCKS ? 8 : 4;
@@ -692,7 +693,8 @@ Split kv4_split(long long blocks, int col_groups, int batch, int max_kv_len) {
   auto parts = [&] { return (max_kv_len + chunk - 1) / chunk; };
   chunk = in_steps(chunk);
   auto fits = [&](long long n) { return blocks * n * 8 <= resident * 7; };
-  if (parts() > KA_CLUSTER && parts() <= KA_CLUSTER * 5 / 4 && fits(KA_CLUSTER)) chunk = in_steps((max_kv_len + KA_CLUSTER - 1) / KA_CLUSTER);
+  for (const int n : {KA_CLUSTER, KA_JOIN_ROUND})
+    if (parts() > n && parts() <= n * 5 / 4 && (n > KA_CLUSTER || fits(n))) chunk = in_steps((max_kv_len + n - 1ll) / n);
   sp.n = static_cast<int>(parts());
   sp.chunk = static_cast<int>(chunk);
   sp.together = sp.n > 1 && sp.n <= KA_CLUSTER && fits(sp.n);
