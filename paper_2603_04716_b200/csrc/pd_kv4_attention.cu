@@ -13,8 +13,8 @@
 // follows the maximum lazily, so a tile costs one vote instead of a reduction over its keys.  Softmax statistics and O are fp32.
 // A tile of 32 keys costs a warp 565 instructions (128 conversions, 128 products with scales, 32 MMAs), a warp 660 more at both ends:
 // instructions and their latency bind as much as HBM.  Measured, heads of 128: 256 sequences of 2,304 keys, 32 / 8 heads (640 MB)
-// 117 to 131 us, 4.9 to 5.5 TB/s; each 1,024 keys more cost 52 us (5.8 TB/s), and pages shared in L2 take the same time.  24 sequences of
-// 100 to 4,351 keys, two tokens, 64 / 8 heads 30 us; one of 32,768 keys 17.
+// 117 to 137 us with the machine's clock, 4.7 to 5.5 TB/s; each 1,024 keys more cost 52 us (5.8 TB/s), and pages shared in L2 take the same time.  24 sequences of
+// 100 to 4,351 keys, two tokens, 64 / 8 heads 30 us; one of 32,768 keys 16.4.
 #include <math_constants.h>
 
 #include <algorithm>
@@ -673,7 +673,7 @@ pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int col_groups, const Sp
 // blocks: 42 us with half as many again, 37 with twice as many; 64 sequences of 2000 keys, 512 blocks: 36 and 41).  No more than 16
 // parts are made for the length alone, since max_kv_len may be a capacity far above the lengths.
 // Blocks have 4 warps, which costs a short stream of tiles less at both ends (256 sequences of 2304 keys: 122 us, 134 with 8), or 8 where
-// the keys of a block are cut into many parts, of which there are half as many to join (one sequence of 32768 keys: 19 and 17 us).
+// the keys of a block are cut into many parts, of which there are half as many to join (one sequence of 32768 keys: 19 and 17 us, in 37 parts).
 // Up to KA_CLUSTER parts that all run at once, with some room (a cluster's blocks need places in one part of the GPU), are a cluster
 // and join in shared memory instead of in a kernel of their own (8 sequences of 2,000 keys: 10.6 and 8.7 us; 16 of 1,000: 10.7 and 9.0; 18
 // of 3,000, 97 % of what runs at once: 21.2 and 24.0), and nine or ten parts are made eight for it (4 of 4,000: 10.8 and 9.1; two of 4,000,
