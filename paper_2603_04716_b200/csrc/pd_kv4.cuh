@@ -379,7 +379,17 @@ __device__ __forceinline__ void store_kv4(const float (&t)[8], int exp, const He
   const float unit = pow2f(exp), inv_unit = pow2f(-exp);
   // (toward zero: a finite value stays one, and an infinite one stays infinite)
   const uint32_t s0 = kv4_scale(__fmul_rz(amax[0], inv_unit)), s1 = PAIRS ? s0 : kv4_scale(__fmul_rz(amax[1], inv_unit));
-  const uint32_t c = kv4_codes(t, e4m3_value(s0) * unit, e4m3_value(s1) * unit);
+  // Values beyond 8 times the largest scale have the largest code whatever they are.  They are held to that where their quotients
+  // would leave fp32: the remainder of an infinite one is infinite with the other sign, and the code would lose it.
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = t[e];
+  if (exp < -8) {
+    const float most = 8.f * 448.f * unit;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fminf(fmaxf(v[e], -most), most);
+  }
+  const uint32_t c = kv4_codes(v, e4m3_value(s0) * unit, e4m3_value(s1) * unit);
   if (PAIRS) {
     *reinterpret_cast<uint32_t*>(codes + at.a / 2) = c;
     if ((j & 1) == 0) scales[j / 2] = static_cast<uint8_t>(s0);
