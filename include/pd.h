@@ -562,7 +562,7 @@ pd_status pd_qk_norm_rope(const pd_layer_cfg* cfg, const pd_qk_transform* transf
  *   page_len            16, 32, 64 or 128;  table_ld * page_len below 2^31, n_pages * Hkv * page_len at most 2^32 - 1
  * value = code * scale * 2^exp[head].  Of 16 neighbouring features x, in units of 2^exp: scale = E4M3(max|x| / 6), saturating at
  * 448, code = E2M1(x / scale), saturating at 6, both rounded to nearest even from the exact quotient; a scale of 0 has codes of
- * 0.  So magnitudes from 2^-10 to 2688 times 2^exp are represented, and 16 features none of which exceeds 6 * 2^-10 times 2^exp are
+ * 0, under any other a negative x that rounds to 0 keeps its sign (code 8), and a zero of either sign is code 0.  So magnitudes from 2^-10 to 2688 times 2^exp are represented, and 16 features none of which exceeds 6 * 2^-10 times 2^exp are
  * stored as zeros.  16 features of which one is infinite or NaN are stored as
  * NaN (a scale of NaN).  A row has scales of its own: appending touches no other row, and rows may be appended again, in any
  * order.  A value has six significant bits: reading back to bf16 is exact.

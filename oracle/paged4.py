@@ -5,7 +5,8 @@ TEST INFRASTRUCTURE ONLY: shares no code with the CUDA path.  numpy, float64.
   * cache: K (or V) codes uint8 [n_pages, Hkv, page_len, hd / 2], two E2M1 codes a byte (feature 2 i in bits 0-3), scales uint8
     [n_pages, Hkv, page_len, hd / 16] in E4M3, one power of two per head; value = code * scale * 2^exp;
   * of 16 neighbouring values x in units of 2^exp: scale = E4M3(max|x| / 6), code = E2M1(x / scale), nearest, ties to even, both
-    saturating, decided by comparing x with exact borders; 16 values of which one is not finite have a scale of NaN;
+    saturating, decided by comparing x with exact borders; 16 values of which one is not finite have a scale of NaN; a code has the
+    sign of a negative x, but under a scale of 0 all codes are 0;
   * transform of a head: x * rsqrt(mean x^2 + eps) * gain, then (a, b) -> (a c - b s, b c + a s) of the pairs of its first features.
 
 Pins: tests/test_oracle_paged4.py.
@@ -52,7 +53,7 @@ def quantise(x):
         out[i:i + 4096] = _place(flat[i:i + 4096], np.full(flat[i:i + 4096].shape, 6.0), e4m3)
     s = e4m3[scales]
     mag = np.where(s[..., None] > 0, _place(np.abs(b), np.where(s > 0, s, 1.0)[..., None] * np.ones(GROUP), E2M1), 0)
-    codes = (mag | (np.signbit(b) << 3)).astype(np.uint8).reshape(x.shape)
+    codes = (mag | (((b < 0) & (s[..., None] > 0)) << 3)).astype(np.uint8).reshape(x.shape)
     return codes[..., 0::2] | (codes[..., 1::2] << 4), np.where(fine, scales, E4M3_NAN).astype(np.uint8)
 
 

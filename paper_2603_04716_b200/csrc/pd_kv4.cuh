@@ -340,7 +340,8 @@ __device__ __forceinline__ uint32_t kv4_codes(const float (&t)[8], float scale0,
     const uint64_t inv2 = dup_f32x2(inv), neg2 = dup_f32x2(-scale);
 #pragma unroll
     for (int e = 4 * h; e < 4 * h + 4; e += 2) {
-      const uint64_t v = ptx::pack_f32x2(t[e], t[e + 1]), p = ptx::mul_f32x2(v, inv2);
+      // (a zero added: 0 is +0 whatever the sign of t)
+      const uint64_t v = ptx::pack_f32x2(t[e], t[e + 1]), p = ptx::fma_f32x2(v, inv2, dup_f32x2(0.f));
       ptx::unpack_f32x2(ptx::fma_f32x2(ptx::fma_f32x2(p, neg2, v), inv2, p), q[e], q[e + 1]);
     }
   }

@@ -55,3 +55,44 @@ def test_values_beyond_the_largest_keep_their_sign(pdlib, hd, exps):
     c = cache(pdlib, hd, exps)
     write(pdlib, c, x[:, HKV:2 * HKV], x[:, 2 * HKV:])
     c.assert_equal("write")
+
+
+def small(hd):
+    """Zeros and values that round to 0, of either sign: in groups whose scale is 0, in groups with ordinary values, -0 itself."""
+    rng = np.random.default_rng(hd + 1)
+    x = rows_of(4, N, HKV, HKV, hd).reshape(N, -1, hd // 16, 16)
+    sign = np.where(rng.random(x.shape) < 0.5, -1.0, 1.0).astype(np.float32)
+    x[:10] = 1e-5 * sign[:10]                                      # below 6 * 2^-10: a scale of 0
+    x[10:20, ..., :8] = 1e-3 * sign[10:20, ..., :8]                # below a quarter of a scale
+    x[20:25] = 0.0 * sign[20:25]
+    x[25:30, ..., ::2] = 0.0 * sign[25:30, ..., ::2]
+    x[30:34, ..., ::5] = 1e-40 * sign[30:34, ..., ::5]             # (not normal in fp32)
+    x[34] = 6 * 2.0 ** -10 * sign[34]                              # on the border to the smallest scale
+    return gen.bf16_round(x.reshape(N, -1, hd))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_codes_of_zeros(pdlib, hd):
+    """The bytes themselves: a scale of 0 has codes of 0, under any other a negative value that rounds to 0 keeps its sign, and a
+    zero of either sign is code 0."""
+    for exps in ((0, 1), (-4, 3)):
+        x = small(hd)
+        x[:, HKV:] = gen.bf16_round(x[:, HKV:] * np.exp2(np.array(exps * 2))[:, None].astype(np.float32))
+        for pairs, rot in ((False, 0), (True, 0), (False, hd), (True, hd // 2)):
+            c, t = cache(pdlib, hd, exps), Transform(pdlib, hd, rot, N, pairs, gains=False)
+            append(pdlib, c, t, x, [0], [0, N], q=False)
+            expect(c, t, x, [0], [0, N])
+            check_bytes(c)
+        c = cache(pdlib, hd, exps)
+        write(pdlib, c, x[:, HKV:2 * HKV], x[:, 2 * HKV:])
+        check_bytes(c)
+
+
+def check_bytes(c):
+    for d, ds, h, hs in ((c.dk, c.dks, c.k, c.ks), (c.dv, c.dvs, c.v, c.vs)):
+        got, scales = d.cpu().numpy(), ds.cpu().numpy()
+        np.testing.assert_array_equal(scales, hs)
+        zero = np.repeat(hs == 0, 8, axis=-1)
+        assert zero.any() and not got[zero].any()
+        live = np.repeat((hs & 0x7F) != 0x7F, 8, axis=-1)
+        np.testing.assert_array_equal(got[live], h[live])
