@@ -502,8 +502,9 @@ pd_status pd_paged_prefill_attention(const pd_layer_cfg* cfg, const void* q, int
  *   PD_ROPE_SCALE_TURNS   w f_i + (1 - w) f_i / factor, w = (n_i - low) / (high - low) within 0 .. 1, where
  *                         n_i = trained_len * f_i / (2 pi) is how often pair i turns within the trained length
  *   PD_ROPE_SCALE_INDEX   the same with w = 1 - (i - a) / (b - a) within 0 .. 1, where a = max(floor(I(high)), 0),
- *                         b = min(ceil(I(low)), rot_dim/2 - 1), I(n) = rot_dim ln(trained_len / (2 pi n)) / (2 ln theta) is the
- *                         (fractional) pair that turns n times; b - a below 0.001 counts as 0.001
+ *                         b = min(ceil(I(low)), rot_dim - 1), I(n) = rot_dim ln(trained_len / (2 pi n)) / (2 ln theta) is the
+ *                         (fractional) pair that turns n times; b - a below 0.001 counts as 0.001.  (b may lie behind the last
+ *                         pair, which then keeps a part of its own frequency)
  * and the table holds magnitude * cos and magnitude * sin of position * f_i. */
 enum { PD_ROPE_SCALE_NONE = 0, PD_ROPE_SCALE_LINEAR = 1, PD_ROPE_SCALE_BASE = 2, PD_ROPE_SCALE_TURNS = 3, PD_ROPE_SCALE_INDEX = 4 };
 typedef struct {

@@ -97,7 +97,7 @@ def frequencies(rot: int, theta: float, scaling: str = "none", factor: float = 1
     if scaling == "index":
         def pair(turns):
             return rot * np.log(trained_len / (2 * np.pi * turns)) / (2 * np.log(theta))
-        a, b = max(np.floor(pair(high)), 0), min(np.ceil(pair(low)), rot // 2 - 1)
+        a, b = max(np.floor(pair(high)), 0), min(np.ceil(pair(low)), rot - 1)
         w = 1 - np.clip((i - a) / max(b - a, 1e-3), 0, 1)
         return w * f + (1 - w) * f / factor
     return f

@@ -56,7 +56,7 @@ void rope_frequencies(const pd_rope_cfg& r, double* f) {
   if (r.scaling == PD_ROPE_SCALE_INDEX) {
     auto pair_of = [&](double turns) { return r.rot_dim * std::log(r.trained_len / (2 * pi * turns)) / (2 * std::log(theta)); };
     a = std::fmax(std::floor(pair_of(r.high)), 0.0);
-    b = std::fmin(std::ceil(pair_of(r.low)), pairs - 1.0);
+    b = std::fmin(std::ceil(pair_of(r.low)), r.rot_dim - 1.0);  // (behind the last pair: the slowest keeps a part)
   }
   for (int i = 0; i < pairs; ++i) {
     f[i] = std::pow(theta, -2.0 * i / r.rot_dim);
