@@ -631,7 +631,8 @@ pd_status pd_paged_kv4_read(const pd_layer_cfg* cfg, const pd_paged_kv4_cache* c
  *   err_word      optional device int32, set to 2 where a sequence reaches past the table or a page number lies outside the pool
  *                 (the keys of such a page are left out)
  * A key stored as NaN makes the rows that see it NaN, a value their 16 features of it; rows in front of it are not touched.
- * Roundings: K, V and q are exact (q down to 2^-24 of its row's largest entry; |q| below 2^90); a weight of the softmax is off by
+ * |q| * 2^k_exp stays below 2^110 (scores of larger ones leave fp32, and the rows may be NaN).
+ * Roundings: K, V and q are exact (q down to 2^-24 of its row's largest entry); a weight of the softmax is off by
  * 2^-11 of itself, or by 2^-32 of its row's largest where that is more; sums are fp32.  The result does not depend on the order in which the GPU does the work.
  * Only the head counts and head_dim of cfg are used.  Only enqueues work. */
 pd_status pd_paged_kv4_decode_attention_workspace_bytes(const pd_layer_cfg* cfg, int32_t B, int32_t n_new, int32_t max_kv_len,
