@@ -658,10 +658,11 @@ pd_status pd_test_inject_wait_timeout(int32_t kernel_kind, uint64_t wait_limit_n
 int64_t pd_launch_count(void);
 
 /* Optional per-kernel-class timing for roofline reports.  Between pd_trace_begin and
- * pd_trace_end every kernel the calling thread launches through the layer calls is bracketed
- * by a pair of CUDA events on its stream; pd_trace_end waits for them and sums the elapsed
+ * pd_trace_end every kernel the calling thread launches through the layer calls, and through the calls around
+ * the paged KV caches, is bracketed by a pair of CUDA events on its stream; pd_trace_end waits for them and sums the elapsed
  * time and the launch count per class.  Tracing adds two event records per kernel, so a
- * traced pass is for attribution, not for the headline time. */
+ * traced pass is for attribution, not for the headline time.  Norms of q and k heads count as PD_K_RMSNORM, everything that
+ * writes or reads a cache without attending as PD_K_KV_APPEND; rotary tables are made ahead of a step and left out. */
 #define PD_TRACE_CLASSES 16
 enum {
   PD_K_GEMM_QKV = 0, PD_K_GEMM_O = 1, PD_K_GEMM_GATE_UP = 2, PD_K_GEMM_DOWN = 3, PD_K_ATTN_PREFILL = 4,

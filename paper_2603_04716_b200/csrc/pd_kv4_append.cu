@@ -363,6 +363,7 @@ extern "C" pd_status pd_paged_kv4_read(const pd_layer_cfg* cfg, const pd_paged_k
   const dim3 grid((max_len + (rows - 1ll)) / rows, cfg->n_kv_heads, n_seqs), block(KW_THREADS);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & 31u) == 0;
+  TraceScope ts(PD_K_KV_APPEND, st);
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, st, a); };
   PD_CUDA_TRY(cfg->head_dim == 128 ? (wide ? go(kv4_read_kernel<128, true>) : go(kv4_read_kernel<128, false>))
                                    : (wide ? go(kv4_read_kernel<64, true>) : go(kv4_read_kernel<64, false>)));

@@ -174,6 +174,7 @@ extern "C" pd_status pd_qk_norm_rope(const pd_layer_cfg* cfg, const pd_qk_transf
   const int y = a.q_blocks + (k_out ? (cfg->n_kv_heads + heads - 1) / heads : 0);
   const dim3 grid((T + (NR_WARPS - 1ll)) / NR_WARPS, y), block(NR_WARPS * 32);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  TraceScope ts(PD_K_RMSNORM, st);
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, st, a); };
   const bool pairs = transform->layout == PD_ROPE_PAIRS;
   PD_CUDA_TRY(hd == 128 ? (pairs ? go(qk_norm_rope_kernel<128, true>) : go(qk_norm_rope_kernel<128, false>))
