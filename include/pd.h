@@ -547,7 +547,8 @@ typedef struct {
  *   positions  device int32 [T]; a negative one leaves its row out (nothing is written)
  *   err_word   optional device int32, set to 2 where a position lies beyond the table (the row is left out)
  * Outputs that overlap qkv in any other way, or each other, are undefined.  Tensors start on 16-byte boundaries, pitches are
- * multiples of 8.  fp32 arithmetic, rounded once; the squares of a head must sum to less than 3e38.  Only head_dim and the head counts of cfg
+ * multiples of 8.  fp32 arithmetic, rounded once; with a norm the squares of a head must
+ * sum to less than 3e38, and mean(x^2) + eps be 1e-36 at least unless the head is zero.  Only head_dim and the head counts of cfg
  * are used.  Enqueues one kernel; T = 0 does nothing. */
 pd_status pd_qk_norm_rope(const pd_layer_cfg* cfg, const pd_qk_transform* transform, const void* qkv, int32_t ldqkv, void* q_out,
                           int32_t ldq_out, void* k_out, int32_t ldk_out, const int32_t* positions, int32_t T, int32_t* err_word,

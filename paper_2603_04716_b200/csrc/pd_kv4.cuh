@@ -1,6 +1,8 @@
 // What the kernels of the 4-bit paged KV cache share: the cache as kernels see it, host-side argument checks, the transform of q
 // and k heads (norm, rotation) and the quantiser.
 #pragma once
+#include <algorithm>
+#include <limits>
 #include <type_traits>
 
 #include "pd_common.cuh"
@@ -67,6 +69,7 @@ struct QkTransform {
   const bf16* q_gain;      // [hd] or NULL
   const bf16* k_gain;
   double eps;
+  float eps_fast;          // of the fp32 transform: eps above 0 stays above 0, so that a head of zeros stays one
   int n_pos, rot;          // rot = 0 without a table
 };
 inline pd_status qk_transform_view(const pd_qk_transform* t, const pd_layer_cfg* cfg, QkTransform* out) {
@@ -77,7 +80,9 @@ inline pd_status qk_transform_view(const pd_qk_transform* t, const pd_layer_cfg*
     return PD_ERR_INVALID_ARG;
   out->table = reinterpret_cast<const float2*>(t->table);
   out->q_gain = static_cast<const bf16*>(t->q_gain); out->k_gain = static_cast<const bf16*>(t->k_gain);
-  out->eps = t->eps; out->n_pos = 0; out->rot = 0;
+  out->eps = t->eps;
+  out->eps_fast = t->eps > 0.0 ? std::max(static_cast<float>(t->eps), std::numeric_limits<float>::denorm_min()) : 0.f;
+  out->n_pos = 0; out->rot = 0;
   if (t->table) {
     if (t->n_pos <= 0 || t->rot_dim <= 0 || t->rot_dim > cfg->head_dim) return PD_ERR_INVALID_ARG;
     if (t->rot_dim % 16 != 0) return PD_ERR_UNSUPPORTED_SHAPE;

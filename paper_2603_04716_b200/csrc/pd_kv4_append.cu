@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(KW_THREADS, STEPS == 4 ? 8 : 5) kv4_append_ker
       bf16* const dst = a.q_out + (static_cast<size_t>(row) * a.n_q_heads + h0) * HD;
 #pragma unroll 1
       for (int h = 0;;) {
-        transform(w, dst + h * HD, n_heads - h, at, static_cast<float>(a.t.eps));
+        transform(w, dst + h * HD, n_heads - h, at, a.t.eps_fast);
         if ((h += HEADS) >= n_heads) break;
         load_heads<HD, PAIRS>(w, src + h * HD, n_heads - h, at);
       }

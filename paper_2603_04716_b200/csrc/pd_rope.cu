@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(NR_WARPS * 32, 8) qk_norm_rope_kernel(const No
   with_flags(gain != nullptr, a.t.rot == HD, [&](auto norm, auto whole) {
     constexpr bool NORM = decltype(norm)::value, WHOLE = decltype(whole)::value;
     const FastTransform<HD, PAIRS, NORM, WHOLE> transform(at, gain, a.t.table + static_cast<size_t>(pos) * (a.t.rot / 2), j);
-    transform(w, dst, n_heads, at, static_cast<float>(a.t.eps));
+    transform(w, dst, n_heads, at, a.t.eps_fast);
   });
 }
 
