@@ -97,6 +97,7 @@ __device__ __forceinline__ void report_place(int* err_word) {
   if (err_word) atomicExch(err_word, 2);
 }
 
+// Eight bf16 values, in memory order (of a share: of its chunks).
 __device__ __forceinline__ void unpack8(const uint4& v, float* f) {
   f[0] = ptx::bf16_lo(v.x); f[1] = ptx::bf16_hi(v.x);
   f[2] = ptx::bf16_lo(v.y); f[3] = ptx::bf16_hi(v.y);
@@ -236,12 +237,6 @@ struct FastTransform {
   }
 };
 
-// The 8 features of a share in memory order of its chunks.
-__device__ __forceinline__ void unpack_share(const uint4& w, float (&f)[8]) {
-  f[0] = ptx::bf16_lo(w.x); f[1] = ptx::bf16_hi(w.x); f[2] = ptx::bf16_lo(w.y); f[3] = ptx::bf16_hi(w.y);
-  f[4] = ptx::bf16_lo(w.z); f[5] = ptx::bf16_hi(w.z); f[6] = ptx::bf16_lo(w.w); f[7] = ptx::bf16_hi(w.w);
-}
-
 // ---- k, in double.  A product of a gain and a cos or sin has 32 significant bits, its products with a feature 40: all of them are
 // exact, and the factor of the norm comes last.
 template <int HD, bool PAIRS, bool NORM, bool WHOLE>
@@ -253,7 +248,7 @@ struct ExactTransform {
   __device__ __forceinline__ ExactTransform(const HeadShare<PAIRS>& at, const bf16* gain, const float2* angles, int j) {
     turns = WHOLE || at.turns;
     float g[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-    if (NORM) unpack_share(at.load(gain), g);
+    if (NORM) unpack8(at.load(gain), g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) m[e] = static_cast<double>(g[e]);
     if (turns) {
@@ -277,7 +272,7 @@ struct ExactTransform {
   __device__ __forceinline__ void operator()(const uint4& w, double eps, double (&f)[8]) const {
     float x[8];
     double v[8];
-    unpack_share(w, x);
+    unpack8(w, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = static_cast<double>(x[e]);
 #pragma unroll

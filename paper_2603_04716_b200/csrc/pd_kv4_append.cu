@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(KW_THREADS, STEPS == 4 ? 8 : 5) kv4_append_ker
     for (int s = 0; s < STEPS; ++s) {
       if (s * STEP >= n_heads) break;
       float t[8];
-      unpack_share(w[s], t);
+      unpack8(w[s], t);
       store(s, t, plain);
     }
     return;
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(KW_THREADS) kv4_write_kernel(const Kv4CopyArgs
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
     float t[8];
-    unpack_share(w[kv], t);
+    unpack8(w[kv], t);
     store_kv4<HD>(t, kv4_exp(kv ? a.c.v_exp : a.c.k_exp, kvh), at, j, live, nullptr, (kv ? a.c.v : a.c.k) + row * (HD / 2),
                   (kv ? a.c.v_scale : a.c.k_scale) + row * (HD / 16));
   }
