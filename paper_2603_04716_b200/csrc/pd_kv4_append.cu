@@ -8,8 +8,9 @@
 // the prompts below when double throughout took 64.)
 // Bound by a chain of loads (length, page number) at decode sizes; at size reading back is bound by HBM, appending by HBM and
 // by instructions together (two thirds of the issue slots).
-// Measured, 32 + 8 + 8 heads of 128: append of 13,123 rows (284 MB) 59.2 us, 4.8 TB/s; of 256 rows 3.4; of one 2.5; read-back of 24
-// prefixes (625 MB) 99.5 us, 6.3 TB/s.
+// Measured, 32 + 8 + 8 heads of 128: append of 13,123 rows (284 MB) 60 us, 4.7 TB/s; of 256 rows 3.4; of one 2.5; read-back of 24
+// prefixes (625 MB) 99.7 us, 6.3 TB/s; the same prefixes written from a bf16 cache 229 us, 2.7 TB/s (bound by instructions:
+// 77 % of the issue slots, 80 % of the ALU pipe).
 #include "pd_kv4.cuh"
 
 namespace pd {
@@ -42,7 +43,7 @@ __device__ __forceinline__ int request_of(const int32_t* cu, int n_req, int row)
 
 // A warp has a row; blocks along y are groups of query heads, then of K heads, then of V heads, 256 features STEPS times each.  With
 // many rows a warp goes on to further query heads, for what concerns the row (its request, position, angles, gains) is a third of the
-// instructions: 63.3 -> 59.2 us for 13,123 rows of 32 + 8 + 8 heads of 128; with 256 rows it would cost 0.6 of 3.4 us.
+// instructions: 63.3 -> 59.2 us for 13,123 rows of 32 + 8 + 8 heads of 128 (60 now); with 256 rows it would cost 0.6 of 3.4 us.
 constexpr int query_rounds(int steps) { return steps == 4 ? 4 : 1; }
 template <int HD, bool PAIRS, int STEPS>
 __global__ void __launch_bounds__(KW_THREADS, STEPS == 4 ? 8 : 5) kv4_append_kernel(const Kv4AppendArgs a) {
@@ -316,8 +317,8 @@ extern "C" pd_status pd_paged_kv4_append(const pd_layer_cfg* cfg, const pd_qk_tr
   a.qkv = static_cast<const bf16*>(qkv); a.q_out = static_cast<bf16*>(q_out);
   a.cu_seqlens = cu_dev; a.kv_len = kv_len_dev; a.err_word = err_word;
   a.ldqkv = ldqkv; a.n_req = n_req; a.n_tokens = tokens; a.n_q_heads = cfg->n_q_heads; a.n_kv_heads = cfg->n_kv_heads;
-  // few rows: short chains count, so a warp has few heads; many: what concerns a row is done once for many heads (2 throughout: 78 us
-  // for 13,123 rows instead of 63, before the rounds; 4 throughout: 6.3 us for 256 instead of 3.4)
+  // few rows: short chains count, so a warp has few heads; many: what concerns a row is done once for many heads.  Two and four steps, 32 + 8
+  // + 8 heads of 128, in us: 256 rows 3.9 and 6.6, 512 4.9 and 8.3, 1024 8.2 and 9.3, 1280 10.6 and 10.3, 1536 13.7 and 11.2, 4096 33 and 21
   const int steps = tokens <= 1024 ? 2 : 4;
   const int heads = steps * (256 / hd), q_heads = heads * query_rounds(steps), rows = KW_THREADS / 32;
   a.q_blocks = q_out ? (cfg->n_q_heads + q_heads - 1) / q_heads : 0;

@@ -10,11 +10,14 @@
 // is free, so a lane takes hd / 4 neighbouring features of a K row as its share of all k-steps and hd / 8 neighbouring features of
 // four V rows per 16 keys: its scales are a byte or two per row.  Features of two V rows are paired by shifts and masks on whole
 // words before they are converted.  q is scaled by a power of two per head into f16 range.  The reference of the exponent
-// follows the maximum lazily, so a tile costs one vote instead of a reduction over its keys.  Softmax statistics and O are fp32.
+// follows the maximum lazily, so a tile costs one vote instead of a reduction over its keys.  Softmax statistics and O are fp32; weights
+// are f16 in the second product, the operand's type, which is 2^-11 of a weight, an eighth of the result's own rounding (bf16 results
+// differ from those of fp32 weights by 2.4e-4 in norm, and from 64 bits by 1.4e-3 either way).
 // A tile of 32 keys costs a warp 565 instructions (128 conversions, 128 products with scales, 32 MMAs), a warp 660 more at both ends:
 // instructions and their latency bind as much as HBM.  Measured, heads of 128: 256 sequences of 2,304 keys, 32 / 8 heads (640 MB)
-// 117 to 137 us with the machine's clock, 4.7 to 5.5 TB/s; each 1,024 keys more cost 52 us (5.8 TB/s), and pages shared in L2 take the same time.  24 sequences of
-// 100 to 4,351 keys, two tokens, 64 / 8 heads 30 us; one of 32,768 keys 16.4.
+// 118 us in bursts of a few milliseconds at an SM clock of 1,965 MHz (5.4 TB/s), 137 us where calls go on and the power cap holds the
+// clock at 1,690 MHz (4.7 TB/s): 232,000 cycles either way.  In bursts each 1,024 keys more cost 52 us (5.8 TB/s), and pages shared in L2
+// take the same time.  24 sequences of 100 to 4,351 keys, two tokens, 64 / 8 heads 30 us; one of 32,768 keys 16.3.
 #include <math_constants.h>
 
 #include <algorithm>
@@ -666,20 +669,28 @@ pd_status launch_kv4(const Kv4DecodeArgs& a, int batch, int col_groups, const Sp
   return sp.warps == 4 ? launch_kv4<HD, 4, 1>(a, batch, sp.together, s) : launch_kv4<HD, 8, 1>(a, batch, sp.together, s);
 }
 
-// Key ranges are cut into equal parts while there are fewer blocks than run together, into parts of at least KA_MIN_CHUNK keys
-// and at most `longest` keys.  The sequences of a batch may differ in length, which the host does not know, so a part is at most
-// 4096 keys, and from a quarter of the blocks that run together on more parts than would run together even the lengths out: half
-// as many again, or, where they are long enough to be worth their join, twice as many (24 sequences of 100 to 4351 keys, 384
-// blocks: 42 us with half as many again, 37 with twice as many; 64 sequences of 2000 keys, 512 blocks: 36 and 41).  No more than 16
-// parts are made for the length alone, since max_kv_len may be a capacity far above the lengths.
-// Blocks have 4 warps, which costs a short stream of tiles less at both ends (256 sequences of 2304 keys: 122 us, 134 with 8), or 8 where
-// the keys of a block are cut into many parts, of which there are half as many to join (one sequence of 32768 keys: 19 and 17 us, in 37 parts).
+// Key ranges are cut into equal parts while there are fewer blocks than run together, into parts of at least KA_MIN_CHUNK keys.
+// The sequences of a batch may differ in length, which the host does not know, so a part is at most 4096 keys, and from 149
+// blocks on more parts than would run together even the lengths out.  With 16 equal sequences and two tokens, 128 blocks, these cost more than
+// they bring (28 us, 20 without), with 16 ragged ones of up to 4,000 keys less (26 and 29).  They are half as many again, or, for bounds of 4096
+// keys on, twice as many, in us:
+//   bounds of 4,096 keys and more   24 ragged, two tokens 34 and 30   20 of 4,095 keys 32 and 29   40 of 4,095 keys 48 and 45
+//   bounds below                    64 of 2,000 keys 36 and 41        64 of 3,900 keys 63 and 61   64 ragged, to 4,095 keys, 58 and 50
+// so the border is drawn for the sake of short equal sequences.  No more than 16 parts (and what is left) are made for the length
+// alone, since max_kv_len may be a capacity far above the lengths.  A capacity has its price all the same, for parts are cut by it and
+// the join looks at all of them: 256 sequences of 2,304 keys 119 us with that bound, 125 with 4,096, 129 with 8,192 and 151 with
+// 32,768; 24 ragged ones of up to 4,352 keys, two tokens, 31, 42 (8,192) and 62 (32,768); 8 of 2,000 keys 8.8, 12 (4,096) and 19 (32,768).
+// Blocks have 4 warps, which costs a short stream of tiles less at both ends (256 sequences of 2,304 keys 117 to 126 us, 133 with 8; 20 of 4,095 29
+// and 31; but 64 ragged ones 58 and 52), or 8 where the keys of a block are cut into many parts, of which there are half as many to join (one
+// sequence of 32,768 keys 20 us with 4 and 16 with 8; 8 of 8,000 22.8 and 22.2).
 // Up to KA_CLUSTER parts that all run at once, with some room (a cluster's blocks need places in one part of the GPU), are a cluster
 // and join in shared memory instead of in a kernel of their own (8 sequences of 2,000 keys: 10.6 and 8.7 us; 16 of 1,000: 10.7 and 9.0; 18
-// of 3,000, 97 % of what runs at once: 21.2 and 24.0), and nine or ten parts are made eight for it (4 of 4,000: 10.8 and 9.1; two of 4,000,
-// sixteen made eight: 7.6 and 8.7).  Where more blocks than that wait for a place, blocks that end one by one are
+// of 3,000, 97 % of what runs at once: 21.2 and 24.0), and nine or ten parts are made at most eight for it (4 of 4,000: 10.8 and 9.1; two of
+// 4,000, sixteen made eight: 7.6 and 8.7).  Where more blocks than that wait for a place, blocks that end one by one are
 // better (24 ragged sequences: 30 and 42 us).
-// The kernel that joins reads KA_JOIN_ROUND parts at a time, so a few more are made as many (one of 32,768: 37 parts 17.4 us, 32 parts 16.4).
+// The kernel that joins reads KA_JOIN_ROUND parts at a time, so 33 to 40 are made that many at most: one sequence of 32,768 keys, 37
+// parts 17.0 us, 32 parts 16.3; one of 64,000 with 64 / 8 heads 25.7 and 24.7.  (Parts are whole steps of 64 keys, so 36 parts of 256 become 29 of 320: one of
+// 9,000 keys 9.0 us, 9.2 with 29.)
 constexpr int KA_FEW_BLOCKS = 74, KA_MORE_PARTS = 2, KA_JOIN_ROUND = 32;
 Split kv4_split(long long blocks, int col_groups, int batch, int max_kv_len) {
   Split sp;
